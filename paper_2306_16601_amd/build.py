@@ -14,6 +14,7 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
+CACHE_CSRC = os.path.join(HERE, "csrc_cache")        # the paged key/value cache and its attention (include/spmm_cache.h)
 LIB = os.path.join(HERE, "libspmm4x1.so")
 NATIVE = os.path.join(HERE, "_native_call.so")      # CPython entry points of the launch calls (plain C, no GPU code)
 NATIVE_SOURCE = os.path.join(CSRC, "native_call.c")
@@ -32,6 +33,9 @@ STREAM = [64, 32, 16]      # token tiles of the streamed kernel
 WIDE = [(tm, nw, maxs) for tm, nw in ((128, 8), (96, 8), (64, 8), (64, 4), (32, 4)) for maxs in (5, 6, 7, 8)]
 HEADERS = [os.path.join(CSRC, "spmm_internal.h"), os.path.join(CSRC, "spmm_kernels.h"), os.path.join(CSRC, "spmm_wide.h"), os.path.join(CSRC, "team.h"),
            os.path.join(ROOT, "include", "spmm.h")]
+
+CACHE_SOURCES = ["cache_api.cpp", "cache_append.hip", "cache_attend.hip", "cache_pages.hip"]
+CACHE_HEADERS = [os.path.join(CACHE_CSRC, "cache_internal.h"), os.path.join(ROOT, "include", "spmm_cache.h")]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -61,6 +65,11 @@ def units():
     return out
 
 
+def cache_units():
+    """The same of the paged cache."""
+    return [(os.path.splitext(s)[0] + ".o", os.path.join(CACHE_CSRC, s), []) for s in CACHE_SOURCES]
+
+
 def sources():
     return sorted({u[1] for u in units()})
 
@@ -87,7 +96,7 @@ def build_native(verbose: bool = False) -> str:
 
 def build(force: bool = True, verbose: bool = False, jobs: int | None = None) -> str:
     """Compile every source with hipcc (cross-compiles without a GPU) and link the library."""
-    deps = sources() + HEADERS + [NATIVE_SOURCE]
+    deps = sources() + HEADERS + [u[1] for u in cache_units()] + CACHE_HEADERS + [NATIVE_SOURCE]
     if not force and all(os.path.exists(b) and all(os.path.getmtime(b) >= os.path.getmtime(d) for d in deps)
                          for b in (LIB, NATIVE)):
         return LIB
@@ -98,9 +107,9 @@ def build(force: bool = True, verbose: bool = False, jobs: int | None = None) ->
     objdir = OBJDIR + ".%d" % os.getpid()
     os.makedirs(objdir, exist_ok=True)
     try:
-        us = units()
+        us = units() + cache_units()
         # the heaviest objects (pipelined kernels) first
-        us.sort(key=lambda u: 0 if u[0].startswith("cfg_wide_1") else 1 if u[0].startswith(("cfg_1", "cfg_9", "cfg_fed", "cfg_wide")) else 2)
+        us.sort(key=lambda u: 0 if u[0].startswith("cache_attend") else 0 if u[0].startswith("cfg_wide_1") else 1 if u[0].startswith(("cfg_1", "cfg_9", "cfg_fed", "cfg_wide")) else 2)
         cmds = [[hipcc, *HIPCC_FLAGS, *defs, "-x", "hip", "-c", src, "-o", os.path.join(objdir, obj)]
                 for obj, src, defs in us]
         with ThreadPoolExecutor(max_workers=jobs) as pool:

@@ -1,0 +1,177 @@
+"""spmm_cache_append on the device against its definition in 64 bits.
+
+Tolerances: binary32 sums of at most 128 squares, a square root, a division and four products, each off by at most a few units in
+the last place, leave 1e-5 of the largest value that enters a result (a rotation adds two products of either sign); bfloat16
+rounds once (2^-8 of the value), 8 bits to half a step of the scale."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2306_16601_amd as sp
+from cache_reference import Problem
+
+pytestmark = pytest.mark.gpu
+
+
+def expected(p, value, T, q_weight, k_weight, eps, rope, interleaved, positions, padding):
+    """(queries, keys, values) in 64 bits, [T, heads, dim] each; the largest value that enters each of a head's"""
+    x = value.reshape(-1, p.dim, T).transpose(2, 0, 1)
+    q, k, v = np.split(x, [p.q_heads, p.q_heads + p.kv_heads], axis=1)
+
+    def make(y, w):
+        if w is not None:
+            y = y / np.sqrt((y * y).mean(-1, keepdims=True) + eps) * w
+        big = np.abs(y).max(-1, keepdims=True)
+        if rope is not None:
+            half, y = rope.shape[1], y.copy()
+            for t in range(T):
+                if padding[t]:
+                    continue
+                at = positions[t]
+                c, s = (rope[at, :, 0], rope[at, :, 1]) if 0 <= at < rope.shape[0] else (np.full(half, np.nan),) * 2
+                i = slice(0, 2 * half, 2) if interleaved else slice(0, half)
+                j = slice(1, 2 * half, 2) if interleaved else slice(half, 2 * half)
+                a, b = y[t, :, i].copy(), y[t, :, j].copy()
+                y[t, :, i], y[t, :, j] = a * c - b * s, b * c + a * s
+        return y, big
+
+    (q, qb), (k, kb) = make(q, q_weight), make(k, k_weight)
+    q[padding] = 0
+    return q, qb, k, kb, v
+
+
+def run(p, x_type="f32", norm=True, rope_dim=None, interleaved=False, positions=None, rope_len=None, pad=0, stream=None, T=None, offset=0):
+    r = p.rng
+    T = T or max(1, p.tokens)
+    features = (p.q_heads + 2 * p.kv_heads) * p.dim
+    scale, zero = {"f32": (1.0, 0), "s8": (0.03, -5), "u8": (0.03, 120)}[x_type]
+    if x_type == "f32":
+        x = torch.from_numpy(r.standard_normal((features, T + pad), np.float32))
+    else:
+        lo, hi = (-128, 128) if x_type == "s8" else (0, 256)
+        x = torch.from_numpy(r.integers(lo, hi, (features, T + pad)).astype(np.int8 if x_type == "s8" else np.uint8))
+    value = (x[:, :T].double().numpy() - zero) * float(np.float32(scale))
+    qw, kw = (torch.from_numpy(r.uniform(0.5, 1.5, p.dim).astype(np.float32)) if norm else None for _ in range(2))
+    rope = None if rope_dim == 0 else sp.make_rope(rope_len or max(p.lens + [1]), rope_dim or p.dim)
+    seq = np.searchsorted(p.start[1:], np.arange(T), side="right")
+    place = np.array([p.lens[b] - (p.start[b + 1] - t) if b < len(p.news) and t >= p.start[0] else -1 for t, b in enumerate(seq)])
+    padding = place < 0
+    turn = place if positions is None else positions
+    q_ref, qb, k_ref, kb, v_ref = expected(p, value, T, *(None if w is None else w.double().numpy() for w in (qw, kw)), 1e-5,
+                                           None if rope is None else rope.double().numpy(), interleaved, turn, padding)
+
+    cache, batch = p.on_device()
+    before = [None if t is None else t.clone() for t in (p.dk, p.dv, p.dks, p.dvs)]
+    flat = torch.zeros(x.numel() + offset, dtype=x.dtype, device="cuda")
+    flat[offset:] = x.flatten().cuda()
+    dx = flat[offset:].view(x.shape)
+    dev = lambda t: None if t is None else t.cuda()      # noqa: E731
+    how = sp.make_append(p.q_heads, x_type, scale, zero, dev(qw), dev(kw), 1e-5, dev(rope), interleaved,
+                         None if positions is None else torch.from_numpy(np.asarray(positions, np.int32)).cuda())
+    q = torch.full((T, p.q_heads, p.dim), 99.0, dtype=torch.bfloat16, device="cuda")
+    torch.cuda.synchronize()
+    sp.spmm_cache_append(cache, p.layer, batch, dx, T, T + pad, how, q, stream or torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+
+    def near(got, ref, big, tol):
+        assert (np.isnan(got) == np.isnan(ref)).all()
+        with np.errstate(invalid="ignore"):
+            bad = np.abs(got - ref) > tol + 1e-5 * np.broadcast_to(big, ref.shape)
+        assert not bad.any(), (np.argwhere(bad)[:4], got[bad][:4], ref[bad][:4])
+
+    near(q.double().cpu().numpy(), q_ref, qb, 2.0 ** -8 * np.abs(q_ref))
+    # the cache: the new tokens' slots hold what is expected, all others what they held
+    k, v = before[0].double().cpu().numpy(), before[1].double().cpu().numpy()
+    ks, vs = (None if t is None else t.cpu().numpy() for t in before[2:])
+    got_k, got_v = p.dk.cpu(), p.dv.cpu()
+    got_ks, got_vs = (None if t is None else t.cpu().numpy() for t in (p.dks, p.dvs))
+    new = np.zeros((p.layers, p.pages, p.page), bool)
+    for t in range(T):
+        at = place[t]
+        if at < 0 or at // p.page >= p.width or not 0 <= p.table[seq[t], at // p.page] < p.pages:
+            continue
+        page, off = p.table[seq[t], at // p.page], at % p.page
+        new[p.layer, page, off] = True
+        for h in range(p.kv_heads):
+            for got, gs, ref, big in ((got_k[p.layer, page, h, off], got_ks, k_ref[t, h], kb[t, h, 0]), (got_v[p.layer, page, h, :, off], got_vs, v_ref[t, h], 0.0)):
+                got = got.double().numpy()
+                if gs is None:
+                    near(got, ref, big, 2.0 ** -8 * np.abs(ref))
+                else:
+                    s = gs[p.layer, page, h, off]
+                    most = np.abs(ref).max()
+                    assert abs(s - most / 127) <= 2e-5 * max(most, float(big)) / 127 + 1e-12
+                    near(got * s, ref, max(float(big), most), 0.5001 * s)
+    same = lambda a, b: a == b if not a.is_floating_point() else (a == b) | (a.isnan() & b.isnan())     # noqa: E731
+    keep = torch.from_numpy(~new)[:, :, None]
+    assert same(got_k, before[0].cpu())[keep.expand(-1, -1, p.kv_heads, -1)].all()
+    assert same(got_v, before[1].cpu()).transpose(3, 4)[keep.expand(-1, -1, p.kv_heads, -1)].all()
+    if ks is not None:
+        for a, b in ((got_ks, ks), (got_vs, vs)):
+            assert (((a == b) | (np.isnan(a) & np.isnan(b))) | new[:, :, None]).all()
+
+
+HEADS = [(4, 4, 64), (8, 2, 128), (6, 2, 80), (5, 1, 16)]
+
+
+@pytest.mark.parametrize("cache", ["bf16", "s8"])
+@pytest.mark.parametrize("x_type", ["f32", "s8", "u8"])
+@pytest.mark.parametrize("q_heads, kv_heads, dim", HEADS)
+@pytest.mark.parametrize("news, pasts", [([1] * 5, [0, 15, 16, 40, 200]), ([70, 0, 3, 33], [0, 9, 31, 50])])
+def test_heads_and_types(q_heads, kv_heads, dim, news, pasts, x_type, cache):
+    run(Problem(news, pasts, q_heads, kv_heads, dim, 16, cache, seed=21), x_type)
+
+
+@pytest.mark.parametrize("cache", ["bf16", "s8"])
+@pytest.mark.parametrize("norm", [True, False])
+@pytest.mark.parametrize("rope_dim, interleaved", [(0, False), (64, False), (64, True), (32, False), (32, True), (6, False), (2, True)])
+def test_norms_and_rotations(norm, rope_dim, interleaved, cache):
+    run(Problem([40, 5], [3, 100], 4, 2, 64, 32, cache, seed=22), norm=norm, rope_dim=rope_dim, interleaved=interleaved)
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
+def test_page_sizes(page):
+    run(Problem([5, 150], [page - 2, 1], 2, 2, 64, page, seed=23))
+
+
+@pytest.mark.parametrize("x_type", ["f32", "s8"])
+@pytest.mark.parametrize("pad, offset", [(0, 0), (1, 1), (3, 0), (64, 3)])
+def test_pitches_and_addresses(pad, offset, x_type):
+    run(Problem([37, 40], [3, 100], 4, 2, 64, 32, seed=24), x_type, pad=pad, offset=offset)
+
+
+def test_given_positions():
+    p = Problem([6, 20], [3, 7], 4, 2, 64, 16, seed=25)
+    run(p, positions=[int(x) for x in p.rng.integers(0, 30, 26)], rope_len=30)
+
+
+def test_positions_outside_the_table_give_nan():
+    run(Problem([6, 2], [3, 0], 4, 2, 64, 16, seed=26), rope_len=7)
+    run(Problem([3], [3], 4, 2, 64, 16, seed=26), positions=[-1, 2, 9], rope_len=9)
+
+
+def test_padding_and_places_that_are_not_there():
+    p = Problem([4, 1, 40], [0, 0, 0], 2, 1, 64, 16, seed=27)
+    p.lens = [2, 0, 7]
+    run(p)
+    run(Problem([3], [60], 2, 1, 64, 16, seed=28, width=2))
+    p = Problem([30, 3], [0, 5], 2, 1, 64, 16, seed=29)
+    p.table[0, 1] = p.pages + 5         # a page that is not in the pool
+    run(p)
+    run(Problem([3, 4], [5, 0], 2, 1, 64, 16, seed=30, lead=3), T=20)
+
+
+def test_zeros_have_a_scale_of_zero():
+    p = Problem([4], [0], 2, 1, 64, 16, "s8", seed=31)
+    cache, batch = p.on_device()
+    x = torch.zeros((4 * 64, 4), device="cuda")
+    q = torch.empty((4, 2, 64), dtype=torch.bfloat16, device="cuda")
+    sp.spmm_cache_append(cache, 0, batch, x, 4, 4, sp.make_append(2), q, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    page = p.table[0, 0]
+    assert (p.dk[0, page, :, :4] == 0).all() and (p.dks[0, page, :, :4] == 0).all() and (p.dvs[0, page, :, :4] == 0).all()
+
+
+def test_second_layer_other_stream():
+    p = Problem([9, 2], [50, 9], 4, 2, 64, 32, layers=3, layer=1, seed=32)
+    run(p, stream=torch.cuda.Stream().cuda_stream)

@@ -1,0 +1,205 @@
+"""spmm_cache_attend on the device against its definition in 64 bits (cache_reference.py).
+
+Tolerance, per value: weights are rounded to bfloat16 once (unit roundoff 2^-8), so the result is off by at most 2^-8 sum p |v|;
+a bfloat16 result by another 2^-8 of itself, an 8-bit one by half a step.  Scores, exponentials and sums in binary32: a relative
+1e-4 of sum p |v| covers scores up to 100 at these sizes (2^-24 times a few operations times 100, on both sides of the softmax)."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2306_16601_amd as sp
+from cache_reference import Problem
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "s8": torch.int8, "u8": torch.uint8}
+POISON = {"f32": 777.0, "bf16": 776.0, "s8": 77, "u8": 77}
+
+
+def attend(p, max_new=None, scale=None, causal=True, window=0, out="f32", out_scale=1.0, zero=0, pad=0, stream=None):
+    cache, batch = p.on_device()
+    how = sp.make_attend(p.q_heads, max_new or max(p.news + [1]), scale or p.dim ** -0.5, causal, window, out, out_scale, zero)
+    T = max(1, p.tokens)
+    ldo = T + pad
+    o = torch.full((p.q_heads * p.dim, ldo), POISON[out], dtype=DTYPES[out], device="cuda")
+    work = torch.full((sp.spmm_attend_work_bytes(cache, len(p.news), T, how),), 255, dtype=torch.uint8, device="cuda")     # (NaN)
+    q = p.q.cuda()
+    torch.cuda.synchronize()
+    sp.spmm_cache_attend(cache, p.layer, batch, q, T, how, o, ldo, work, stream or torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    o = o.cpu()
+    assert (o[:, T:] == POISON[out]).all()
+    return o[:, :T]
+
+
+def check(p, out="f32", out_scale=1.0, zero=0, **kw):
+    got = attend(p, out=out, out_scale=out_scale, zero=zero, **kw).double().numpy()
+    kw = {k: v for k, v in kw.items() if k in ("causal", "window")}
+    ref, mag = p.attention(p.dim ** -0.5, **kw)
+    there = ~np.isnan(ref)
+    assert (got[~there] == POISON[out]).all()
+    tol = (2.0 ** -8 + 1e-4) * mag
+    if out == "bf16":
+        tol = tol + 2.0 ** -8 * (np.abs(ref) + tol)
+    if out in ("s8", "u8"):
+        lo, hi = (-128, 127) if out == "s8" else (0, 255)
+        edge = lambda x: np.clip(np.rint(x / out_scale) + zero, lo, hi)     # noqa: E731
+        bad = there & ~((got >= edge(ref - tol)) & (got <= edge(ref + tol)))
+    else:
+        bad = there & ~(np.abs(got - ref) <= tol)
+    assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:5], got[bad][:5], ref[bad][:5])
+
+
+HEADS = [(4, 4, 64), (8, 2, 128), (6, 2, 80), (5, 1, 16), (16, 1, 64), (20, 1, 96)]
+
+
+@pytest.mark.parametrize("cache", ["bf16", "s8"])
+@pytest.mark.parametrize("q_heads, kv_heads, dim", HEADS)
+@pytest.mark.parametrize("page", [16, 64])
+def test_one_token_each(q_heads, kv_heads, dim, page, cache):
+    check(Problem([1] * 7, [0, 1, 15, 16, 63, 200, 1000], q_heads, kv_heads, dim, page, cache, seed=1))
+
+
+@pytest.mark.parametrize("cache", ["bf16", "s8"])
+@pytest.mark.parametrize("q_heads, kv_heads, dim", HEADS)
+@pytest.mark.parametrize("causal, window", [(True, 0), (False, 0), (True, 23), (False, 40), (True, 1)])
+def test_chunks_behind_a_past(q_heads, kv_heads, dim, causal, window, cache):
+    check(Problem([3, 0, 70, 17, 1], [0, 5, 31, 130, 64], q_heads, kv_heads, dim, 32, cache, seed=2), causal=causal, window=window)
+
+
+@pytest.mark.parametrize("cache", ["bf16", "s8"])
+@pytest.mark.parametrize("new, past", [(300, 0), (129, 500), (256, 77)])
+@pytest.mark.parametrize("causal, window", [(True, 0), (False, 0), (True, 100)])
+def test_long_chunks(new, past, causal, window, cache):
+    check(Problem([new, 40], [past, 3], 4, 2, 128, 16, cache, seed=3), causal=causal, window=window)
+    check(Problem([new], [past], 2, 2, 64, 128, cache, seed=4), causal=causal, window=window)
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
+def test_page_sizes(page):
+    check(Problem([5, 90], [page - 1, 2 * page - 3], 4, 2, 64, page, seed=5))
+
+
+@pytest.mark.parametrize("new", [1, 40, 200])
+@pytest.mark.parametrize("out, scale, zero", [("bf16", 1, 0), ("s8", 0.02, 3), ("u8", 0.02, 128), ("f32", 1, 0)])
+def test_output_types_and_pitches(new, out, scale, zero):
+    check(Problem([new, 2], [100, 3], 4, 2, 64, 32, seed=6), out=out, out_scale=scale, zero=zero, pad=5)
+
+
+@pytest.mark.parametrize("new", [1, 2, 50, 300])
+def test_long_contexts_are_split_and_joined(new):
+    check(Problem([new, min(new, 3)], [5000, 300], 2, 1, 64, 64, seed=7))
+
+
+def test_many_sequences_of_all_lengths():
+    r = np.random.default_rng(8)
+    check(Problem([1] * 130, [int(x) for x in r.integers(0, 400, 130)], 2, 1, 64, 16, seed=8))
+    check(Problem([int(x) for x in r.integers(0, 9, 70)], [int(x) for x in r.integers(0, 90, 70)], 2, 2, 64, 16, seed=9))
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_rows_that_see_nothing_give_zeros(causal):
+    p = Problem([4, 1, 40], [0, 0, 0], 2, 1, 64, 16, seed=10)
+    p.lens = [2, 0, 7]        # more columns than tokens: the first ones lie before the sequence
+    check(p, causal=causal)
+
+
+def test_what_the_table_cannot_name_is_not_there():
+    p = Problem([3], [60], 2, 1, 64, 16, seed=11, width=2)
+    check(p)
+    check(p, causal=False)
+
+
+def test_columns_of_no_sequence_are_left():
+    check(Problem([3, 20], [7, 1], 2, 1, 64, 16, seed=12, lead=6))
+
+
+@pytest.mark.parametrize("odd", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("new, window", [(8, 0), (70, 0), (70, 9), (1, 9), (260, 0), (260, 40)])
+def test_odd_values_count_only_where_they_are_seen(odd, new, window):
+    """A key or value that is not finite reaches the columns that see it, and no other."""
+    p = Problem([new], [45], 2, 1, 64, 16, seed=13)
+    for at, where in ((45 + new // 2, p.v), (45 + new * 3 // 4, p.v), (20, p.v), (45 + new - 1, p.k)):
+        page, off = p.table[0, at // 16], at % 16
+        if where is p.v:
+            where[0, page, 0, 5, off] = odd
+        else:
+            where[0, page, 0, off, 5] = odd
+    got = attend(p, window=window).double().numpy()
+    with np.errstate(invalid="ignore"):
+        ref, mag = p.attention(p.dim ** -0.5, window=window)
+    fine = np.isfinite(ref) & np.isfinite(mag)
+    assert (np.abs(got[fine] - ref[fine]) <= (2.0 ** -8 + 1e-4) * mag[fine]).all()
+    assert not np.isfinite(got[~fine]).any()
+    assert fine.any() or new == 1       # (a single column sees all of them)
+
+
+@pytest.mark.parametrize("new", [1, 100])
+def test_large_scores_do_not_overflow(new):
+    p = Problem([new], [200], 2, 1, 64, 16, seed=14)
+    p.q = (p.q.float() * 3e4).to(torch.bfloat16)
+    got = attend(p, out="f32").double().numpy()
+    # the softmax is a choice of the largest; where the two largest scores are near, binary32 may weigh them otherwise
+    for t in range(new):
+        for h in range(2):
+            k, v = p.keys(0, 0)[: 201 + t], p.values(0, 0)[: 201 + t]
+            s = np.sort(k @ p.q[t, h].double().numpy() / 8)
+            if s[-1] - s[-2] > 1e3:
+                best = v[np.argmax(k @ p.q[t, h].double().numpy())]
+                assert np.abs(got.reshape(2, 64, -1)[h, :, t] - best).max() <= 1e-6 * np.abs(best).max()
+
+
+def test_layers_and_far_pages():
+    """The second of two layers, and offsets beyond 2^31 elements."""
+    p = Problem([2, 33], [50, 9], 4, 2, 64, 32, layers=2, layer=1, seed=15)
+    check(p)
+    pages = (1 << 32) // (2 * 128 * 64) + 40        # 2^32 bytes of keys and more
+    far = Problem([1, 40], [100, 200], 2, 2, 64, 128, seed=16)
+    ref, mag = far.attention(far.dim ** -0.5)
+    k = torch.zeros((1, pages, 2, 128, 64), dtype=torch.bfloat16, device="cuda")
+    v = torch.zeros((1, pages, 2, 64, 128), dtype=torch.bfloat16, device="cuda")
+    at = torch.arange(far.pages) * 7 + pages - 40 if far.pages * 7 < 40 else torch.arange(far.pages) + pages - far.pages
+    k[:, at.cuda()], v[:, at.cuda()] = far.k.cuda(), far.v.cuda()
+    table = torch.from_numpy(far.table).long()
+    table = torch.where(table >= 0, at[table.clamp(min=0)], -1).to(torch.int32).cuda()
+    cache = sp.make_cache(k, v)
+    batch = sp.make_batch(torch.from_numpy(far.start).cuda(), torch.tensor(far.lens, dtype=torch.int32).cuda(), table)
+    how = sp.make_attend(2, 40, far.dim ** -0.5, out_type="f32")
+    out = torch.zeros((128, far.tokens), device="cuda")
+    work = torch.empty(sp.spmm_attend_work_bytes(cache, 2, far.tokens, how), dtype=torch.uint8, device="cuda")
+    sp.spmm_cache_attend(cache, 0, batch, far.q.cuda(), far.tokens, how, out, far.tokens, work, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert (np.abs(out.cpu().double().numpy() - ref) <= (2.0 ** -8 + 1e-4) * mag).all()
+
+
+@pytest.mark.parametrize("news", [[1] * 5, [40, 200]])
+def test_results_do_not_depend_on_the_run(news):
+    p = Problem(news, [700] * len(news), 4, 1, 128, 16, seed=17)
+    first = attend(p)
+    for _ in range(3):
+        assert torch.equal(attend(p), first)
+
+
+@pytest.mark.parametrize("news", [[1] * 5, [40, 200]])
+def test_on_another_stream_and_in_a_graph(news):
+    p = Problem(news, [700] * len(news), 4, 1, 128, 16, seed=18)
+    first = attend(p)
+    side = torch.cuda.Stream()
+    assert torch.equal(attend(p, stream=side.cuda_stream), first)
+
+    cache, batch = p.on_device()
+    how = sp.make_attend(4, max(news), p.dim ** -0.5, out_type="f32")
+    out = torch.zeros((4 * 128, p.tokens), device="cuda")
+    work = torch.empty(sp.spmm_attend_work_bytes(cache, len(news), p.tokens, how), dtype=torch.uint8, device="cuda")
+    q = p.q.cuda()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        sp.spmm_cache_attend(cache, 0, batch, q, p.tokens, how, out, p.tokens, work, torch.cuda.current_stream().cuda_stream)
+    for _ in range(3):
+        out.fill_(5.0)
+        work.fill_(255)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out.cpu(), first)
