@@ -34,8 +34,8 @@ WIDE = [(tm, nw, maxs) for tm, nw in ((128, 8), (96, 8), (64, 8), (64, 4), (32, 
 HEADERS = [os.path.join(CSRC, "spmm_internal.h"), os.path.join(CSRC, "spmm_kernels.h"), os.path.join(CSRC, "spmm_wide.h"), os.path.join(CSRC, "team.h"),
            os.path.join(ROOT, "include", "spmm.h")]
 
-CACHE_SOURCES = ["cache_api.cpp", "cache_append.hip", "cache_attend.hip", "cache_pages.hip"]
-CACHE_HEADERS = [os.path.join(CACHE_CSRC, "cache_internal.h"), os.path.join(ROOT, "include", "spmm_cache.h")]
+CACHE_SOURCES = ["cache_api.cpp", "cache_append.hip", "cache_attend.cpp", "cache_attend_few.hip", "cache_attend_many.hip", "cache_pages.hip"]
+CACHE_HEADERS = [os.path.join(CACHE_CSRC, "cache_internal.h"), os.path.join(CACHE_CSRC, "cache_attend.h"), os.path.join(ROOT, "include", "spmm_cache.h")]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
