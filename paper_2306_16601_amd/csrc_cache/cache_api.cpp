@@ -156,7 +156,7 @@ spmm_status_t spmm_attend_work_bytes(const spmm_cache_t* cache, int64_t n_seqs, 
     if (!bytes || n_seqs < 1) return SPMM_E_ARG;
     if (const spmm_status_t s = check_attend(cache, T, how)) return s;
     const int64_t max_new = how->max_new < T ? how->max_new : T;
-    *bytes = attend_work_bytes(n_seqs, cache->n_heads, how->q_heads / cache->n_heads, cache->head_dim, max_new);
+    *bytes = attend_work_bytes(cache->type, n_seqs, cache->n_heads, how->q_heads / cache->n_heads, cache->head_dim, max_new);
     return SPMM_OK;
 }
 

@@ -6,9 +6,9 @@ namespace spmm_cache {
 // Columns of a key/value head (query heads that share it times new tokens) up to which the cache is read straight to registers.
 constexpr int64_t FEW = 32;
 
-int64_t attend_work_bytes(int64_t n_seqs, int32_t n_heads, int32_t group, int32_t head_dim, int64_t max_new)
+int64_t attend_work_bytes(spmm_cache_type_t type, int64_t n_seqs, int32_t n_heads, int32_t group, int32_t head_dim, int64_t max_new)
 {
-    return max_new * group <= FEW ? few_work_bytes(n_seqs, head_dim, max_new * group) : many_work_bytes(n_seqs, n_heads, head_dim, max_new * group);
+    return max_new * group <= FEW ? few_work_bytes(n_seqs, head_dim, max_new * group) : many_work_bytes(type, n_seqs, n_heads, head_dim, max_new * group);
 }
 
 int launch_attend(const AttendArgs& a, spmm_cache_type_t type, void* stream)

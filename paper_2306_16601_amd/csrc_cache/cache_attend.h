@@ -142,15 +142,20 @@ __device__ __forceinline__ bool odd_sum(const AttendArgs& a, const int32_t* tabl
     return any;
 }
 
+// store(pointer to results of the call's type, function that makes one of a value)
+template <typename F>
+__device__ __forceinline__ void store_type(const AttendArgs& a, const F& store)
+{
+    const float inv = a.out_inv, zero = (float)a.out_zero_point;
+    if (a.out_type == SPMM_OUT_BF16) store((__bf16*)a.out, [](const float o) { return (__bf16)o; });
+    else if (a.out_type == SPMM_OUT_F32) store((float*)a.out, [](const float o) { return o; });
+    else if (a.out_type == SPMM_OUT_S8) store((int8_t*)a.out, [=](const float o) { return (int8_t)fminf(fmaxf(rintf(o * inv) + zero, -128.0f), 127.0f); });
+    else store((uint8_t*)a.out, [=](const float o) { return (uint8_t)fminf(fmaxf(rintf(o * inv) + zero, 0.0f), 255.0f); });
+}
+
 __device__ __forceinline__ void store_out(const AttendArgs& a, const int64_t at, const float o)
 {
-    if (a.out_type == SPMM_OUT_BF16) ((__bf16*)a.out)[at] = (__bf16)o;
-    else if (a.out_type == SPMM_OUT_F32) ((float*)a.out)[at] = o;
-    else {
-        const float q = rintf(o * a.out_inv) + (float)a.out_zero_point;
-        if (a.out_type == SPMM_OUT_S8) ((int8_t*)a.out)[at] = (int8_t)fminf(fmaxf(q, -128.0f), 127.0f);
-        else ((uint8_t*)a.out)[at] = (uint8_t)fminf(fmaxf(q, 0.0f), 255.0f);
-    }
+    store_type(a, [&](auto* out, auto encode) { out[at] = encode(o); });
 }
 
 }  // namespace spmm_cache

@@ -1,8 +1,8 @@
 // Attention where a key/value head has many columns (chunks of prompts): bound by the matrix instructions and by the
 // exponentials between them.
 //
-// A workgroup takes a block of 128 * NC columns of a sequence's head, 32 * NC for each of its four waves, and walks over
-// tiles of 64 keys that all waves share through LDS (two buffers; the next tile is on its way while this one is multiplied).
+// A workgroup takes a block of 128 columns of a sequence's head, or of 256, 32 for each of its waves, and walks over tiles of
+// 64 keys that all waves share through LDS (two buffers; the next tile is on its way while this one is multiplied).
 // bfloat16 operands go from the pages to LDS without passing through registers, 16 bytes a lane; rows of LDS are 8 or 16 such
 // chunks, whose order is turned by the row's number so that 16 rows read together lie in different banks, and the order is
 // made by where a lane reads, not by where it writes.  Codes of 8 bits are widened to binary16 and multiplied by their scales
@@ -10,55 +10,37 @@
 // 32x32 instruction the lane's 16 scores of a tile of 32 keys are tokens 8 h .. 8 h + 7 of each half (h = lane / 32).
 // The running maximum moves only when a score exceeds it by 2^8: the weights have the room, and the sums need no scaling then.
 //
+// A wave goes through two phases for a tile: products (values of tile i with its weights, then scores of tile i + 1), and
+// the softmax of tile i + 1.  Two waves share a SIMD, and the matrix unit stands still while both are in the second.  With
+// bfloat16 that is left to chance, between two workgroups of 128 columns: two prompts of 4097 tokens, 32 heads on 8 of 128,
+// 332 us (0.83 PFLOP/s, the matrix unit busy for 43 % of the cycles, at 1.9 GHz: the card's power bounds it as well).  With 256
+// columns, waves 4 to 7 held half a tile behind waves 0 to 3 by a barrier after each phase, it took 346 us; so that form is
+// taken for 8 bits only, whose widening twice the columns share (500 tokens behind 15000: 199 us, with 128 columns 270 us).
+//
 // Blocks are dealt out head by head, the longest first, to one XCD after the other, so that blocks that read the same keys
-// share an L2.  Where there are fewer blocks than the device can run, the tiles of all blocks are numbered and cut into equal
-// runs, as in cache_attend_few, and cache_join_many joins the parts.
+// share an L2.  Where the device could run twice as many workgroups as there are blocks, or more, the tiles of each block are
+// dealt to `parts` workgroups, and cache_join_many joins what they write to scratch.
 #include "cache_attend.h"
+
+#include <type_traits>
+
+#define INLINE __attribute__((always_inline))
 
 namespace spmm_cache {
 
-constexpr int WAVES = 4;
-constexpr int THREADS = 64 * WAVES;
 constexpr int TILE = 64;            // keys
 constexpr int CUS = 256, XCDS = 8;
 constexpr float ROOM = 8.0f;
 
-template <int NC>
-constexpr int BLOCK = WAVES * 32 * NC;      // columns
+// GROUPS: of four waves
+template <int GROUPS>
+constexpr int BLOCK = 128 * GROUPS;         // columns
+template <int GROUPS>
+constexpr int ROUND = CUS * 2 / GROUPS;     // workgroups that the device runs at a time
 
-template <int NC>
-constexpr int PER_CU = NC > 1 ? 1 : 2;      // workgroups on a CU
-
-__host__ __device__ inline int64_t parts_at(const int64_t items) { return ((items + 1) * 8 + 15) / 16 * 4; }      // in floats
 __host__ __device__ constexpr int64_t part_floats(const int dim, const int cols) { return (int64_t)cols * (dim + 2); }
 
 __device__ __forceinline__ int uniform(const int v) { return __builtin_amdgcn_readfirstlane(v); }
-__device__ __forceinline__ int64_t uniform(const int64_t v)
-{
-    return (int64_t)(uint32_t)uniform((int)v) | (int64_t)uniform((int)(v >> 32)) << 32;
-}
-
-// Sum over the threads before this one; *all: over all.  Every thread of the workgroup calls it.
-__device__ __forceinline__ int64_t before(const int64_t v, int64_t* const all)
-{
-    __shared__ int64_t waves[WAVES];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    int64_t s = v;
-    for (int i = 1; i < 64; i <<= 1) {
-        const int64_t o = __shfl_up(s, i);
-        if (lane >= i) s += o;
-    }
-    __syncthreads();
-    if (lane == 63) waves[wave] = s;
-    __syncthreads();
-    int64_t base = 0;
-    *all = 0;
-    for (int w = 0; w < WAVES; ++w) {
-        if (w < wave) base += waves[w];
-        *all += waves[w];
-    }
-    return base + s - v;
-}
 
 // A block of columns: c0 .. c1 - 1 of a sequence's head, and its tiles.
 struct Block {
@@ -88,486 +70,518 @@ __device__ __forceinline__ int turned(const int row, const int c)
     return CHUNKS == 16 ? c ^ (row & 15) : c ^ (row >> 1 & 7);
 }
 
+// In place: as an expression, under a condition, it costs copies of all sums where the condition does not hold.
+__device__ __forceinline__ void scale_in_place(float& o, const float by)
+{
+    float y = o;
+    asm volatile("v_mul_f32 %0, %1, %0" : "+v"(y) : "v"(by));
+    o = y;
+}
+
+// A barrier for what is in LDS: stores to memory are not waited for.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 typedef __attribute__((address_space(3))) void lds_void;
 typedef const __attribute__((address_space(1))) void global_void;
 
-// The tiles of keys [64][DIM] and values [DIM][64] in 16 bits.
 template <int DIM>
-struct Tile {
-    uint4 k[TILE * DIM / 8];
-    uint4 v[DIM * TILE / 8];
+struct Half {       // keys [64][DIM], or values [DIM][64], of a tile, in 16 bits
+    uint4 at[TILE * DIM / 8];
 };
 
-template <int DIM, spmm_cache_type_t TYPE, bool EXACT, int NC, bool SPLIT>
-__global__ __launch_bounds__(THREADS, PER_CU<NC>) void cache_attend_many(const AttendArgs a, const int blocks)
+template <int DIM, spmm_cache_type_t TYPE, bool EXACT, int GROUPS, bool SPLIT>
+__global__ __launch_bounds__(256 * GROUPS, 2) void cache_attend_many(const AttendArgs a, const int blocks, const int parts)
 {
     constexpr bool S8 = TYPE == SPMM_CACHE_S8;
+    constexpr int WAVES = 4 * GROUPS, THREADS = 64 * WAVES;
     constexpr int KC = DIM / 8, DT = DIM / 32, KS = DIM / 16;       // chunks of a key's row, dim tiles, steps of scores
-    constexpr int UNITS = DIM / 64;                                 // 16 codes that a thread widens, of keys and of values
-    constexpr int CPI = DIM / 32;                                   // instructions of a wave for a tile's keys, and for its values
-    __shared__ Tile<DIM> tile0, tile1;
+    constexpr int CPI = DIM / 8 / WAVES;                            // instructions of a wave for a tile's keys, and for its values
+    constexpr int UNITS = 2 * TILE * DIM / 16 / THREADS;            // 16 codes that a thread widens
+    __shared__ Half<DIM> keys0, keys1, values0, values1;       // (apart, so that loads to one are not waited for by reads of another)
+    __shared__ float scales[S8 ? WAVES : 1][2][TILE];
     __shared__ int odd_found;
-    __shared__ int64_t found[2];
 
     const int tid = threadIdx.x, lane = tid % 64, wave = uniform(tid / 64), col = lane % 32, half = lane / 32;
     const int D = EXACT ? DIM : a.pool.head_dim, G = a.group, H = a.pool.n_heads, shift = a.pool.page_shift, inside = (1 << shift) - 1;
 
     if constexpr (!EXACT) {     // what lies beyond the head's dims is never loaded
-        for (int i = tid; i < TILE * DIM / 8; i += THREADS) tile0.k[i] = tile0.v[i] = tile1.k[i] = tile1.v[i] = uint4{0, 0, 0, 0};
+        for (int i = tid; i < TILE * DIM / 8; i += THREADS) keys0.at[i] = keys1.at[i] = values0.at[i] = values1.at[i] = uint4{0, 0, 0, 0};
         __syncthreads();
     }
 
-    // what this workgroup does: block `item` of head h, tiles u0 .. u1 - 1 of it; in runs, more of them
-    int64_t item, at = 0, done = 0, to = 1;
-    int h = 0;
-    if constexpr (SPLIT) {
-        const int64_t items = (int64_t)a.batch.n_seqs * blocks;
-        int64_t* const prefix = (int64_t*)a.work;
-        int64_t total = 0, mine = 0, ahead = 0;
-        for (int pass = 0; pass < 2; ++pass) {
-            int64_t sum = 0;
-            for (int64_t i0 = 0; i0 < items; i0 += THREADS) {
-                const int64_t i = i0 + tid;
-                if (pass == 0 || items > THREADS) {
-                    mine = i < items ? (int64_t)block_of(a, sequence(a, (int)(i / blocks)), (int)(i % blocks), BLOCK<NC>).tiles * H : 0;
-                    int64_t all;
-                    ahead = sum + before(mine, &all);
-                    sum += all;
-                } else {
-                    sum = total;
-                }
-                if (pass == 0) {
-                    if (blockIdx.x == 0 && i < items) prefix[i] = ahead;
-                    continue;
-                }
-                if (done >= ahead && done < ahead + mine) {
-                    found[0] = i;
-                    found[1] = done - ahead;
-                }
-                if (done < sum) break;
-            }
-            if (pass == 0) {
-                total = sum;
-                if (blockIdx.x == 0 && tid == 0) prefix[items] = total;
-                const int64_t runs = min((int64_t)gridDim.x, total);
-                if (blockIdx.x >= runs) return;
-                done = blockIdx.x * total / runs;
-                to = (blockIdx.x + 1) * total / runs;
-            }
-        }
-        __syncthreads();
-        item = uniform(found[0]);
-        at = uniform(found[1]);
-    } else {
-        // XCD x takes the x-th part of all (head, sequence) pairs with their blocks
-        const uint32_t all = gridDim.x / XCDS, id = blockIdx.x % XCDS * all + blockIdx.x / XCDS;
-        const uint32_t pair = id / (uint32_t)blocks, j = blocks - 1 - id % (uint32_t)blocks;
-        h = (int)(pair / (uint32_t)a.batch.n_seqs);
-        if (h >= H) return;
-        item = (int64_t)(pair % (uint32_t)a.batch.n_seqs) * blocks + j;
-    }
+    // where a lane reads the first operands of a tile; step k of keys lies at off_k ^ 32 k, step e of values at off_v ^ 32 e.
+    // Row r of a tile of scores is token r with bits 2 and 3 exchanged.
+    const int k_row = (col & 0x13) | (col & 4) << 1 | (col & 8) >> 1;
+    int off_k = (k_row * KC + turned<KC>(k_row, half)) * 16, off_v = (col * 8 + turned<8>(col, half)) * 16;
 
-    while (done < to) {
-        const int b = (int)(item / blocks);
-        const Sequence s = sequence(a, b);
-        const Block blk = block_of(a, s, (int)(item % blocks), BLOCK<NC>);
-        if constexpr (SPLIT) {
-            if (at >= (int64_t)blk.tiles * H) {
-                ++item;
-                at = 0;
-                continue;
-            }
-            h = (int)(at / blk.tiles);
-        } else {
-            if (blk.tiles == 0) return;
-        }
-        const int u0 = SPLIT ? (int)(at % blk.tiles) : 0;
-        const int u1 = SPLIT ? (int)min((int64_t)blk.tiles, u0 + (to - done)) : blk.tiles;
-        const int32_t* const table = a.batch.table + b * a.batch.ld_table;
-        const int last_page = max(s.len - 1, 0) >> shift;
+    // XCD x takes the x-th part of all (head, sequence) pairs with their blocks
+    const uint32_t all = gridDim.x / XCDS, id = blockIdx.x % XCDS * all + blockIdx.x / XCDS;
+    const uint32_t place = SPLIT ? id / (uint32_t)parts : id, part = SPLIT ? id % (uint32_t)parts : 0;
+    const uint32_t pair = place / (uint32_t)blocks, j = blocks - 1 - place % (uint32_t)blocks;
+    const int h = (int)(pair / (uint32_t)a.batch.n_seqs), b = (int)(pair % (uint32_t)a.batch.n_seqs);
+    if (h >= H) return;
+    const Sequence s = sequence(a, b);
+    const Block blk = block_of(a, s, (int)j, BLOCK<GROUPS>);
+    if (blk.tiles == 0) return;
+    const int u0 = SPLIT ? (int)((int64_t)blk.tiles * part / parts) : 0;
+    const int u1 = SPLIT ? (int)((int64_t)blk.tiles * (part + 1) / parts) : blk.tiles;
+    if (SPLIT && u0 == u1) return;
+    const int32_t* const table = a.batch.table + b * a.batch.ld_table;
+    const int last_page = max(s.len - 1, 0) >> shift;
 
-        // columns
-        int lo[NC], hi[NC];
-        u32x4 q[NC][KS];
-        float unit[NC];
+    const int seen_from = s.first_seen(a, blk.c0 / G), seen_to = s.last_seen(a, (blk.c1 - 1) / G);          // by some column
+    const int all_from = s.first_seen(a, (blk.c1 - 1) / G), all_to = s.last_seen(a, blk.c0 / G);            // by all
+
+    // ---- a tile on its way to LDS: the keys of tile i + 1 with the values of tile i ----
+    // bfloat16: instruction j of the wave fills 1 KB, 16 bytes a lane.  Page numbers are asked for a tile ahead.  A wave's
+    // keys lie in one page; values of a tile do where pages have 64 tokens and more.
+    const uint32_t page_bytes = (uint32_t)(H * D) << shift << (S8 ? 0 : 1);
+    const char* const k_head = (const char*)a.pool.k + ((int64_t)h * D << shift) * 2;
+    const char* const v_head = (const char*)a.pool.v + (((int64_t)h * D + wave * CPI * 8) << shift) * 2;
+    constexpr int NP = CPI > 1 ? 2 : 1;        // of a wave's rows of values, that are turned differently
+    int page_k = 0, page_v[2] = {0, 0};
+    uint32_t off_fk[S8 ? 1 : CPI], off_fv[NP];
+    if constexpr (!S8) {
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const int i = blk.c0 + (wave * NC + c) * 32 + col;
-            const bool there = i < blk.c1;
-            const int token = there ? i / G : 0, head = h * G + (there ? i % G : 0);
-            lo[c] = s.first_seen(a, token);
-            hi[c] = there ? s.last_seen(a, token) : -1;
-            unit[c] = a.scale_log2;
-            const __bf16* const src = a.q + ((int64_t)(s.first + token) * (H * G) + head) * D;
-            float most = 0.0f;
+        for (int j = 0; j < CPI; ++j) {
+            const int row = (wave * CPI + j) * (64 / KC) + lane / KC;
+            off_fk[j] = ((row - wave * CPI * (64 / KC)) * D + 8 * turned<KC>(row, lane % KC)) * 2;
+        }
+#pragma unroll
+        for (int j = 0; j < NP; ++j) off_fv[j] = ((lane / 8 << shift) + (8 * turned<8>((wave * CPI + j) * 8 + lane / 8, lane % 8) & inside)) * 2;
+    }
+    constexpr int ROWS = 64 / WAVES;        // keys that a wave fetches
+    const auto page_at = [&](const int key) INLINE { return table[min(max(key, 0) >> shift, last_page)]; };       // (never beyond the sequence's)
+    const auto name = [&](const int k0) INLINE {       // of the keys of the tile at k0 + TILE, and the values of that at k0
+        if constexpr (!S8) {
+            page_k = page_at(k0 + TILE + ROWS * wave);
+#pragma unroll
+            for (int j = 0; j < NP; ++j) page_v[j] = page_at(k0 + (shift < 6 ? 8 * turned<8>((wave * CPI + j) * 8 + lane / 8, lane % 8) : 0));
+        }
+    };
+    // (in parts, so that a step can issue them between its products: all at once they fill the address unit's queue)
+    const char *k_from = nullptr, *v_from[NP] = {};
+    const auto aim = [&](const int k0) INLINE {      // at the keys of the tile at k0 + TILE, and the values of that at k0
+        k_from = k_head + (int64_t)page_in_pool(uniform(page_k), a.pool.n_pages) * page_bytes + ((k0 + TILE + ROWS * wave) & inside) * D * 2;
+        if (shift >= 6) {
+            const char* const v = v_head + (int64_t)page_in_pool(uniform(page_v[0]), a.pool.n_pages) * page_bytes + (k0 & inside) * 2;
+#pragma unroll
+            for (int j = 0; j < NP; ++j) v_from[j] = v + off_fv[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < NP; ++j) v_from[j] = v_head + off_fv[j] + (uint64_t)(uint32_t)page_in_pool(page_v[j], a.pool.n_pages) * page_bytes;
+        }
+    };
+    const auto fetch_k = [&](Half<DIM>& t, const int j) INLINE {
+        if (EXACT || 8 * turned<KC>((wave * CPI + j) * (64 / KC) + lane / KC, lane % KC) < D)
+            __builtin_amdgcn_global_load_lds((global_void*)(k_from + off_fk[j]), (lds_void*)(t.at + (wave * CPI + j) * 64), 16, 0, 0);
+    };
+    const auto fetch_v = [&](Half<DIM>& t, const int j) INLINE {
+        if (EXACT || (wave * CPI + j) * 8 < D)
+            __builtin_amdgcn_global_load_lds((global_void*)(v_from[j % NP] + (((int64_t)8 * j) << shift) * 2), (lds_void*)(t.at + (wave * CPI + j) * 64), 16, 0, 0);
+    };
+    // 8 bits: a thread has units of 16 codes in registers until the phases before have ended, keys in the first half of
+    // all units and values in the second; a lane has the scales of a key, and of a value's token
+    u32x4 raw[S8 ? UNITS : 1];
+    int unit_page[S8 ? UNITS : 1], lane_page_k = 0, lane_page_v = 0;
+    float lane_k = 0.0f, lane_v = 0.0f;
+    constexpr int UPR = DIM / 16, HALF_UNITS = TILE * DIM / 16;     // units of a key's row, and of a tile's keys
+    const auto is_key = [&](const int i) INLINE { return UNITS > 1 ? i < UNITS / 2 : tid < HALF_UNITS; };
+    const auto unit_of = [&](const int i) INLINE { return UNITS > 1 ? tid + THREADS * (i % (UNITS / 2 > 0 ? UNITS / 2 : 1)) : tid % HALF_UNITS; };
+    const auto name_codes = [&](const int k0) INLINE {
+        if constexpr (S8) {
+#pragma unroll
+            for (int i = 0; i < UNITS; ++i) unit_page[i] = page_at(is_key(i) ? k0 + TILE + unit_of(i) / UPR : k0 + unit_of(i) % 4 * 16);
+            lane_page_k = page_at(k0 + TILE + lane);
+            lane_page_v = page_at(k0 + lane);
+        }
+    };
+    const auto fetch_codes = [&](const int k0) INLINE {        // keys of the tile at k0 + TILE, values of that at k0
+        if constexpr (S8) {
+#pragma unroll
+            for (int i = 0; i < UNITS; ++i) {
+                const int64_t page = (int64_t)page_in_pool(unit_page[i], a.pool.n_pages) * H + h;
+                const int u = unit_of(i), d = is_key(i) ? u % UPR * 16 : u / 4;
+                const int64_t at = is_key(i) ? ((page << shift) + ((k0 + TILE + u / UPR) & inside)) * D + d : ((page * D + d) << shift) + ((k0 + u % 4 * 16) & inside);
+                raw[i] = EXACT || d < D ? *(const u32x4*)((const int8_t*)(is_key(i) ? a.pool.k : a.pool.v) + at) : u32x4{0, 0, 0, 0};
+            }
+            lane_k = a.pool.k_scale[(((int64_t)page_in_pool(lane_page_k, a.pool.n_pages) * H + h) << shift) + ((k0 + TILE + lane) & inside)];
+            lane_v = a.pool.v_scale[(((int64_t)page_in_pool(lane_page_v, a.pool.n_pages) * H + h) << shift) + ((k0 + lane) & inside)];
+        }
+    };
+    float k_up = 1.0f, k_up_next = 1.0f, v_up = __builtin_bit_cast(float, 2u << 23), v_less = 1.0f;
+    const auto widen_codes = [&](Half<DIM>& tk, Half<DIM>& tv, const int k0) INLINE {
+        if constexpr (S8) {
+            const bool k_here = k0 + TILE + lane >= seen_from && k0 + TILE + lane <= seen_to, v_here = k0 + lane >= seen_from && k0 + lane <= seen_to;
+            if (!k_here) lane_k = 0.0f;     // (they may be anything)
+            if (!v_here) lane_v = 0.0f;
+            float mk = fabsf(lane_k) <= 3.4e38f ? fabsf(lane_k) : 0.0f, mv = fabsf(lane_v) <= 3.4e38f ? fabsf(lane_v) : 0.0f;
+#pragma unroll
+            for (int i = 1; i < 64; i <<= 1) {
+                mk = fmaxf(mk, __shfl_xor(mk, i));
+                mv = fmaxf(mv, __shfl_xor(mv, i));
+            }
+            float up;
+            const float k_down = to_unit(mk, &k_up_next);
+            to_unit(mv, &up);
+            up = fmaxf(up, v_up);
+            v_less = v_up / up;     // (for the sums, before they are added to)
+            v_up = up;
+            const float v_down = __builtin_bit_cast(float, (254u << 23) - __builtin_bit_cast(uint32_t, up));
+            __builtin_amdgcn_wave_barrier();
+            scales[wave][0][lane] = lane_k * k_down;
+            scales[wave][1][lane] = lane_v * v_down;
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int i = 0; i < UNITS; ++i) {
+                const int u = unit_of(i), row = is_key(i) ? u / UPR : u / 4;
+                f16x8 x = widen(raw[i][0], raw[i][1]), y = widen(raw[i][2], raw[i][3]);
+                if (is_key(i)) {        // (rounded once, after the scale)
+                    const float by = scales[wave][0][row];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        x[j] = (_Float16)((float)x[j] * by);
+                        y[j] = (_Float16)((float)y[j] * by);
+                    }
+                    const int c = u % UPR * 2;
+                    *(f16x8*)(tk.at + row * KC + turned<KC>(row, c)) = x;
+                    *(f16x8*)(tk.at + row * KC + turned<KC>(row, c + 1)) = y;
+                } else {
+                    const float* const by = scales[wave][1] + u % 4 * 16;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        x[j] = (_Float16)((float)x[j] * by[j]);
+                        y[j] = (_Float16)((float)y[j] * by[8 + j]);
+                    }
+                    const int c = u % 4 * 2;
+                    *(f16x8*)(tv.at + row * 8 + turned<8>(row, c)) = x;
+                    *(f16x8*)(tv.at + row * 8 + turned<8>(row, c + 1)) = y;
+                }
+            }
+        }
+    };
+    // What no column sees may hold anything (pages are not cleared): it counts as 0, and so does what is not finite where
+    // some columns see it and others do not (odd_sum).
+    const auto clean = [&](Half<DIM>& t, const int k0) INLINE {
+        bool odd = false;
+        for (int i = tid; i < DIM * 8; i += THREADS) {
+            const int row = i / 8, c = turned<8>(row, i % 8);
+            u32x4 v = __builtin_bit_cast(u32x4, t.at[i]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int key = k0 + 8 * c + 2 * j;
+                if (key < seen_from || key > seen_to) v[j] &= 0xffff0000u;
+                if (key + 1 < seen_from || key + 1 > seen_to) v[j] &= 0xffffu;
+            }
+            const u32x4 w = S8 ? finite_half_or_zero(v) : finite_or_zero(v);
+            odd |= (v[0] != w[0]) | (v[1] != w[1]) | (v[2] != w[2]) | (v[3] != w[3]);
+            t.at[i] = __builtin_bit_cast(uint4, w);
+        }
+        if (odd) odd_found = 1;
+    };
+
+    if (tid == 0) odd_found = 0;
+    const int first = (blk.tile0 + u0) * TILE;
+    const int end = min((blk.tile0 + u1) * TILE, seen_to + 1);      // (where nobody sees anything there is a tile all the same)
+    const int n = first < end ? (end - first + TILE - 1) / TILE : 0;
+    if (n) {        // the first keys, before the queries are asked for
+        if constexpr (S8) {
+            name_codes(first - TILE);       // (the values of a tile before the first one: in the pool, and written over)
+            fetch_codes(first - TILE);
+            name_codes(first);
+        } else {
+            name(first - TILE);
+            aim(first - TILE);
+#pragma unroll
+            for (int j = 0; j < CPI; ++j) fetch_k(keys0, j);
+            name(first);
+        }
+    }
+
+    // columns
+    const int mine = blk.c0 + wave * 32 + col;
+    int lo, hi;
+    u32x4 q[KS];
+    float unit = a.scale_log2;      // of scores: log2(e) * scale, and the power of two that the queries were divided by
+    {
+        const bool there = mine < blk.c1;
+        const int token = there ? mine / G : 0, head = h * G + (there ? mine % G : 0);
+        lo = s.first_seen(a, token);
+        hi = there ? s.last_seen(a, token) : -1;
+        const __bf16* const src = a.q + ((int64_t)(s.first + token) * (H * G) + head) * D;
+        float most = 0.0f;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            const int d = 16 * k + 8 * half;
+            q[k] = there && (EXACT || d < D) ? *(const u32x4*)(src + d) : u32x4{0, 0, 0, 0};
+            if constexpr (S8) {
+                const bf16x8 v = __builtin_bit_cast(bf16x8, q[k]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf((float)v[j]));
+            }
+        }
+        if constexpr (S8) {
+            most = fmaxf(most, other_half(most));
+            float up;
+            const float down = to_unit(most, &up);
+            unit *= up;
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
-                const int d = 16 * k + 8 * half;
-                q[c][k] = there && (EXACT || d < D) ? *(const u32x4*)(src + d) : u32x4{0, 0, 0, 0};
-                if constexpr (S8) {
-                    const bf16x8 v = __builtin_bit_cast(bf16x8, q[c][k]);
+                const bf16x8 v = __builtin_bit_cast(bf16x8, q[k]);
+                f16x8 w;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf((float)v[j]));
-                }
-            }
-            if constexpr (S8) {
-                most = fmaxf(most, other_half(most));
-                float up;
-                const float down = to_unit(most, &up);
-                unit[c] *= up;
-#pragma unroll
-                for (int k = 0; k < KS; ++k) {
-                    const bf16x8 v = __builtin_bit_cast(bf16x8, q[c][k]);
-                    f16x8 w;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) w[j] = (_Float16)((float)v[j] * down);
-                    q[c][k] = __builtin_bit_cast(u32x4, w);
-                }
+                for (int j = 0; j < 8; ++j) w[j] = (_Float16)((float)v[j] * down);
+                q[k] = __builtin_bit_cast(u32x4, w);
             }
         }
-        const int seen_from = s.first_seen(a, blk.c0 / G), seen_to = s.last_seen(a, (blk.c1 - 1) / G);          // by some column
-        const int all_from = s.first_seen(a, (blk.c1 - 1) / G), all_to = s.last_seen(a, blk.c0 / G);            // by all
-
-        f32x16 o[NC][DT];
-        float m[NC], l[NC];
+    }
+    f32x16 o[DT], sc[2];
+    u32x4 p[4];
+    float m = NONE, l = 0.0f;
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            m[c] = NONE;
-            l[c] = 0.0f;
+    for (int e = 0; e < 4; ++e) p[e] = u32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+
+    // ---- products: values of a tile with its weights, then scores of the next one (if there is one) ----
+    const auto multiply = [&](const Half<DIM>& tv, const Half<DIM>& tk, const bool scores, auto&& between) INLINE {
+        asm volatile("" : "+v"(off_k), "+v"(off_v));        // (worked out for each tile: registers are scarce)
+        constexpr int PV = 4 * DT, QK = 2 * KS, AHEAD = 6;      // operands are read so many instructions ahead
+        u32x4 x[PV + QK];
+        const auto read = [&](const int i) INLINE {
+            if (i < PV) x[i] = *(const u32x4*)((const char*)tv.at + (off_v ^ 32 * (i / DT)) + 32 * (i % DT) * 8 * 16);
+            else x[i] = *(const u32x4*)((const char*)tk.at + (off_k ^ 32 * ((i - PV) / 2)) + 32 * ((i - PV) % 2) * KC * 16);
+        };
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) read(i);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < PV; ++i) {
+            read(i + AHEAD);
+            const int d = i % DT, e = i / DT;
+            if constexpr (S8) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x[i]), __builtin_bit_cast(f16x8, p[e]), o[d], 0, 0, 0);
+            else o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x[i]), __builtin_bit_cast(bf16x8, p[e]), o[d], 0, 0, 0);
+            between(i);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (!scores) return;
+#pragma unroll
+        for (int i = 0; i < QK; ++i) {
+            if (i + AHEAD < QK) read(PV + i + AHEAD);
+            const int g = i % 2, k = i / 2;
+            const f32x16 zero = {};
+            if constexpr (S8) sc[g] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x[PV + i]), __builtin_bit_cast(f16x8, q[k]), k ? sc[g] : zero, 0, 0, 0);
+            else sc[g] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x[PV + i]), __builtin_bit_cast(bf16x8, q[k]), k ? sc[g] : zero, 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+
+    // ---- softmax of a tile's scores ----
+    const auto weigh = [&](const int k0, const float keys_up, auto&& between) INLINE {
+        const float by = S8 ? unit * keys_up : unit;
+        if (k0 < all_from || k0 + TILE - 1 > all_to) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                const int key = k0 + 16 * (i / 8) + 8 * half + i % 8;
+                sc[i / 16][i % 16] = key >= lo && key <= hi ? sc[i / 16][i % 16] : NONE;
+            }
+        }
+        float top = sc[0][0];
+#pragma unroll
+        for (int i = 1; i < 32; ++i) top = fmaxf(top, sc[i / 16][i % 16]);
+        top = fmaxf(top, other_half(top)) * by;
+        if (__any(top > m + ROOM)) {
+            const float mn = fmaxf(m, top);
+            float fade = __builtin_amdgcn_exp2f(m - (mn == NONE ? 0.0f : mn));
+            m = mn;
+            l *= fade;
+            asm volatile("s_nop 1" : "+v"(fade));       // (the exponential needs that before its result is read)
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) o[c][d][i] = 0.0f;
+                for (int i = 0; i < 16; ++i) { float y = o[d][i]; scale_in_place(y, fade); o[d][i] = y; }
         }
-
-        // ---- a tile on its way to LDS ----
-        const auto page_of = [&](const int key) { return (int64_t)page_in_pool(table[min(key >> shift, last_page)], a.pool.n_pages) * H + h; };
-
-        // bfloat16: instruction j of the wave fills 1 KB, 16 bytes a lane.  The page numbers of a tile are asked for with the
-        // tile before it.
-        int page_k = 0, page_v[2] = {0, 0};
-        const auto name = [&](const int k0) {
-            if constexpr (!S8) {
-                page_k = table[min((k0 + 16 * wave) >> shift, last_page)];
-                page_v[0] = table[min((k0 + 8 * turned<8>(lane / 8, lane % 8)) >> shift, last_page)];
-                page_v[1] = table[min((k0 + 8 * turned<8>(8 + lane / 8, lane % 8)) >> shift, last_page)];
-            }
-        };
-        const auto fetch = [&](Tile<DIM>& t, const int k0) {
-            if constexpr (!S8) {
-                const int64_t slot = (((int64_t)page_in_pool(uniform(page_k), a.pool.n_pages) * H + h) << shift) + ((k0 + 16 * wave) & inside);
-                const char* const k = (const char*)a.pool.k + slot * D * 2;
+        const float ms = m == NONE ? 0.0f : m;
 #pragma unroll
-                for (int j = 0; j < CPI; ++j) {
-                    const int row = j * (64 / KC) + lane / KC, c = turned<KC>(row, lane % KC);
-                    if (EXACT || 8 * c < D)
-                        __builtin_amdgcn_global_load_lds((global_void*)(k + (row * D + 8 * c) * 2), (lds_void*)(t.k + (wave * CPI + j) * 64), 16, 0, 0);
-                }
+        for (int e = 0; e < 4; ++e) {
+            float x[8];
 #pragma unroll
-                for (int j = 0; j < CPI; ++j) {
-                    const int row = (wave * CPI + j) * 8 + lane / 8, c = turned<8>((j & 1) * 8 + lane / 8, lane % 8);
-                    const int64_t page = (int64_t)page_in_pool(page_v[j & 1], a.pool.n_pages) * H + h;
-                    const int64_t from = ((page * D + row) << shift) + ((k0 + 8 * c) & inside);
-                    if (EXACT || row < D)
-                        __builtin_amdgcn_global_load_lds((global_void*)((const char*)a.pool.v + from * 2), (lds_void*)(t.v + (wave * CPI + j) * 64), 16, 0, 0);
-                }
-                name(k0 + TILE);
-            }
-        };
-        // 8 bits: codes and scales in registers until the tile before has been multiplied
-        u32x4 raw_k[S8 ? UNITS : 1], raw_v[S8 ? UNITS : 1];
-        float k_scale[S8 ? UNITS : 1], lane_k = 0.0f, lane_v = 0.0f;
-        f32x4 v_scale[S8 ? 4 : 1];
-        constexpr int UPR = DIM / 16;       // units of a key's row
-        const auto fetch_codes = [&](const int k0) {
+            for (int j = 0; j < 8; ++j) x[j] = __builtin_amdgcn_exp2f(__fmaf_rn(sc[e / 2][e % 2 * 8 + j], by, -ms));
             if constexpr (S8) {
+                f16x8 w;
 #pragma unroll
-                for (int i = 0; i < UNITS; ++i) {
-                    const int row = (tid + THREADS * i) / UPR, d = tid % UPR * 16;
-                    const int64_t slot = (page_of(k0 + row) << shift) + ((k0 + row) & inside);
-                    raw_k[i] = EXACT || d < D ? *(const u32x4*)((const int8_t*)a.pool.k + slot * D + d) : u32x4{0, 0, 0, 0};
-                    k_scale[i] = a.pool.k_scale[slot];
-                }
-                const int key = k0 + tid % 4 * 16;
-                const int64_t page = page_of(key);
+                for (int j = 0; j < 8; ++j) w[j] = (_Float16)x[j];
+                l = sum_of(w, l);
+                p[e] = __builtin_bit_cast(u32x4, w);
+            } else {
+                bf16x8 w;
 #pragma unroll
-                for (int i = 0; i < UNITS; ++i) {
-                    const int d = tid / 4 + TILE * i;
-                    raw_v[i] = EXACT || d < D ? *(const u32x4*)((const int8_t*)a.pool.v + ((page * D + d) << shift) + (key & inside)) : u32x4{0, 0, 0, 0};
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v_scale[i] = *(const f32x4*)(a.pool.v_scale + (page << shift) + (key & inside) + 4 * i);
-                const int64_t slot = (page_of(k0 + lane) << shift) + ((k0 + lane) & inside);
-                lane_k = a.pool.k_scale[slot];
-                lane_v = a.pool.v_scale[slot];
+                for (int j = 0; j < 8; ++j) w[j] = (__bf16)x[j];
+                l = sum_of(w, l);
+                p[e] = __builtin_bit_cast(u32x4, w);
             }
-        };
-        float k_up = 1.0f, k_up_next = 1.0f, v_up = __builtin_bit_cast(float, 2u << 23), v_less = 1.0f;
-        const auto widen_codes = [&](Tile<DIM>& t, const int k0) {
-            if constexpr (S8) {
-                const bool here = k0 + lane >= seen_from && k0 + lane <= seen_to;       // (others' scales may be anything)
-                float k_down, up;
-                const float k_most = here && fabsf(lane_k) <= 3.4e38f ? fabsf(lane_k) : 0.0f, v_most = here && fabsf(lane_v) <= 3.4e38f ? fabsf(lane_v) : 0.0f;
-                float mk = k_most, mv = v_most;
-#pragma unroll
-                for (int i = 1; i < 64; i <<= 1) {
-                    mk = fmaxf(mk, __shfl_xor(mk, i));
-                    mv = fmaxf(mv, __shfl_xor(mv, i));
-                }
-                k_down = to_unit(mk, &k_up_next);
-                to_unit(mv, &up);
-                up = fmaxf(up, v_up);
-                v_less = v_up / up;
-                v_up = up;
-                const float v_down = __builtin_bit_cast(float, (254u << 23) - __builtin_bit_cast(uint32_t, up));
-#pragma unroll
-                for (int i = 0; i < UNITS; ++i) {
-                    const int row = (tid + THREADS * i) / UPR, c = tid % UPR * 2;
-                    const _Float16 f = (_Float16)(k0 + row <= seen_to && k0 + row >= seen_from ? k_scale[i] * k_down : 0.0f);
-                    const f16x8 by = {f, f, f, f, f, f, f, f};
-                    const f16x8 x = widen(raw_k[i][0], raw_k[i][1]) * by, y = widen(raw_k[i][2], raw_k[i][3]) * by;
-                    *(f16x8*)(t.k + row * KC + turned<KC>(row, c)) = x;
-                    *(f16x8*)(t.k + row * KC + turned<KC>(row, c + 1)) = y;
-                }
-                f16x8 by[2];
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int key = k0 + tid % 4 * 16 + i;
-                    by[i / 8][i % 8] = (_Float16)(key <= seen_to && key >= seen_from ? v_scale[i / 4][i % 4] * v_down : 0.0f);
-                }
-#pragma unroll
-                for (int i = 0; i < UNITS; ++i) {
-                    const int row = tid / 4 + TILE * i, c = tid % 4 * 2;
-                    *(f16x8*)(t.v + row * 8 + turned<8>(row, c)) = widen(raw_v[i][0], raw_v[i][1]) * by[0];
-                    *(f16x8*)(t.v + row * 8 + turned<8>(row, c + 1)) = widen(raw_v[i][2], raw_v[i][3]) * by[1];
-                }
-            }
-        };
+            between(e);
+        }
+    };
 
-        // ---- a tile multiplied ----
-        const auto multiply = [&](Tile<DIM>& t, const int k0) {
-            const bool partial = k0 < all_from || k0 + TILE - 1 > all_to;
-            if (partial) {
-                // What no column sees may hold anything (pages are not cleared): it counts as 0, and so does what is not
-                // finite where some columns see it and others do not (store_odd).
-                bool mine = false;
-                for (int i = tid; i < DIM * 8; i += THREADS) {
-                    const int row = i / 8, c = turned<8>(row, i % 8);
-                    u32x4 v = __builtin_bit_cast(u32x4, t.v[i]);
+    if (n) {
+        if constexpr (S8) widen_codes(keys0, values1, first - TILE);
+        v_up = __builtin_bit_cast(float, 2u << 23);
+        v_less = 1.0f;
+        __syncthreads();
+    }
+    // Step t: waves ahead multiply values t - 1 and keys t, then weigh tile t; waves behind weigh tile t - 1, then multiply.
+    const auto step = [&](auto is_ahead, Half<DIM>& k_now, Half<DIM>& k_next, Half<DIM>& v_now, Half<DIM>& v_last, const int t) INLINE {
+        constexpr bool ahead = decltype(is_ahead)::value;
+        const int k0 = first + t * TILE;
+        const bool more = t < n, more_k = t + 1 < n;
+        if constexpr (S8) {
+            if (more) {
+                fetch_codes(k0);
+                name_codes(k0 + TILE);
+            }
+        } else {
+            aim(k0);
+        }
+        // a quarter of the wave's loads to LDS
+        const auto fetch = [&](const int part) INLINE {
+            if constexpr (!S8) {
+                constexpr int EACH = (2 * CPI + 3) / 4;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int key = k0 + 8 * c + 2 * j;
-                        if (key < seen_from || key > seen_to) v[j] &= 0xffff0000u;
-                        if (key + 1 < seen_from || key + 1 > seen_to) v[j] &= 0xffffu;
+                for (int i = part * EACH; i < (part + 1) * EACH && i < 2 * CPI; ++i) {
+                    if (i < CPI) {
+                        if (more_k) fetch_k(k_next, i);
+                    } else {
+                        if (more) fetch_v(v_now, i - CPI);
                     }
-                    const u32x4 w = S8 ? finite_half_or_zero(v) : finite_or_zero(v);
-                    mine |= (v[0] != w[0]) | (v[1] != w[1]) | (v[2] != w[2]) | (v[3] != w[3]);
-                    t.v[i] = __builtin_bit_cast(uint4, w);
                 }
-                if (mine) odd_found = 1;
-                __syncthreads();
+                if (part == 3 && more) name(k0 + TILE);
             }
+        };
+        const auto nothing = [](const int) INLINE {};
+        __builtin_amdgcn_sched_barrier(0);
+        const float k_up_last = k_up;
+        k_up = k_up_next;       // of the keys that this step multiplies
+        const auto products = [&](auto&& between) INLINE {
             if constexpr (S8) {
                 if (v_less != 1.0f) {
 #pragma unroll
-                    for (int c = 0; c < NC; ++c)
+                    for (int d = 0; d < DT; ++d)
 #pragma unroll
-                        for (int d = 0; d < DT; ++d) o[c][d] *= v_less;
+                        for (int i = 0; i < 16; ++i) { float y = o[d][i]; scale_in_place(y, v_less); o[d][i] = y; }
                 }
             }
-            f32x16 sc[NC][2];
+            multiply(v_last, k_now, more, between);
+            if (t == 0) {       // (there were no weights yet)
 #pragma unroll
-            for (int g = 0; g < 2; ++g) {
+                for (int d = 0; d < DT; ++d)
 #pragma unroll
-                for (int c = 0; c < NC; ++c)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) sc[c][g][i] = 0.0f;
-                // row r of a tile of scores is token r with bits 2 and 3 exchanged
-                const int row = 32 * g + ((col & 0x13) | (col & 4) << 1 | (col & 8) >> 1);
-#pragma unroll
-                for (int k = 0; k < KS; ++k) {
-                    const u32x4 x = __builtin_bit_cast(u32x4, t.k[row * KC + turned<KC>(row, 2 * k + half)]);
-#pragma unroll
-                    for (int c = 0; c < NC; ++c) {
-                        if constexpr (S8) sc[c][g] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, q[c][k]), sc[c][g], 0, 0, 0);
-                        else sc[c][g] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, q[c][k]), sc[c][g], 0, 0, 0);
-                    }
-                }
-            }
-            u32x4 p[NC][4];
-#pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                const float by = S8 ? unit[c] * k_up : unit[c];
-                if (partial) {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        const int key = k0 + 16 * (i / 8) + 8 * half + i % 8;
-                        sc[c][i / 16][i % 16] = key >= lo[c] && key <= hi[c] ? sc[c][i / 16][i % 16] : NONE;
-                    }
-                }
-                float top = sc[c][0][0];
-#pragma unroll
-                for (int i = 1; i < 32; ++i) top = fmaxf(top, sc[c][i / 16][i % 16]);
-                top = fmaxf(top, other_half(top)) * by;
-                if (__any(top > m[c] + ROOM)) {
-                    const float mn = fmaxf(m[c], top), fade = __builtin_amdgcn_exp2f(m[c] - (mn == NONE ? 0.0f : mn));
-                    m[c] = mn;
-                    l[c] *= fade;
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) o[c][d] *= fade;
-                }
-                const float ms = m[c] == NONE ? 0.0f : m[c];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float x[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) x[j] = __builtin_amdgcn_exp2f(__fmaf_rn(sc[c][e / 2][e % 2 * 8 + j], by, -ms));
-                    if constexpr (S8) {
-                        f16x8 w;
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) w[j] = (_Float16)x[j];
-                        l[c] = sum_of(w, l[c]);
-                        p[c][e] = __builtin_bit_cast(u32x4, w);
-                    } else {
-                        bf16x8 w;
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) w[j] = (__bf16)x[j];
-                        l[c] = sum_of(w, l[c]);
-                        p[c][e] = __builtin_bit_cast(u32x4, w);
-                    }
-                }
-            }
-#pragma unroll
-            for (int d = 0; d < DT; ++d) {
-                const int row = 32 * d + col;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const u32x4 x = __builtin_bit_cast(u32x4, t.v[row * 8 + turned<8>(row, 2 * e + half)]);
-#pragma unroll
-                    for (int c = 0; c < NC; ++c) {
-                        if constexpr (S8) o[c][d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, p[c][e]), o[c][d], 0, 0, 0);
-                        else o[c][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, p[c][e]), o[c][d], 0, 0, 0);
-                    }
-                }
+                    for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
             }
         };
+        if constexpr (ahead) {
+            products([&](const int i) INLINE {
+                if (i % DT == DT - 1) fetch(i / DT);
+            });
+        } else if (t > 0) {
+            weigh(k0 - TILE, k_up_last, fetch);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) fetch(i);
+        }
+        if (GROUPS > 1) asm volatile("s_barrier" ::: "memory");
+        if constexpr (!ahead) products(nothing);
+        else if (more) weigh(k0, k_up, nothing);
+        if (more) widen_codes(k_next, v_now, k0);
+        __syncthreads();
+        if (more && (k0 < all_from || k0 + TILE - 1 > all_to)) {
+            clean(v_now, k0);
+            __syncthreads();
+        }
+    };
+    const auto walk = [&](auto is_ahead) INLINE {
+        for (int t = 0; t <= n; t += 2) {
+            step(is_ahead, keys0, keys1, values0, values1, t);
+            if (t + 1 <= n) step(is_ahead, keys1, keys0, values1, values0, t + 1);
+        }
+    };
+    if (n) {
+        if (GROUPS == 1 || wave < 4) walk(std::true_type{});
+        else walk(std::false_type{});
+    }
 
-        if (tid == 0) odd_found = 0;
-        const int first = (blk.tile0 + u0) * TILE, last = (blk.tile0 + u1) * TILE;
-        const int end = min(last, seen_to + 1);        // (what nobody sees has no tiles, but for one where nothing is seen)
-        if (first < end) {
-            if constexpr (S8) {
-                fetch_codes(first);
-                widen_codes(tile0, first);
-            } else {
-                name(first);
-                fetch(tile0, first);
-            }
+    float* const slot = SPLIT ? a.work + (((int64_t)b * blocks + j) * H + h) * parts * part_floats(DIM, BLOCK<GROUPS>) + part * part_floats(DIM, BLOCK<GROUPS>) : nullptr;
+    l += other_half(l);
+    int i = mine;
+    asm volatile("" : "+v"(i));     // (or addresses of results are worked out before the loop, and spilled)
+    if constexpr (SPLIT) {
+        if (half == 0) {
+            slot[wave * 32 + col] = m;
+            slot[BLOCK<GROUPS> + wave * 32 + col] = l;
         }
-        for (int k0 = first; k0 < end; k0 += 2 * TILE) {
-            k_up = k_up_next;
-            __syncthreads();
-            if (k0 + TILE < end) {
-                if constexpr (S8) fetch_codes(k0 + TILE);
-                else fetch(tile1, k0 + TILE);
-            }
-            multiply(tile0, k0);
-            if (k0 + TILE >= end) break;
-            if constexpr (S8) widen_codes(tile1, k0 + TILE);
-            k_up = k_up_next;
-            __syncthreads();
-            if (k0 + 2 * TILE < end) {
-                if constexpr (S8) fetch_codes(k0 + 2 * TILE);
-                else fetch(tile0, k0 + 2 * TILE);
-            }
-            multiply(tile1, k0 + TILE);
-            if constexpr (S8) {
-                if (k0 + 2 * TILE < end) widen_codes(tile0, k0 + 2 * TILE);
-            }
-        }
-
-        const bool whole = !SPLIT || (u0 == 0 && u1 == blk.tiles);
-        float* const slot = SPLIT ? a.work + parts_at((int64_t)a.batch.n_seqs * blocks) + (2 * (int64_t)blockIdx.x + (u0 == 0)) * part_floats(DIM, BLOCK<NC>) : nullptr;
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            l[c] += other_half(l[c]);
-            int i = blk.c0 + (wave * NC + c) * 32 + col;
-            asm volatile("" : "+v"(i));     // (or addresses of results are worked out before the loop, and spilled)
-            if (SPLIT && !whole) {
-                const int w = (wave * NC + c) * 32;
-                if (half == 0) {
-                    slot[w + col] = m[c];
-                    slot[BLOCK<NC> + w + col] = l[c];
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) slot[2 * BLOCK<GROUPS> + wave * 32 * DIM + (d * 16 + r) * 64 + lane] = o[d][r] * (S8 ? v_up : 1.0f);
+    } else if (i < blk.c1) {
+        const float inv = l == 0.0f ? 0.0f : (S8 ? v_up : 1.0f) / l;
+        const int64_t to = ((int64_t)(h * G + i % G) * D + 4 * half) * a.ldo + s.first + i / G;
+        store_type(a, [&](auto* out, auto encode) INLINE {
+            auto* const column = out + to;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int row = 32 * d + 8 * (r / 4) + r % 4;
+                    if (EXACT || row + 4 * half < D) column[row * a.ldo] = encode(l == 0.0f ? 0.0f : o[d][r] * inv);
                 }
-#pragma unroll
-                for (int d = 0; d < DT; ++d)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) slot[2 * BLOCK<NC> + w * DIM + (d * 16 + r) * 64 + lane] = o[c][d][r] * (S8 ? v_up : 1.0f);
-            } else if (i < blk.c1) {
-                const float inv = l[c] == 0.0f ? 0.0f : (S8 ? v_up : 1.0f) / l[c];
-                const int token = i / G, head = h * G + i % G;
-#pragma unroll
-                for (int d = 0; d < DT; ++d)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int row = 32 * d + 8 * (r / 4) + 4 * half + r % 4;
-                        if (EXACT || row < D) store_out(a, ((int64_t)head * D + row) * a.ldo + s.first + token, l[c] == 0.0f ? 0.0f : o[c][d][r] * inv);
-                    }
-            }
+        });
+    }
+    lds_barrier();
+    if (!odd_found) return;
+    __syncthreads();        // (the results are written)
+    for (int i = tid; i < BLOCK<GROUPS> * DIM; i += THREADS) {
+        const int row = i % DIM, c = blk.c0 + i / DIM, token = c / G;
+        float sum;
+        if (c >= blk.c1 || row >= D || !odd_sum<TYPE, TILE>(a, table, last_page, h, row, max(first, s.first_seen(a, token)), min(end - 1, s.last_seen(a, token)), all_from, all_to, &sum))
+            continue;
+        if constexpr (SPLIT) {
+            const int w = i / DIM / 32, r = row % 8;
+            slot[2 * BLOCK<GROUPS> + w * 32 * DIM + (row / 32 * 16 + row % 32 / 8 * 4 + r % 4) * 64 + r / 4 * 32 + i / DIM % 32] = sum;
+        } else {
+            store_out(a, ((int64_t)(h * G + c % G) * D + row) * a.ldo + s.first + token, sum);
         }
-        __syncthreads();        // (the results are written; the tiles are filled again)
-        if (odd_found) {
-            for (int i = tid; i < BLOCK<NC> * DIM; i += THREADS) {
-                const int row = i % DIM, c = blk.c0 + i / DIM, token = c / G;
-                float sum;
-                if (c >= blk.c1 || row >= D || !odd_sum<TYPE, TILE>(a, table, last_page, h, row, max(first, s.first_seen(a, token)), min(end - 1, s.last_seen(a, token)), all_from, all_to, &sum))
-                    continue;
-                if (SPLIT && !whole) {
-                    const int w = i / DIM / 32, r = row % 8;
-                    slot[2 * BLOCK<NC> + w * 32 * DIM + (row / 32 * 16 + row % 32 / 8 * 4 + r % 4) * 64 + r / 4 * 32 + i / DIM % 32] = sum;
-                } else {
-                    store_out(a, ((int64_t)(h * G + c % G) * D + row) * a.ldo + s.first + token, sum);
-                }
-            }
-            __syncthreads();
-        }
-        done += u1 - u0;
-        at += u1 - u0;
-        if constexpr (!SPLIT) return;
     }
 }
 
-// Joins the parts of a block that several runs had a share of, in the order of the keys: a wave for 32 columns and 32 dims.
-template <int DIM, int NC>
-__global__ __launch_bounds__(64) void cache_join_many(const AttendArgs a, const int blocks, const int most)
+// Joins the parts of a block, in the order of the keys: a wave for 32 columns and 32 dims.
+template <int DIM, int GROUPS>
+__global__ __launch_bounds__(64) void cache_join_many(const AttendArgs a, const int blocks, const int parts)
 {
     const int lane = threadIdx.x, col = lane % 32, half = lane / 32, h = blockIdx.y, w = blockIdx.x / (DIM / 32), d = blockIdx.x % (DIM / 32);
-    const int64_t item = blockIdx.z, items = (int64_t)a.batch.n_seqs * blocks;
-    const int64_t* const prefix = (const int64_t*)a.work;
-    const int64_t total = prefix[items], first = prefix[item], n = (prefix[item + 1] - first) / a.pool.n_heads;
-    if (n <= 0) return;
-    const int64_t runs = min((int64_t)most, total);
-    const auto run_of = [&](const int64_t x) { return (int)(((x + 1) * runs - 1) / total); };
-    const int w0 = run_of(first + h * n), w1 = run_of(first + (h + 1) * n - 1);
-    if (w0 == w1) return;
-    const Sequence s = sequence(a, (int)(item / blocks));
-    const Block blk = block_of(a, s, (int)(item % blocks), BLOCK<NC>);
-    const float* const parts = a.work + parts_at(items);
-    const auto part_of = [&](const int x) { return parts + (2 * (int64_t)x + (x == w0)) * part_floats(DIM, BLOCK<NC>); };
-    float top = NONE;
-    for (int x = w0; x <= w1; ++x) top = fmaxf(top, part_of(x)[w * 32 + col]);
-    const float ms = top == NONE ? 0.0f : top;
-    float all = 0.0f, y[16];
+    const int b = (int)(blockIdx.z / (uint32_t)blocks), j = (int)(blockIdx.z % (uint32_t)blocks);
+    const Sequence s = sequence(a, b);
+    const Block blk = block_of(a, s, j, BLOCK<GROUPS>);
+    const int i = blk.c0 + w * 32 + col;
+    if (blk.tiles == 0 || blk.c0 + w * 32 >= blk.c1) return;
+    const float* const first = a.work + (((int64_t)b * blocks + j) * a.pool.n_heads + h) * parts * part_floats(DIM, BLOCK<GROUPS>);
+    float top = NONE, all = 0.0f, y[16];
 #pragma unroll
     for (int r = 0; r < 16; ++r) y[r] = 0.0f;
-    for (int x = w0; x <= w1; ++x) {
-        const float* const p = part_of(x);
-        const float share = __builtin_amdgcn_exp2f(p[w * 32 + col] - ms);
-        all += p[BLOCK<NC> + w * 32 + col] * share;
+#pragma unroll 2
+    for (int x = 0; x < parts; ++x) {
+        if ((int64_t)blk.tiles * x / parts == (int64_t)blk.tiles * (x + 1) / parts) continue;       // (a part of no tiles)
+        const float* const p = first + x * part_floats(DIM, BLOCK<GROUPS>);
+        const float m = p[w * 32 + col], l = p[BLOCK<GROUPS> + w * 32 + col], mn = fmaxf(top, m), ms = mn == NONE ? 0.0f : mn;
+        const float fade = __builtin_amdgcn_exp2f(top - ms), share = __builtin_amdgcn_exp2f(m - ms);
+        top = mn;
+        all = all * fade + l * share;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) y[r] += p[2 * BLOCK<NC> + w * 32 * DIM + (d * 16 + r) * 64 + lane] * share;
+        for (int r = 0; r < 16; ++r) y[r] = y[r] * fade + p[2 * BLOCK<GROUPS> + w * 32 * DIM + (d * 16 + r) * 64 + lane] * share;
     }
-    const int i = blk.c0 + w * 32 + col;
     if (i >= blk.c1) return;
     const float inv = all == 0.0f ? 0.0f : 1.0f / all;
     const int token = i / a.group, head = h * a.group + i % a.group;
@@ -578,21 +592,35 @@ __global__ __launch_bounds__(64) void cache_join_many(const AttendArgs a, const 
     }
 }
 
-// Whether there are too few blocks to go round, and how many blocks a sequence has.
-template <int NC>
-static bool split(const int64_t n_seqs, const int n_heads, const int64_t cols, int* const blocks)
+// Blocks of 256 columns for 8 bits, where they fill the matrix instructions nearly as well as blocks of 128 do.
+static bool wide_blocks(const spmm_cache_type_t type, const int64_t cols)
 {
-    *blocks = (int)((cols + BLOCK<NC> - 1) / BLOCK<NC>);
-    return n_seqs * n_heads * *blocks < 2 * CUS * PER_CU<NC>;
+    if (type != SPMM_CACHE_S8) return false;
+    return (cols + 255) / 256 * 16 <= (cols + 127) / 128 * 9;        // (at most 9 / 8 of the padded columns)
 }
 
-constexpr int TILES_OF_COLUMNS = 1;     // of a wave
+// How many blocks a sequence has, and workgroups a block: more than one where the device could run two for each block.
+template <int GROUPS>
+static int parts_of(const int64_t n_seqs, const int n_heads, const int64_t cols, const int64_t tiles, int* const blocks)
+{
+    *blocks = (int)((cols + BLOCK<GROUPS> - 1) / BLOCK<GROUPS>);
+    const int64_t parts = ROUND<GROUPS> / (n_seqs * n_heads * *blocks);
+    return (int)(parts < 2 ? 1 : parts < tiles ? parts : tiles);
+}
 
-int64_t many_work_bytes(const int64_t n_seqs, const int n_heads, const int dim, const int64_t cols)
+static int64_t tiles_of(const int64_t tokens) { return (tokens + TILE - 1) / TILE; }
+
+template <int GROUPS>
+static int64_t work_bytes(const int64_t n_seqs, const int n_heads, const int dim, const int64_t cols)
 {
     int blocks;
-    if (!split<TILES_OF_COLUMNS>(n_seqs, n_heads, cols, &blocks)) return 16;
-    return 4 * (parts_at(n_seqs * blocks) + (int64_t)2 * CUS * PER_CU<TILES_OF_COLUMNS> * part_floats(dim > 64 ? 128 : 64, BLOCK<TILES_OF_COLUMNS>));
+    const int64_t parts = parts_of<GROUPS>(n_seqs, n_heads, cols, ROUND<GROUPS>, &blocks);
+    return parts < 2 ? 16 : 4 * n_seqs * n_heads * blocks * parts * part_floats(dim > 64 ? 128 : 64, BLOCK<GROUPS>);
+}
+
+int64_t many_work_bytes(const spmm_cache_type_t type, const int64_t n_seqs, const int n_heads, const int dim, const int64_t cols)
+{
+    return wide_blocks(type, cols) ? work_bytes<2>(n_seqs, n_heads, dim, cols) : work_bytes<1>(n_seqs, n_heads, dim, cols);
 }
 
 static int launch_two(const void* kernel, const dim3 grid, const dim3 block, const AttendArgs& a, int x, int y, void* stream)
@@ -601,29 +629,31 @@ static int launch_two(const void* kernel, const dim3 grid, const dim3 block, con
     return (int)hipLaunchKernel(kernel, grid, block, args, 0, (hipStream_t)stream);
 }
 
-template <int DIM, spmm_cache_type_t TYPE, int NC>
+template <int DIM, spmm_cache_type_t TYPE, int GROUPS>
 static int launch_typed(const AttendArgs& a, void* stream)
 {
     int blocks;
-    const bool parts = split<NC>(a.batch.n_seqs, a.pool.n_heads, (int64_t)a.max_new * a.group, &blocks), exact = a.pool.head_dim == DIM;
-    const int64_t all = (int64_t)a.batch.n_seqs * a.pool.n_heads * blocks;
-    if (!parts) {
-        const dim3 grid((unsigned)((all + XCDS - 1) / XCDS * XCDS));
-        return launch_two(exact ? (const void*)cache_attend_many<DIM, TYPE, true, NC, false> : (const void*)cache_attend_many<DIM, TYPE, false, NC, false>, grid,
-                          dim3(THREADS), a, blocks, 0, stream);
-    }
-    constexpr int runs = CUS * PER_CU<NC>;
-    const int rc = launch_two(exact ? (const void*)cache_attend_many<DIM, TYPE, true, NC, true> : (const void*)cache_attend_many<DIM, TYPE, false, NC, true>, dim3(runs),
-                              dim3(THREADS), a, blocks, 0, stream);
-    if (rc) return rc;
-    return launch_two((const void*)cache_join_many<DIM, NC>, dim3(WAVES * NC * (DIM / 32), a.pool.n_heads, a.batch.n_seqs * blocks), dim3(64), a, blocks, runs, stream);
+    const int parts = parts_of<GROUPS>(a.batch.n_seqs, a.pool.n_heads, (int64_t)a.max_new * a.group, tiles_of(a.batch.ld_table << a.pool.page_shift), &blocks);
+    const int64_t all = (int64_t)a.batch.n_seqs * a.pool.n_heads * blocks * parts;
+    const bool exact = a.pool.head_dim == DIM;
+    const void* const kernel =
+        parts > 1 ? exact ? (const void*)cache_attend_many<DIM, TYPE, true, GROUPS, true> : (const void*)cache_attend_many<DIM, TYPE, false, GROUPS, true>
+                  : exact ? (const void*)cache_attend_many<DIM, TYPE, true, GROUPS, false> : (const void*)cache_attend_many<DIM, TYPE, false, GROUPS, false>;
+    const int rc = launch_two(kernel, dim3((unsigned)((all + XCDS - 1) / XCDS * XCDS)), dim3(256 * GROUPS), a, blocks, parts, stream);
+    if (rc || parts < 2) return rc;
+    return launch_two((const void*)cache_join_many<DIM, GROUPS>, dim3(4 * GROUPS * (DIM / 32), a.pool.n_heads, a.batch.n_seqs * blocks), dim3(64), a, blocks, parts, stream);
+}
+
+template <int DIM>
+static int launch_dim(const AttendArgs& a, const spmm_cache_type_t type, void* stream)
+{
+    if (type == SPMM_CACHE_BF16) return launch_typed<DIM, SPMM_CACHE_BF16, 1>(a, stream);
+    return wide_blocks(type, (int64_t)a.max_new * a.group) ? launch_typed<DIM, SPMM_CACHE_S8, 2>(a, stream) : launch_typed<DIM, SPMM_CACHE_S8, 1>(a, stream);
 }
 
 int launch_attend_many(const AttendArgs& a, const spmm_cache_type_t type, void* stream)
 {
-    constexpr int NC = TILES_OF_COLUMNS;
-    if (a.pool.head_dim > 64) return type == SPMM_CACHE_S8 ? launch_typed<128, SPMM_CACHE_S8, NC>(a, stream) : launch_typed<128, SPMM_CACHE_BF16, NC>(a, stream);
-    return type == SPMM_CACHE_S8 ? launch_typed<64, SPMM_CACHE_S8, NC>(a, stream) : launch_typed<64, SPMM_CACHE_BF16, NC>(a, stream);
+    return a.pool.head_dim > 64 ? launch_dim<128>(a, type, stream) : launch_dim<64>(a, type, stream);
 }
 
 }  // namespace spmm_cache

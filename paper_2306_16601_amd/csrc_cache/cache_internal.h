@@ -80,8 +80,8 @@ int launch_attend(const AttendArgs& a, spmm_cache_type_t type, void* stream);
 int launch_attend_few(const AttendArgs& a, spmm_cache_type_t type, void* stream);
 int64_t few_work_bytes(int64_t n_seqs, int dim, int64_t cols);
 int launch_attend_many(const AttendArgs& a, spmm_cache_type_t type, void* stream);
-int64_t many_work_bytes(int64_t n_seqs, int n_heads, int dim, int64_t cols);
-int64_t attend_work_bytes(int64_t n_seqs, int32_t n_heads, int32_t group, int32_t head_dim, int64_t max_new);
+int64_t many_work_bytes(spmm_cache_type_t type, int64_t n_seqs, int n_heads, int dim, int64_t cols);
+int64_t attend_work_bytes(spmm_cache_type_t type, int64_t n_seqs, int32_t n_heads, int32_t group, int32_t head_dim, int64_t max_new);
 int launch_copy(const CopyArgs& a, void* stream);
 int launch_fork(const ForkArgs& a, const CopyArgs& c, void* stream);
 int launch_compact(const CompactArgs& a, const CopyArgs& c, void* stream);
