@@ -34,6 +34,8 @@ WIDE = [(tm, nw, maxs) for tm, nw in ((128, 8), (96, 8), (64, 8), (64, 4), (32, 
 HEADERS = [os.path.join(CSRC, "spmm_internal.h"), os.path.join(CSRC, "spmm_kernels.h"), os.path.join(CSRC, "spmm_wide.h"), os.path.join(CSRC, "team.h"),
            os.path.join(ROOT, "include", "spmm.h")]
 
+CACHE_NATIVE = os.path.join(HERE, "_native_cache.so")
+CACHE_NATIVE_SOURCE = os.path.join(CACHE_CSRC, "native_cache.c")
 CACHE_SOURCES = ["cache_api.cpp", "cache_append.hip", "cache_attend.cpp", "cache_attend_few.hip", "cache_attend_many.hip", "cache_pages.hip"]
 CACHE_HEADERS = [os.path.join(CACHE_CSRC, "cache_internal.h"), os.path.join(CACHE_CSRC, "cache_attend.h"), os.path.join(ROOT, "include", "spmm_cache.h")]
 
@@ -86,19 +88,20 @@ def _run(cmd, verbose):
 
 
 def build_native(verbose: bool = False) -> str:
-    """Compile the CPython module that marshals the launch calls."""
-    tmp = NATIVE + ".tmp.%d" % os.getpid()
-    _run([os.environ.get("CC", "gcc"), "-O2", "-std=gnu11", "-shared", "-fPIC", "-Wall",
-          "-I", sysconfig.get_paths()["include"], "-I", os.path.join(ROOT, "include"), NATIVE_SOURCE, "-o", tmp], verbose)
-    os.replace(tmp, NATIVE)
+    """Compile the CPython modules that marshal the launch calls."""
+    for source, target in ((NATIVE_SOURCE, NATIVE), (CACHE_NATIVE_SOURCE, CACHE_NATIVE)):
+        tmp = target + ".tmp.%d" % os.getpid()
+        _run([os.environ.get("CC", "gcc"), "-O2", "-std=gnu11", "-shared", "-fPIC", "-Wall",
+              "-I", sysconfig.get_paths()["include"], "-I", os.path.join(ROOT, "include"), source, "-o", tmp], verbose)
+        os.replace(tmp, target)
     return NATIVE
 
 
 def build(force: bool = True, verbose: bool = False, jobs: int | None = None) -> str:
     """Compile every source with hipcc (cross-compiles without a GPU) and link the library."""
-    deps = sources() + HEADERS + [u[1] for u in cache_units()] + CACHE_HEADERS + [NATIVE_SOURCE]
+    deps = sources() + HEADERS + [u[1] for u in cache_units()] + CACHE_HEADERS + [NATIVE_SOURCE, CACHE_NATIVE_SOURCE]
     if not force and all(os.path.exists(b) and all(os.path.getmtime(b) >= os.path.getmtime(d) for d in deps)
-                         for b in (LIB, NATIVE)):
+                         for b in (LIB, NATIVE, CACHE_NATIVE)):
         return LIB
     build_native(verbose)
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -1,11 +1,15 @@
 """Binding of the paged key/value cache (include/spmm_cache.h): argument marshalling and checks of tensors.
 
 Functions have the names of their C declarations.  Device operands are torch tensors, whose types, layouts and sizes are
-checked here, or raw integer addresses, which are not; sizes that a tensor's shape says are taken from it.
+checked here, or raw integer addresses, which are not; sizes that a tensor's shape says are taken from it.  What is as it
+should be is marshalled in C (csrc_cache/native_cache.c, which takes the place of the functions here at the end of this
+file and hands everything else back to them).
 """
 from __future__ import annotations
 
 import ctypes
+import importlib.util
+import os
 from typing import Optional
 
 from .binding import OUT_TYPES, SPMM_OUT_F32, SPMM_OUT_S8, SPMM_OUT_U8, _check, _nbytes, lib
@@ -46,7 +50,7 @@ class spmm_attend_t(ctypes.Structure):
                 ("out_scale", _f32), ("out_zero_point", _i32)]
 
 
-_bound = None
+_bound = _native = None
 
 
 def _functions() -> ctypes.CDLL:
@@ -65,8 +69,16 @@ def _functions() -> ctypes.CDLL:
                 ("spmm_cache_work_bytes", [cache, _i64, ctypes.POINTER(_i64)])):
             f = getattr(L, name)
             f.restype, f.argtypes = ctypes.c_int, args
+        if _native is not None:
+            _native.bind(*(ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in (
+                "spmm_cache_append", "spmm_cache_attend", "spmm_attend_work_bytes", "spmm_cache_fork", "spmm_cache_compact", "spmm_cache_work_bytes")))
         _bound = L
     return _bound
+
+
+def _struct(v, kind):
+    """A description as a ctypes structure (those made in C hold the same bytes)."""
+    return v if isinstance(v, kind) else kind.from_buffer_copy(v)
 
 
 def _name(t) -> str:
@@ -154,45 +166,51 @@ def _matrix(t, what: str, dtype: Optional[str], rows: int, cols: int, ld: int):
 
 def spmm_cache_append(cache: spmm_cache_t, layer: int, batch: spmm_batch_t, x, T: int, ldx: int, how: spmm_append_t, q, stream=None) -> None:
     """New tokens' queries to q, their keys and values to the cache; asynchronous on `stream` (a raw hipStream_t value, None = default stream)."""
+    keep = getattr(how, "_keepalive", (None,) * 4)
+    cache, batch, how = _struct(cache, spmm_cache_t), _struct(batch, spmm_batch_t), _struct(how, spmm_append_t)
     rows = (how.q_heads + 2 * cache.n_heads) * cache.head_dim
-    for w in (how._keepalive[:2] if hasattr(how, "_keepalive") else ()):
+    for w in keep[:2]:
         _tensor(w, "weight", "float32", need=cache.head_dim)
-    if getattr(how, "_keepalive", (None,) * 4)[3] is not None:
-        _tensor(how._keepalive[3], "positions", "int32", need=T)
+    if keep[3] is not None:
+        _tensor(keep[3], "positions", "int32", need=T)
     _check(_functions().spmm_cache_append(cache, layer, batch, _matrix(x, "x", _X_TYPES.get(how.x_type), rows, T, ldx), T, ldx, how,
                                           _tensor(q, "q", "bfloat16", need=T * how.q_heads * cache.head_dim), stream), "spmm_cache_append")
 
 
 def spmm_attend_work_bytes(cache: spmm_cache_t, n_seqs: int, T: int, how: spmm_attend_t) -> int:
     n = _i64()
+    cache, how = _struct(cache, spmm_cache_t), _struct(how, spmm_attend_t)
     _check(_functions().spmm_attend_work_bytes(cache, n_seqs, T, how, n), "spmm_attend_work_bytes")
     return n.value
 
 
 def spmm_cache_attend(cache: spmm_cache_t, layer: int, batch: spmm_batch_t, q, T: int, how: spmm_attend_t, out, ldo: int, work, stream=None) -> None:
     """out [q_heads * head_dim][ldo] = attention of the new tokens; work: a tensor of spmm_attend_work_bytes bytes."""
+    cache, batch, how = _struct(cache, spmm_cache_t), _struct(batch, spmm_batch_t), _struct(how, spmm_attend_t)
     values = how.q_heads * cache.head_dim
-    if work is not None and not isinstance(work, int) and _nbytes(work) < spmm_attend_work_bytes(cache, batch.n_seqs, T, how):
-        raise ValueError("work holds %d bytes, %d are wanted" % (_nbytes(work), spmm_attend_work_bytes(cache, batch.n_seqs, T, how)))
+    if work is not None and not isinstance(work, int) and _nbytes(work) < _in_python["spmm_attend_work_bytes"](cache, batch.n_seqs, T, how):
+        raise ValueError("work holds %d bytes, %d are wanted" % (_nbytes(work), _in_python["spmm_attend_work_bytes"](cache, batch.n_seqs, T, how)))
     _check(_functions().spmm_cache_attend(cache, layer, batch, _tensor(q, "q", "bfloat16", need=T * values), T, how,
                                           _matrix(out, "out", _O_TYPES.get(how.out_type), values, T, ldo), ldo, work if work is None or isinstance(work, int) else _address(work, "work"), stream), "spmm_cache_attend")
 
 
 def spmm_cache_work_bytes(cache: spmm_cache_t, n_rows: int) -> int:
     n = _i64()
+    cache = _struct(cache, spmm_cache_t)
     _check(_functions().spmm_cache_work_bytes(cache, n_rows, n), "spmm_cache_work_bytes")
     return n.value
 
 
 def _page_work(cache, n_rows, work):
-    if work is not None and not isinstance(work, int) and _nbytes(work) < spmm_cache_work_bytes(cache, n_rows):
-        raise ValueError("work holds %d bytes, %d are wanted" % (_nbytes(work), spmm_cache_work_bytes(cache, n_rows)))
+    if work is not None and not isinstance(work, int) and _nbytes(work) < _in_python["spmm_cache_work_bytes"](cache, n_rows):
+        raise ValueError("work holds %d bytes, %d are wanted" % (_nbytes(work), _in_python["spmm_cache_work_bytes"](cache, n_rows)))
     return work if work is None or isinstance(work, int) else _address(work, "work")
 
 
 def spmm_cache_fork(cache: spmm_cache_t, table, kv_len, parent, keep, want, table_out, kv_len_out, info, work, stream=None) -> None:
     """The next generation of the sequences: int32 tensors table [rows, width], kv_len [rows] -> table_out [new rows, width], kv_len_out;
     parent, keep, want [new rows]; info [4]; work: spmm_cache_work_bytes bytes."""
+    cache = _struct(cache, spmm_cache_t)
     (rows_in, width), rows = table.shape, table_out.shape[0]
     i = "int32"
     _check(_functions().spmm_cache_fork(
@@ -203,6 +221,7 @@ def spmm_cache_fork(cache: spmm_cache_t, table, kv_len, parent, keep, want, tabl
 
 def spmm_cache_compact(cache: spmm_cache_t, table, table_out, info, work, stream=None) -> None:
     """Pages in use to the front of the pool; table_out (which may be table) takes the new numbers."""
+    cache = _struct(cache, spmm_cache_t)
     rows, width = table.shape
     _check(_functions().spmm_cache_compact(cache, _tensor(table, "table", "int32"), width, rows, _tensor(table_out, "table_out", "int32", (rows, width)),
                                            _tensor(info, "info", "int32", need=4), _page_work(cache, rows, work), stream), "spmm_cache_compact")
@@ -210,4 +229,18 @@ def spmm_cache_compact(cache: spmm_cache_t, table, table_out, info, work, stream
 
 def spmm_cache_copy(cache: spmm_cache_t, src, dst, n: int, stream=None) -> None:
     """Pages src[i] to dst[i] in all layers, i < n (int32 tensors)."""
+    cache = _struct(cache, spmm_cache_t)
     _check(_functions().spmm_cache_copy(cache, _tensor(src, "src", "int32", need=n), _tensor(dst, "dst", "int32", need=n), n, stream), "spmm_cache_copy")
+
+
+_FAST = ("make_cache", "make_batch", "make_append", "make_attend", "spmm_cache_append", "spmm_cache_attend", "spmm_attend_work_bytes", "spmm_cache_fork",
+         "spmm_cache_compact", "spmm_cache_work_bytes")
+NATIVE_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "_native_cache.so")
+_in_python = {n: globals()[n] for n in _FAST}       # (the tests of the checks call these too)
+
+if os.path.exists(NATIVE_PATH):
+    _spec = importlib.util.spec_from_file_location(__package__ + "._native_cache", NATIVE_PATH)
+    _native = importlib.util.module_from_spec(_spec)
+    _spec.loader.exec_module(_native)
+    _native.hooks(_check, *_in_python.values())
+    globals().update({n: getattr(_native, n) for n in _FAST})

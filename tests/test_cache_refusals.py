@@ -145,9 +145,8 @@ def test_the_binding_checks_tensors():
     refused(lambda: sp.spmm_cache_append(CACHE, 0, BATCH, P, 9, 9, how, q), device=True)
     refused(lambda: sp.spmm_cache_attend(CACHE, 0, BATCH, P, 9, att, out, 9, P), device=True)
     refused(lambda: sp.spmm_cache_attend(CACHE, 0, BATCH, P, 9, att, P, 9, work), device=True)
-    weights = changed(how)
+    weights, places = changed(APPEND), changed(APPEND)
     weights._keepalive = (torch.zeros(63), None, None, None)
-    places = changed(how)
     places._keepalive = (None, None, None, ints(8))
     for bad in (lambda: sp.spmm_cache_append(CACHE, 0, BATCH, x[:-1].clone(), 9, 9, how, P), lambda: sp.spmm_cache_append(CACHE, 0, BATCH, x, 9, 10, how, P),
                 lambda: sp.spmm_cache_append(CACHE, 0, BATCH, x.double(), 9, 9, how, P), lambda: sp.spmm_cache_append(CACHE, 0, BATCH, P, 9, 9, how, q[:8]),
