@@ -10,6 +10,7 @@ namespace {
 constexpr int64_t TABLE_TOKENS = (int64_t)1 << 30;      // most tokens that a row of a page table may name
 constexpr int64_t MOST_ROWS = (int64_t)1 << 20;         // of a page table
 constexpr int64_t MOST_ENTRIES = ((int64_t)1 << 31) - 1;
+constexpr int64_t MOST_BLOCKS = (int64_t)1 << 22;       // of 128 columns, of all sequences and heads: the same
 constexpr int64_t MOST_COLUMNS = (int64_t)1 << 27;      // tokens times query heads: a grid's size
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -175,7 +176,8 @@ spmm_status_t spmm_cache_attend(const spmm_cache_t* cache, int32_t layer, const 
         return SPMM_E_ARG;
     const int esz = ot == SPMM_OUT_F32 ? 4 : ot == SPMM_OUT_BF16 ? 2 : 1;
     if ((reinterpret_cast<uintptr_t>(out) & (esz - 1)) || ldo > (int64_t)1 << 40) return (ldo > (int64_t)1 << 40) ? SPMM_E_UNSUPPORTED : SPMM_E_ARG;
-    if (batch->n_seqs > 65535) return SPMM_E_UNSUPPORTED;
+    const int64_t max_new = how->max_new < T ? how->max_new : T;
+    if (batch->n_seqs > 65535 || batch->n_seqs * cache->n_heads > MOST_BLOCKS / ((max_new * (how->q_heads / cache->n_heads) + 127) / 128)) return SPMM_E_UNSUPPORTED;
 
     AttendArgs a = {};
     a.pool = pool_of(cache, layer);
@@ -186,7 +188,7 @@ spmm_status_t spmm_cache_attend(const spmm_cache_t* cache, int32_t layer, const 
     a.ldo = ldo;
     a.T = (int32_t)T;
     a.group = how->q_heads / cache->n_heads;
-    a.max_new = (int32_t)(how->max_new < T ? how->max_new : T);
+    a.max_new = (int32_t)max_new;
     a.causal = how->causal != 0;
     a.window = how->window;
     a.out_type = ot;
@@ -240,7 +242,7 @@ spmm_status_t spmm_cache_fork(const spmm_cache_t* cache, const int32_t* table, i
     c.src = a.src;
     c.dst = a.dst;
     c.count = a.count;
-    c.most = (int32_t)p.most;
+    c.most = (int32_t)n_rows;       // (a row copies one page at most)
     return status_of(launch_fork(a, c, hip_stream));
 }
 
@@ -267,7 +269,8 @@ spmm_status_t spmm_cache_compact(const spmm_cache_t* cache, const int32_t* table
     c.src = a.src;
     c.dst = a.dst;
     c.count = a.count;
-    c.most = (int32_t)p.most;
+    const int64_t half = cache->n_pages / 2;        // (holes and pages behind them are as many, and no page is both)
+    c.most = (int32_t)(half < a.entries ? half > 1 ? half : 1 : a.entries);
     return status_of(launch_compact(a, c, hip_stream));
 }
 

@@ -19,6 +19,8 @@ constexpr int COLS = 16;            // columns of a tile
 template <int DIM, int NC>
 constexpr int PER_CU = DIM > 64 && NC > 1 ? 1 : 2;
 constexpr int CUS = 256;
+// keys up to which a workgroup takes a whole head: nothing to join
+constexpr int64_t SHORT = 1024;
 
 template <spmm_cache_type_t TYPE>
 constexpr int KEYS = TYPE == SPMM_CACHE_S8 ? 64 : 32;       // of a wave's step
@@ -60,6 +62,16 @@ __device__ __forceinline__ int64_t before(const int64_t v, int64_t* const all)
     return base + s - v;
 }
 
+// x / y, and x's share of i of n: in 32 bits where they suffice (a division of 64 takes a hundred instructions)
+__device__ __forceinline__ int quotient(const int64_t x, const int64_t y)
+{
+    return (x | y) >> 32 ? (int)(x / y) : (int)((uint32_t)x / (uint32_t)y);
+}
+__device__ __forceinline__ int64_t share_of(const int64_t x, const int64_t i, const int64_t n)
+{
+    return x >> 22 ? x * i / n : (int64_t)((uint32_t)x * (uint32_t)i / (uint32_t)n);       // (i and n are at most 2^10)
+}
+
 __device__ __forceinline__ int uniform(const int v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ __forceinline__ int64_t uniform(const int64_t v)
 {
@@ -77,7 +89,7 @@ struct Loads {
     static constexpr int LANE = 16 / BYTES;             // elements of a register
 };
 
-template <int DIM, spmm_cache_type_t TYPE, bool EXACT, int NC>
+template <int DIM, spmm_cache_type_t TYPE, bool EXACT, int NC, bool WHOLE>
 __global__ __launch_bounds__(THREADS, (PER_CU<DIM, NC>)) void cache_attend_few(const AttendArgs a)
 {
     using L = Loads<DIM, TYPE>;
@@ -92,54 +104,61 @@ __global__ __launch_bounds__(THREADS, (PER_CU<DIM, NC>)) void cache_attend_few(c
     const int D = EXACT ? DIM : a.pool.head_dim, G = a.group, H = a.pool.n_heads, shift = a.pool.page_shift, inside = (1 << shift) - 1;
     const int n_seqs = a.batch.n_seqs;
 
-    // the run: units from .. to - 1 of all, beginning `at` units into sequence b
-    int64_t* const prefix = (int64_t*)a.work;
-    int64_t total = 0;
-    int64_t mine = 0, ahead = 0;        // units of this thread's sequence, and before it
-    for (int b0 = 0; b0 < n_seqs; b0 += THREADS) {
-        int skip;
-        mine = b0 + tid < n_seqs ? (int64_t)units_of<TYPE>(a, sequence(a, b0 + tid), &skip) * H : 0;
-        int64_t all;
-        ahead = total + before(mine, &all);
-        if (blockIdx.x == 0 && b0 + tid < n_seqs) prefix[b0 + tid] = ahead;
-        total += all;
-    }
-    if (blockIdx.x == 0 && tid == 0) prefix[n_seqs] = total;
-    const int64_t runs = min((int64_t)gridDim.x, total);        // none is empty
-    if (blockIdx.x >= runs) return;
-    const int64_t from = blockIdx.x * total / runs, to = (blockIdx.x + 1) * total / runs;
-    int64_t sum = n_seqs <= THREADS ? 0 : total;
-    for (int b0 = 0; b0 < n_seqs; b0 += THREADS) {
-        if (n_seqs > THREADS) {
-            if (b0 == 0) sum = 0;
+    int b;
+    int64_t at, from = 0, to = 1;
+    if constexpr (WHOLE) {
+        b = (int)(blockIdx.x / (uint32_t)H);
+        at = blockIdx.x % (uint32_t)H;      // (the head; its units below)
+    } else {
+        // the run: units from .. to - 1 of all, beginning `at` units into sequence b
+        int64_t* const prefix = (int64_t*)a.work;
+        int64_t total = 0, sum = 0;
+        int64_t mine = 0, ahead = 0;        // units of this thread's sequence, and before it
+        for (int b0 = 0; b0 < n_seqs; b0 += THREADS) {
             int skip;
             mine = b0 + tid < n_seqs ? (int64_t)units_of<TYPE>(a, sequence(a, b0 + tid), &skip) * H : 0;
             int64_t all;
-            ahead = sum + before(mine, &all);
-            sum += all;
-        } else {
-            sum = total;
+            ahead = total + before(mine, &all);
+            if (blockIdx.x == 0 && b0 + tid < n_seqs) prefix[b0 + tid] = ahead;
+            total += all;
         }
-        if (from >= ahead && from < ahead + mine) {
-            found[0] = b0 + tid;
-            found[1] = from - ahead;
+        if (blockIdx.x == 0 && tid == 0) prefix[n_seqs] = total;
+        const int64_t runs = min((int64_t)gridDim.x, total);        // none is empty
+        if (blockIdx.x >= runs) return;
+        from = share_of(total, blockIdx.x, runs);
+        to = share_of(total, blockIdx.x + 1, runs);
+        for (int b0 = 0; b0 < n_seqs; b0 += THREADS) {
+            if (n_seqs > THREADS) {
+                int skip;
+                mine = b0 + tid < n_seqs ? (int64_t)units_of<TYPE>(a, sequence(a, b0 + tid), &skip) * H : 0;
+                int64_t all;
+                ahead = sum + before(mine, &all);
+                sum += all;
+            } else {
+                sum = total;
+            }
+            if (from >= ahead && from < ahead + mine) {
+                found[0] = b0 + tid;
+                found[1] = from - ahead;
+            }
+            if (from < sum) break;
         }
-        if (from < sum) break;
+        __syncthreads();
+        b = uniform((int)found[0]);
+        at = uniform(found[1]);
     }
-    __syncthreads();
-    int b = uniform((int)found[0]);
-    int64_t at = uniform(found[1]);
 
     for (int64_t done = from; done < to;) {
         const Sequence s = sequence(a, b);
         int u_first = 0;
         const int n = units_of<TYPE>(a, s, &u_first);
-        if (n == 0 || at >= (int64_t)n * H) {
+        if (WHOLE && n == 0) return;
+        if (!WHOLE && (n == 0 || at >= (int64_t)n * H)) {
             ++b;
             at = 0;
             continue;
         }
-        const int h = (int)(at / n), u0 = (int)(at % n), u1 = (int)min((int64_t)n, u0 + (to - done));
+        const int h = WHOLE ? (int)at : quotient(at, n), u0 = WHOLE ? 0 : (int)(at - (int64_t)h * n), u1 = WHOLE ? n : (int)min((int64_t)n, u0 + (to - done));
         const int32_t* const table = a.batch.table + b * a.batch.ld_table;
         const int rows = s.tokens * G;
 
@@ -415,7 +434,7 @@ __global__ __launch_bounds__(THREADS, (PER_CU<DIM, NC>)) void cache_attend_few(c
         }
 
         // the waves' parts together: written if they are the whole of the head, else to scratch
-        const bool whole = u0 == 0 && u1 == n;
+        const bool whole = WHOLE || (u0 == 0 && u1 == n);
         int g_out = g;
         asm volatile("" : "+v"(g_out));     // (or the addresses of results are worked out before the loop, and spilled)
         float* const slot = a.work + parts_at(n_seqs) + (2 * (int64_t)blockIdx.x + (u0 == 0)) * part_floats(DIM, NC);
@@ -472,6 +491,7 @@ __global__ __launch_bounds__(THREADS, (PER_CU<DIM, NC>)) void cache_attend_few(c
                 else store_out(a, ((int64_t)(h * G + c % G) * D + row) * a.ldo + s.first + t, sum);
             }
         }
+        if constexpr (WHOLE) return;
         done += u1 - u0;
         at += u1 - u0;
     }
@@ -481,43 +501,66 @@ __global__ __launch_bounds__(THREADS, (PER_CU<DIM, NC>)) void cache_attend_few(c
 template <int DIM, int NC>
 __global__ __launch_bounds__(THREADS) void cache_join(const AttendArgs a, const int most)
 {
-    constexpr int N = DIM / 16;
-    const int b = blockIdx.y, h = blockIdx.x, tid = threadIdx.x, lane = tid % 64, wave = tid / 64, col = lane % 16, g = lane / 16;
+    constexpr int N = DIM / 16, ROWS = NC * N * 4, SLICE = ROWS / 4 / WAVES;      // registers of a part; of a wave of a workgroup of 4
+    constexpr int PARTS = THREADS / COLS / NC;       // whose statistics are read at a time
+    __shared__ float shares[PARTS][NC * COLS], tops[PARTS][NC * COLS], sums[PARTS][NC * COLS];
+    const int b = blockIdx.y, h = blockIdx.x / 4, slice = blockIdx.x % 4, tid = threadIdx.x, lane = tid % 64, wave = tid / 64, col = lane % 16, g = lane / 16;
     const int64_t* const prefix = (const int64_t*)a.work;
-    const int64_t total = prefix[a.batch.n_seqs], first = prefix[b], n = (prefix[b + 1] - first) / a.pool.n_heads;
-    if (n <= 0) return;
-    const int64_t runs = min((int64_t)most, total);
+    const int64_t total = prefix[a.batch.n_seqs], first = prefix[b], next = prefix[b + 1];
+    const Sequence s = sequence(a, b);
+    if (next <= first) return;
+    const int64_t n = quotient(next - first, a.pool.n_heads), runs = min((int64_t)most, total);
     // the run that unit x lies in is the last one that begins at or before it
-    const auto run_of = [&](const int64_t x) { return (int)(((x + 1) * runs - 1) / total); };
+    const auto run_of = [&](const int64_t x) { return quotient((x + 1) * runs - 1, total); };
     const int w0 = run_of(first + h * n), w1 = run_of(first + (h + 1) * n - 1);
     if (w0 == w1) return;
-    const Sequence s = sequence(a, b);
     const int D = a.pool.head_dim, rows = s.tokens * a.group;
     const float* const parts = a.work + parts_at(a.batch.n_seqs);
     const auto part_of = [&](const int w) { return parts + (2 * (int64_t)w + (w == w0)) * part_floats(DIM, NC); };
+
+    // statistics of all parts: a thread has a column of every PARTS-th
+    const int c16 = tid % (NC * COLS), p0 = tid / (NC * COLS);
+    float top = NONE, sum = 0.0f;
+    for (int w = w0 + p0; w <= w1; w += PARTS) {
+        const float* const p = part_of(w);
+        const float m = p[c16], l = p[NC * COLS + c16], mn = fmaxf(top, m), ms = mn == NONE ? 0.0f : mn;
+        sum = sum * __builtin_amdgcn_exp2f(top - ms) + l * __builtin_amdgcn_exp2f(m - ms);
+        top = mn;
+    }
+    tops[p0][c16] = top;
+    sums[p0][c16] = sum;
+    __syncthreads();
+    top = NONE;
+    for (int i = 0; i < PARTS; ++i) top = fmaxf(top, tops[i][c16]);
+    const float ms = top == NONE ? 0.0f : top;
+    sum = 0.0f;
+    for (int i = 0; i < PARTS; ++i) sum += sums[i][c16] * __builtin_amdgcn_exp2f(tops[i][c16] - ms);
+    __syncthreads();
+    if (p0 == 0) sums[0][c16] = sum;
+
+    float y[SLICE];
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-        const int i0 = c * COLS + col;
-        float top = NONE;
-        for (int w = w0; w <= w1; ++w) top = fmaxf(top, part_of(w)[i0]);
-        const float ms = top == NONE ? 0.0f : top;
-        float all = 0.0f, y[N];
+    for (int i = 0; i < SLICE; ++i) y[i] = 0.0f;
+    const int r0 = (slice * WAVES + wave) * SLICE, c = r0 / (N * 4);        // the wave's registers: all of one tile of columns
+    for (int w = w0; w <= w1; w += PARTS) {
+        if (w + p0 <= w1) shares[p0][c16] = __builtin_amdgcn_exp2f(part_of(w + p0)[c16] - ms);
+        __syncthreads();
+#pragma unroll 4
+        for (int x = w; x <= min(w + PARTS - 1, w1); ++x) {
+            const float* const p = part_of(x) + 2 * NC * COLS + r0 * 64 + lane;
+            const float share = shares[x - w][c * COLS + col];
 #pragma unroll
-        for (int i = 0; i < N; ++i) y[i] = 0.0f;
-        for (int w = w0; w <= w1; ++w) {
-            const float* const p = part_of(w);
-            const float share = __builtin_amdgcn_exp2f(p[i0] - ms);
-            all += p[NC * COLS + i0] * share;
-#pragma unroll
-            for (int i = 0; i < N; ++i) y[i] += p[2 * NC * COLS + (c * N * 4 + wave * N + i) * 64 + lane] * share;
+            for (int i = 0; i < SLICE; ++i) y[i] += p[i * 64] * share;
         }
-        const float inv = all == 0.0f ? 0.0f : 1.0f / all;
-        const int token = i0 / a.group, head = h * a.group + i0 % a.group;
+        __syncthreads();
+    }
+    const float all = sums[0][c * COLS + col], inv = all == 0.0f ? 0.0f : 1.0f / all;
+    const int i0 = c * COLS + col, token = i0 / a.group, head = h * a.group + i0 % a.group;
+    if (i0 >= rows) return;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int j = wave * N + i, row = 16 * (j / 4) + 4 * g + j % 4;
-            if (i0 < rows && row < D) store_out(a, ((int64_t)head * D + row) * a.ldo + s.first + token, all == 0.0f ? 0.0f : y[i] * inv);
-        }
+    for (int i = 0; i < SLICE; ++i) {
+        const int j = r0 % (N * 4) + i, row = 16 * (j / 4) + 4 * g + j % 4;
+        if (row < D) store_out(a, ((int64_t)head * D + row) * a.ldo + s.first + token, all == 0.0f ? 0.0f : y[i] * inv);
     }
 }
 
@@ -526,23 +569,30 @@ int64_t few_work_bytes(const int64_t n_seqs, const int dim, const int64_t cols)
     return 4 * (parts_at(n_seqs) + (int64_t)2 * CUS * 2 * part_floats(dim > 64 ? 128 : 64, cols > COLS ? 2 : 1));
 }
 
+template <int DIM, spmm_cache_type_t TYPE, int NC, bool WHOLE>
+static int launch_exact(const AttendArgs& a, const int runs, void* stream)
+{
+    return a.pool.head_dim == DIM ? launch(cache_attend_few<DIM, TYPE, true, NC, WHOLE>, dim3(runs), dim3(THREADS), a, stream)
+                                  : launch(cache_attend_few<DIM, TYPE, false, NC, WHOLE>, dim3(runs), dim3(THREADS), a, stream);
+}
+
+template <int DIM, spmm_cache_type_t TYPE, int NC>
+static int launch_typed(const AttendArgs& a, void* stream)
+{
+    const int64_t keys = a.batch.ld_table << a.pool.page_shift, heads = (int64_t)a.batch.n_seqs * a.pool.n_heads;
+    if (keys <= SHORT) return launch_exact<DIM, TYPE, NC, true>(a, (int)heads, stream);
+    // no more runs than units, as far as the host can say
+    const int64_t most = heads * ((keys + UNIT<TYPE> - 1) / UNIT<TYPE>), full = CUS * PER_CU<DIM, NC>;
+    const int runs = (int)(most < full ? most : full);
+    if (const int rc = launch_exact<DIM, TYPE, NC, false>(a, runs, stream)) return rc;
+    void* args[] = {const_cast<AttendArgs*>(&a), const_cast<int*>(&runs)};
+    return (int)hipLaunchKernel((const void*)cache_join<DIM, NC>, dim3(4 * a.pool.n_heads, a.batch.n_seqs), dim3(THREADS), args, 0, (hipStream_t)stream);
+}
+
 template <int DIM, int NC>
 static int launch_dim(const AttendArgs& a, const spmm_cache_type_t type, void* stream)
 {
-    // no more runs than units, as far as the host can say
-    const int64_t unit = type == SPMM_CACHE_S8 ? UNIT<SPMM_CACHE_S8> : UNIT<SPMM_CACHE_BF16>;
-    const int64_t most = (int64_t)a.batch.n_seqs * a.pool.n_heads * (((a.batch.ld_table << a.pool.page_shift) + unit - 1) / unit);
-    constexpr int64_t full = CUS * PER_CU<DIM, NC>;
-    const int runs = (int)(most < full ? most : full);
-    const bool exact = a.pool.head_dim == DIM;
-    const dim3 grid(runs), block(THREADS);
-    const int rc = type == SPMM_CACHE_S8 ? (exact ? launch(cache_attend_few<DIM, SPMM_CACHE_S8, true, NC>, grid, block, a, stream)
-                                                  : launch(cache_attend_few<DIM, SPMM_CACHE_S8, false, NC>, grid, block, a, stream))
-                                         : (exact ? launch(cache_attend_few<DIM, SPMM_CACHE_BF16, true, NC>, grid, block, a, stream)
-                                                  : launch(cache_attend_few<DIM, SPMM_CACHE_BF16, false, NC>, grid, block, a, stream));
-    if (rc) return rc;
-    void* args[] = {const_cast<AttendArgs*>(&a), const_cast<int*>(&runs)};
-    return (int)hipLaunchKernel((const void*)cache_join<DIM, NC>, dim3(a.pool.n_heads, a.batch.n_seqs), block, args, 0, (hipStream_t)stream);
+    return type == SPMM_CACHE_S8 ? launch_typed<DIM, SPMM_CACHE_S8, NC>(a, stream) : launch_typed<DIM, SPMM_CACHE_BF16, NC>(a, stream);
 }
 
 int launch_attend_few(const AttendArgs& a, const spmm_cache_type_t type, void* stream)
