@@ -56,11 +56,32 @@ __device__ __forceinline__ Block block_of(const AttendArgs& a, const Sequence& s
     return k;
 }
 
-// the other half of the wave's value
+// the other half of the wave's value.  (The operands are told apart: of the swap of a value with itself, the compiler may take
+// one result for both.)
 __device__ __forceinline__ float other_half(const float v)
 {
-    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+    uint32_t same = __builtin_bit_cast(uint32_t, v);
+    asm volatile("" : "+v"(same));
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), same, false, false);
     return __builtin_bit_cast(float, threadIdx.x & 32 ? r[0] : r[1]);
+}
+
+// largest of a wave: within rows of 16 lanes, then of the rows
+template <int CONTROL>
+__device__ __forceinline__ float max_dpp(const float v)
+{
+    return fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CONTROL, 0xf, 0xf, false)));
+}
+__device__ __forceinline__ float wave_max(float v)
+{
+    v = max_dpp<0x121>(v);      // row_ror:1
+    v = max_dpp<0x122>(v);
+    v = max_dpp<0x124>(v);
+    v = max_dpp<0x128>(v);
+    float most = v;
+#pragma unroll
+    for (int row = 0; row < 64; row += 16) most = fmaxf(most, __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), row)));
+    return most;
 }
 
 // chunk of LDS, of 16 bytes, that chunk c of a row lies in: rows of 8 chunks (two rows cover the banks), or of 16
@@ -76,6 +97,18 @@ __device__ __forceinline__ void scale_in_place(float& o, const float by)
     float y = o;
     asm volatile("v_mul_f32 %0, %1, %0" : "+v"(y) : "v"(by));
     o = y;
+}
+
+// Eight codes times scales, in binary16, rounded once: (n + 128) s - 128 s is n s but for the last place of binary32.
+template <typename F>
+__device__ __forceinline__ f16x8 scaled(uint32_t a, uint32_t b, const F& by)
+{
+    a ^= 0x80808080u;
+    b ^= 0x80808080u;
+    f16x8 r;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r[j] = (_Float16)__fmaf_rn((float)((j < 4 ? a : b) >> 8 * (j % 4) & 0xff), by(j), -128.0f * by(j));
+    return r;
 }
 
 // A barrier for what is in LDS: stores to memory are not waited for.
@@ -209,23 +242,21 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void cache_attend_many(const Atten
             lane_v = a.pool.v_scale[(((int64_t)page_in_pool(lane_page_v, a.pool.n_pages) * H + h) << shift) + ((k0 + lane) & inside)];
         }
     };
-    float k_up = 1.0f, k_up_next = 1.0f, v_up = __builtin_bit_cast(float, 2u << 23), v_less = 1.0f;
+    // powers of two that are left out: of the keys widened last, and before them; of the values; what the sums have to be
+    // multiplied by before the values widened last are added, and before those widened before them are
+    float k_up = 1.0f, k_up_last = 1.0f, v_up = __builtin_bit_cast(float, 2u << 23), v_less_next = 1.0f, v_less = 1.0f;
     const auto widen_codes = [&](Half<DIM>& tk, Half<DIM>& tv, const int k0) INLINE {
         if constexpr (S8) {
             const bool k_here = k0 + TILE + lane >= seen_from && k0 + TILE + lane <= seen_to, v_here = k0 + lane >= seen_from && k0 + lane <= seen_to;
             if (!k_here) lane_k = 0.0f;     // (they may be anything)
             if (!v_here) lane_v = 0.0f;
-            float mk = fabsf(lane_k) <= 3.4e38f ? fabsf(lane_k) : 0.0f, mv = fabsf(lane_v) <= 3.4e38f ? fabsf(lane_v) : 0.0f;
-#pragma unroll
-            for (int i = 1; i < 64; i <<= 1) {
-                mk = fmaxf(mk, __shfl_xor(mk, i));
-                mv = fmaxf(mv, __shfl_xor(mv, i));
-            }
+            const float mk = wave_max(fabsf(lane_k) <= 3.4e38f ? fabsf(lane_k) : 0.0f), mv = wave_max(fabsf(lane_v) <= 3.4e38f ? fabsf(lane_v) : 0.0f);
+            k_up_last = k_up;
             float up;
-            const float k_down = to_unit(mk, &k_up_next);
+            const float k_down = to_unit(mk, &k_up);
             to_unit(mv, &up);
             up = fmaxf(up, v_up);
-            v_less = v_up / up;     // (for the sums, before they are added to)
+            v_less_next = v_up / up;
             v_up = up;
             const float v_down = __builtin_bit_cast(float, (254u << 23) - __builtin_bit_cast(uint32_t, up));
             __builtin_amdgcn_wave_barrier();
@@ -236,27 +267,16 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void cache_attend_many(const Atten
 #pragma unroll
             for (int i = 0; i < UNITS; ++i) {
                 const int u = unit_of(i), row = is_key(i) ? u / UPR : u / 4;
-                f16x8 x = widen(raw[i][0], raw[i][1]), y = widen(raw[i][2], raw[i][3]);
-                if (is_key(i)) {        // (rounded once, after the scale)
+                if (is_key(i)) {
                     const float by = scales[wave][0][row];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        x[j] = (_Float16)((float)x[j] * by);
-                        y[j] = (_Float16)((float)y[j] * by);
-                    }
                     const int c = u % UPR * 2;
-                    *(f16x8*)(tk.at + row * KC + turned<KC>(row, c)) = x;
-                    *(f16x8*)(tk.at + row * KC + turned<KC>(row, c + 1)) = y;
+                    *(f16x8*)(tk.at + row * KC + turned<KC>(row, c)) = scaled(raw[i][0], raw[i][1], [&](int) { return by; });
+                    *(f16x8*)(tk.at + row * KC + turned<KC>(row, c + 1)) = scaled(raw[i][2], raw[i][3], [&](int) { return by; });
                 } else {
                     const float* const by = scales[wave][1] + u % 4 * 16;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        x[j] = (_Float16)((float)x[j] * by[j]);
-                        y[j] = (_Float16)((float)y[j] * by[8 + j]);
-                    }
                     const int c = u % 4 * 2;
-                    *(f16x8*)(tv.at + row * 8 + turned<8>(row, c)) = x;
-                    *(f16x8*)(tv.at + row * 8 + turned<8>(row, c + 1)) = y;
+                    *(f16x8*)(tv.at + row * 8 + turned<8>(row, c)) = scaled(raw[i][0], raw[i][1], [&](const int j) { return by[j]; });
+                    *(f16x8*)(tv.at + row * 8 + turned<8>(row, c + 1)) = scaled(raw[i][2], raw[i][3], [&](const int j) { return by[8 + j]; });
                 }
             }
         }
@@ -428,9 +448,13 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void cache_attend_many(const Atten
     };
 
     if (n) {
-        if constexpr (S8) widen_codes(keys0, values1, first - TILE);
-        v_up = __builtin_bit_cast(float, 2u << 23);
-        v_less = 1.0f;
+        if constexpr (S8) {
+            widen_codes(keys0, values1, first - TILE);
+            v_up = __builtin_bit_cast(float, 2u << 23);
+            v_less_next = v_less = 1.0f;
+            fetch_codes(first);
+            name_codes(first + TILE);
+        }
         __syncthreads();
     }
     // Step t: waves ahead multiply values t - 1 and keys t, then weigh tile t; waves behind weigh tile t - 1, then multiply.
@@ -438,14 +462,17 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void cache_attend_many(const Atten
         constexpr bool ahead = decltype(is_ahead)::value;
         const int k0 = first + t * TILE;
         const bool more = t < n, more_k = t + 1 < n;
-        if constexpr (S8) {
-            if (more) {
-                fetch_codes(k0);
-                name_codes(k0 + TILE);
+        if constexpr (!S8) aim(k0);
+        // 8 bits: the codes of this step are in registers; those of the next are asked for as soon as they are not
+        const auto widen_now = [&]() INLINE {
+            if (S8 && more) {
+                widen_codes(k_next, v_now, k0);
+                if (more_k) {
+                    fetch_codes(k0 + TILE);
+                    name_codes(k0 + 2 * TILE);
+                }
             }
-        } else {
-            aim(k0);
-        }
+        };
         // a quarter of the wave's loads to LDS
         const auto fetch = [&](const int part) INLINE {
             if constexpr (!S8) {
@@ -463,8 +490,6 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void cache_attend_many(const Atten
         };
         const auto nothing = [](const int) INLINE {};
         __builtin_amdgcn_sched_barrier(0);
-        const float k_up_last = k_up;
-        k_up = k_up_next;       // of the keys that this step multiplies
         const auto products = [&](auto&& between) INLINE {
             if constexpr (S8) {
                 if (v_less != 1.0f) {
@@ -486,17 +511,25 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void cache_attend_many(const Atten
             products([&](const int i) INLINE {
                 if (i % DT == DT - 1) fetch(i / DT);
             });
-        } else if (t > 0) {
-            weigh(k0 - TILE, k_up_last, fetch);
         } else {
+            if (t > 0) {
+                weigh(k0 - TILE, k_up_last, fetch);
+            } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) fetch(i);
+                for (int i = 0; i < 4; ++i) fetch(i);
+            }
+            widen_now();        // (beside the other waves' products)
         }
         if (GROUPS > 1) asm volatile("s_barrier" ::: "memory");
-        if constexpr (!ahead) products(nothing);
-        else if (more) weigh(k0, k_up, nothing);
-        if (more) widen_codes(k_next, v_now, k0);
-        __syncthreads();
+        if constexpr (!ahead) {
+            products(nothing);
+        } else {
+            if (more) weigh(k0, k_up, nothing);
+            widen_now();
+        }
+        v_less = v_less_next;
+        if constexpr (S8) lds_barrier();
+        else __syncthreads();       // (loads to LDS are waited for as memory is)
         if (more && (k0 < all_from || k0 + TILE - 1 > all_to)) {
             clean(v_now, k0);
             __syncthreads();
