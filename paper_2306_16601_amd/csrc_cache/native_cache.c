@@ -38,10 +38,19 @@ static void record_free(PyObject *self)
     Py_XDECREF(((Record *)self)->keep);
     PyObject_Free(self);
 }
+/* the tensors, as cache_binding.py keeps them: of a call to append (q_weight, k_weight, rope, positions) */
+static PyObject *record_keep(PyObject *self, void *unused)
+{
+    const Record *const r = (Record *)self;
+    (void)unused;
+    if (r->kind != APPEND) return Py_NewRef(r->keep);
+    return PyTuple_Pack(4, PyTuple_GET_ITEM(r->keep, 4), PyTuple_GET_ITEM(r->keep, 5), PyTuple_GET_ITEM(r->keep, 7), Py_None);
+}
+static PyGetSetDef record_attributes[] = {{"_keepalive", record_keep, NULL, NULL, NULL}, {NULL, NULL, NULL, NULL, NULL}};
 static PyBufferProcs record_as_buffer = {record_buffer, NULL};
 static PyTypeObject RecordType = {
     PyVarObject_HEAD_INIT(NULL, 0).tp_name = "spmm_cache_record", .tp_basicsize = sizeof(Record), .tp_dealloc = record_free,
-    .tp_as_buffer = &record_as_buffer, .tp_flags = Py_TPFLAGS_DEFAULT,
+    .tp_as_buffer = &record_as_buffer, .tp_getset = record_attributes, .tp_flags = Py_TPFLAGS_DEFAULT,
     .tp_doc = "A cache, a batch or a call of include/spmm_cache.h, described"};
 
 enum { F_APPEND, F_ATTEND, F_ATTEND_WORK, F_FORK, F_COMPACT, F_CACHE_WORK, FUNCTIONS };
