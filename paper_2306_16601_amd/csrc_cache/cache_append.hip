@@ -7,9 +7,11 @@
 // cache_append_rows (heads of 64 or 128 dims, rotated in all of them or in none): a lane has a token, as x has its tokens
 // contiguous, and a wave two sets of consecutive dims that lie half a head apart, so that either form of rotation pairs values
 // of one lane; only the sum of the squares, and the largest value for 8 bits, go through LDS.  All loads of a head are under way
-// at once (32 a lane).  q and k take 16 or 32 bytes of each token at a time.
+// at once (32 a lane).  q and k take 16 or 32 bytes of each token at a time.  Prompts of up to 1100 tokens, 3712 in all, 32 heads on
+// 8 of 128: 36 us, 3.8 TB/s (43 us with inputs that come from HBM); 8 single tokens, 12 heads of 64: 4.2 us.
 // cache_append (any other head): a workgroup turns a tile of TOKENS tokens x one head over in LDS (binary32, 17 KB at 128
-// dims); 16 lanes a token of 8 dims each then work on it, whose sums stay inside a row of 16 lanes.
+// dims); 16 lanes a token of 8 dims each then work on it, whose sums stay inside a row of 16 lanes.  It took 90 us for the same
+// prompts: two reads of LDS for each value are what the other form saves.
 #include "cache_internal.h"
 
 namespace spmm_cache {

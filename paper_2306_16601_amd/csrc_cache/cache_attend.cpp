@@ -4,6 +4,8 @@
 namespace spmm_cache {
 
 // Columns of a key/value head (query heads that share it times new tokens) up to which the cache is read straight to registers.
+// At 32 columns, 8 heads of 128 dims, that way against tiles in LDS: one sequence of 2000 keys 16.5 / 31.2 us, 8 of 30000 179 /
+// 194, in 8 bits 121 / 220, 32 of 500 18.1 / 27.2; its registers hold no more columns.
 constexpr int64_t FEW = 32;
 
 int64_t attend_work_bytes(spmm_cache_type_t type, int64_t n_seqs, int32_t n_heads, int32_t group, int32_t head_dim, int64_t max_new)

@@ -5,7 +5,9 @@
 // workgroup first sums up the sequences' units to find its run (lengths are known on the device only).  Its four waves take
 // the keys of a unit in turn; a wave loads operands straight from the pages to registers, 16 bytes a lane, the next step's
 // keys and page numbers while it works on this one's: 64 KB on the way for each workgroup.  Where a run covers a whole head
-// the result is written; parts of a head go to scratch and are joined by cache_join, in the order of the keys.
+// the result is written; parts of a head go to scratch and are joined by cache_join, in the order of the keys.  64 tokens on
+// contexts of up to 8191, 32 heads on 8 of 128: 222 us, 5.3 TB/s; with a workgroup for each head 574 us, as long as the longest
+// takes.  4 x 3 tokens on 131 thousand keys in 8 bits: 213 us and 8 to join.
 #include "cache_attend.h"
 
 #include <cfloat>
@@ -19,8 +21,11 @@ constexpr int COLS = 16;            // columns of a tile
 template <int DIM, int NC>
 constexpr int PER_CU = DIM > 64 && NC > 1 ? 1 : 2;
 constexpr int CUS = 256;
-// keys up to which a workgroup takes a whole head: nothing to join
-constexpr int64_t SHORT = 1024;
+// Keys, and bytes of a head's keys, up to which a workgroup takes the whole head and nothing is joined.  Whole against runs and join,
+// one token, one sequence: 8 heads of 128 dims in bfloat16 512 keys 11.2 / 11.6 us, 1024 keys 18.2 / 12.0; in 8 bits 1024 keys
+// 13.2 / 13.9, 2048 keys 20.5 / 14.3; 16 heads of 64 in bfloat16 1024 keys 8.1 / 10.3, 2048 keys 12.4 / 11.5, in 8 bits 8.7 / 10.8
+// and 13.4 / 11.4; 64 sequences of 512 keys 23.9 / 29.3.
+constexpr int64_t SHORT_KEYS = 1024, SHORT_BYTES = 128 << 10;
 
 template <spmm_cache_type_t TYPE>
 constexpr int KEYS = TYPE == SPMM_CACHE_S8 ? 64 : 32;       // of a wave's step
@@ -580,7 +585,7 @@ template <int DIM, spmm_cache_type_t TYPE, int NC>
 static int launch_typed(const AttendArgs& a, void* stream)
 {
     const int64_t keys = a.batch.ld_table << a.pool.page_shift, heads = (int64_t)a.batch.n_seqs * a.pool.n_heads;
-    if (keys <= SHORT) return launch_exact<DIM, TYPE, NC, true>(a, (int)heads, stream);
+    if (keys <= SHORT_KEYS && keys * DIM * Loads<DIM, TYPE>::BYTES <= SHORT_BYTES) return launch_exact<DIM, TYPE, NC, true>(a, (int)heads, stream);
     // no more runs than units, as far as the host can say
     const int64_t most = heads * ((keys + UNIT<TYPE> - 1) / UNIT<TYPE>), full = CUS * PER_CU<DIM, NC>;
     const int runs = (int)(most < full ? most : full);

