@@ -1,6 +1,15 @@
 """The paged cache's operators from their definition, token by token, in 64 bits on the host (test infrastructure)."""
+import functools
+
 import numpy as np
 import torch
+
+
+@functools.lru_cache(None)
+def side_stream():
+    """One stream for all these tests: streams share a few hardware queues in the order of their first use, and a test of the same
+    process that looks at whether work on a stream of its own holds up the default one depends on how many came before."""
+    return torch.cuda.Stream()
 
 
 class Problem:

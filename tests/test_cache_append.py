@@ -8,7 +8,7 @@ import pytest
 import torch
 
 import paper_2306_16601_amd as sp
-from cache_reference import Problem
+from cache_reference import Problem, side_stream
 
 pytestmark = pytest.mark.gpu
 
@@ -174,4 +174,4 @@ def test_zeros_have_a_scale_of_zero():
 
 def test_second_layer_other_stream():
     p = Problem([9, 2], [50, 9], 4, 2, 64, 32, layers=3, layer=1, seed=32)
-    run(p, stream=torch.cuda.Stream().cuda_stream)
+    run(p, stream=side_stream().cuda_stream)

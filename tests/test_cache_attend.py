@@ -8,7 +8,7 @@ import pytest
 import torch
 
 import paper_2306_16601_amd as sp
-from cache_reference import Problem
+from cache_reference import Problem, side_stream
 
 pytestmark = pytest.mark.gpu
 
@@ -184,7 +184,7 @@ def test_results_do_not_depend_on_the_run(news):
 def test_on_another_stream_and_in_a_graph(news):
     p = Problem(news, [700] * len(news), 4, 1, 128, 16, seed=18)
     first = attend(p)
-    side = torch.cuda.Stream()
+    side = side_stream()
     assert torch.equal(attend(p, stream=side.cuda_stream), first)
 
     cache, batch = p.on_device()
@@ -194,7 +194,7 @@ def test_on_another_stream_and_in_a_graph(news):
     q = p.q.cuda()
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
-    with torch.cuda.graph(graph):
+    with torch.cuda.graph(graph, stream=side):
         sp.spmm_cache_attend(cache, 0, batch, q, p.tokens, how, out, p.tokens, work, torch.cuda.current_stream().cuda_stream)
     for _ in range(3):
         out.fill_(5.0)

@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import paper_2306_16601_amd as sp
+from cache_reference import side_stream
 
 pytestmark = pytest.mark.gpu
 
@@ -203,7 +204,7 @@ def test_copy(heads, page, dim, kind):
     for x in ref:
         for a, b in zip(src[:4], dst[:4]):
             x[:, b] = x[:, a]
-    side = torch.cuda.Stream()
+    side = side_stream()
     a, b = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in (src, dst))
     torch.cuda.synchronize()
     sp.spmm_cache_copy(cache, a, b, 6, side.cuda_stream)
