@@ -51,8 +51,6 @@ __device__ __forceinline__ Sequence sequence(const AttendArgs& a, const int b)
     return s;
 }
 
-__device__ __forceinline__ bool not_finite(const __bf16 v) { return !(fabsf((float)v) <= 3.4e38f); }
-
 __device__ __forceinline__ u32x4 finite_or_zero(u32x4 v)
 {
 #pragma unroll

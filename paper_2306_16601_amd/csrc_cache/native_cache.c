@@ -191,16 +191,6 @@ static Record *record(int kind, PyObject *const *args, Py_ssize_t nargs)
     return r;
 }
 
-static int64_t bytes_of(const int64_t *shape, int dims, int64_t each)
-{
-    __int128 n = each;
-    for (int i = 0; i < dims; ++i) {
-        n *= shape[i];
-        if (n > INT64_MAX) return INT64_MAX;
-    }
-    return (int64_t)n;
-}
-
 static PyObject *make_cache(PyObject *self, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
 {
     int64_t ks[5], vs[5], ss[4];
