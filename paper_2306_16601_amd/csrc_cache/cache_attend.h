@@ -29,23 +29,23 @@ constexpr float NONE = -__builtin_inff();       // score of what is not seen
 struct Sequence {
     int first, tokens;      // first column of the batch, number of columns that are computed
     int past, len;          // position of the first new token (it may be negative); tokens in the cache
-    __device__ __forceinline__ int last_seen(const AttendArgs& a, const int token) const
+    __host__ __device__ __forceinline__ int last_seen(const AttendArgs& a, const int token) const
     {
         const int at = past + token;
         return at < 0 ? -1 : a.causal ? min(at, len - 1) : len - 1;
     }
-    __device__ __forceinline__ int first_seen(const AttendArgs& a, const int token) const
+    __host__ __device__ __forceinline__ int first_seen(const AttendArgs& a, const int token) const
     {
         return a.window ? max(past + token - a.window + 1, 0) : 0;
     }
 };
 
-__device__ __forceinline__ Sequence sequence(const AttendArgs& a, const int b)
+__host__ __device__ __forceinline__ Sequence sequence(const AttendArgs& a, const int b)
 {
     Sequence s;
     s.first = a.batch.q_start[b];
     const int end = a.batch.q_start[b + 1];
-    s.tokens = s.first < 0 ? 0 : max(min(min(end, a.T) - s.first, a.max_new), 0);
+    s.tokens = s.first < 0 || end <= s.first ? 0 : max(min(min(end, a.T) - s.first, a.max_new), 0);     // (no difference overflows)
     s.len = tokens_of(a.batch, b, a.pool.page_shift);
     s.past = a.batch.kv_len[b] - (end - s.first);
     return s;

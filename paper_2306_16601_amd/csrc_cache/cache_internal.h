@@ -118,7 +118,7 @@ __device__ __forceinline__ int sequence_of(const Batch& s, const int t)
 }
 
 // Tokens of a sequence that its table can name (a table's row names less than 2^30: cache_api.cpp).
-__device__ __forceinline__ int tokens_of(const Batch& s, const int b, const int page_shift)
+__host__ __device__ __forceinline__ int tokens_of(const Batch& s, const int b, const int page_shift)
 {
     const int64_t most = s.ld_table << page_shift;
     const int n = s.kv_len[b];
