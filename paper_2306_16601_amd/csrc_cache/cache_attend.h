@@ -28,7 +28,7 @@ constexpr float NONE = -__builtin_inff();       // score of what is not seen
 // A sequence's new tokens, and what they see.
 struct Sequence {
     int first, tokens;      // first column of the batch, number of columns that are computed
-    int past, len;          // position of the first new token (it may be negative); tokens in the cache
+    int past, len;          // position of the first new token (it may be negative, from -2^30 on); tokens in the cache
     __host__ __device__ __forceinline__ int last_seen(const AttendArgs& a, const int token) const
     {
         const int at = past + token;
@@ -36,7 +36,8 @@ struct Sequence {
     }
     __host__ __device__ __forceinline__ int first_seen(const AttendArgs& a, const int token) const
     {
-        return a.window ? max(past + token - a.window + 1, 0) : 0;
+        // 0 .. len: a window may be as wide as an int, and positions may lie far beyond the table's width
+        return a.window ? min(max((int)((uint32_t)past + token + 1), a.window) - a.window, len) : 0;
     }
 };
 
@@ -47,7 +48,7 @@ __host__ __device__ __forceinline__ Sequence sequence(const AttendArgs& a, const
     const int end = a.batch.q_start[b + 1];
     s.tokens = s.first < 0 || end <= s.first ? 0 : max(min(min(end, a.T) - s.first, a.max_new), 0);     // (no difference overflows)
     s.len = tokens_of(a.batch, b, a.pool.page_shift);
-    s.past = a.batch.kv_len[b] - (end - s.first);
+    s.past = (int)max((int64_t)a.batch.kv_len[b] - ((int64_t)end - s.first), (int64_t)-(1 << 30));     // (there are at most 2^27 columns)
     return s;
 }
 

@@ -62,3 +62,30 @@ def test_columns_lie_in_the_operands(ask):
         start, end, T, most = c[0], c[1], c[5], c[6]
         assert max(tokens, 0) == columns(start, end, T, most), c
         assert tokens <= 0 or (0 <= first and first + tokens <= T), c
+
+
+def seen(start, end, kv_len, width, shift, causal, window, token):
+    """(first, last) key that a column sees."""
+    n = max(0, min(kv_len, width << shift))
+    at = kv_len - (end - start) + token
+    if at < 0:
+        return 0, -1
+    return min(max(0, at - window + 1), n) if window else 0, min(at, n - 1) if causal else n - 1
+
+
+def test_positions_and_windows_of_any_size(ask):
+    r = random.Random(2)
+    windows, lengths = (0, 1, 9, 1 << 30, HIGHEST - 1, HIGHEST), (LOWEST, LOWEST + 3, -7, 0, 2, 40, 64, 1000, 1 << 30, HIGHEST - 2, HIGHEST)
+    cases = [(start, start + new, n, width, shift, 100, 100, causal, w, t) for start in (0, 3) for new in (1, 7, 60) for n in lengths
+             for width, shift in ((1, 4), (4, 6), ((1 << 26) - 1, 4)) for causal in (0, 1) for w in windows for t in (0, new - 1)]
+    cases += [(0, HIGHEST, n, 4, 6, 100, 100, 1, w, t) for n in lengths for w in windows for t in (0, 50)]
+    for _ in range(4000):
+        start, new, shift = r.randint(0, 50), r.randint(1, 50), r.randint(4, 8)
+        cases.append((start, start + new, r.choice((r.randint(LOWEST, HIGHEST), r.randint(-100, 2000))), r.randint(1, (1 << 30 >> shift) - 1), shift, 100, 100,
+                      r.randint(0, 1), r.choice((0, r.randint(1, HIGHEST), r.randint(1, 2000))), r.randint(0, new - 1)))
+    for c, (first, tokens, length, last, begin) in zip(cases, ask(cases)):
+        start, end, n, width, shift, _, _, causal, window, token = c
+        assert tokens > token and length == max(0, min(n, width << shift)), c
+        want = seen(start, end, n, width, shift, causal, window, token)
+        assert -1 <= last < max(length, 1) and 0 <= begin <= length, (c, begin, last)
+        assert ((begin, last) == want) if want[0] <= want[1] else begin > last, (c, begin, last, want)
