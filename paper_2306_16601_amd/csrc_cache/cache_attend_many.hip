@@ -25,6 +25,7 @@
 // 8 bits: 236 instead of 685 us).
 #include "cache_attend.h"
 
+#include <cfloat>
 #include <type_traits>
 
 #define INLINE __attribute__((always_inline))
@@ -404,7 +405,8 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void cache_attend_many(const Atten
 
     // ---- softmax of a tile's scores ----
     const auto weigh = [&](const int k0, const float keys_up, auto&& between) INLINE {
-        const float by = S8 ? unit * keys_up : unit;
+        // (never 0, which what is hidden, -inf, must not be multiplied by: scores are below 2^19, and with less than that 0)
+        const float by = S8 ? fmaxf(unit * keys_up, FLT_MIN) : unit;
         if (k0 < all_from || k0 + TILE - 1 > all_to) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) {
