@@ -196,7 +196,7 @@ __global__ __launch_bounds__(THREADS, (PER_CU<DIM, NC>)) void cache_attend_few(c
                 most = fmaxf(most, __shfl_xor(most, 32));
                 float up;
                 const float down = to_unit(most, &up);
-                unit[c] *= up;
+                unit[c] = fmaxf(unit[c] * up, FLT_TRUE_MIN);        // (never 0, which what is hidden, -inf, must not be multiplied by)
 #pragma unroll
                 for (int i8 = 0; i8 < KS * 2; ++i8) {
                     const bf16x8 v = __builtin_bit_cast(bf16x8, raw[i8]);

@@ -49,3 +49,18 @@ def test_zero_columns_before_their_sequence_give_zeros(new):
     p.k_scale = torch.where(p.k_scale.isnan(), p.k_scale, torch.zeros_like(p.k_scale))
     check(p)
     check(p, causal=False)
+
+
+@pytest.mark.parametrize("cache", CACHES)
+@pytest.mark.parametrize("new", [1, 40, 300])
+@pytest.mark.parametrize("scale", [1e-9, 1e-30, 1e-45])
+def test_small_scales(scale, new, cache):
+    """Scores too small to tell from zero: with zero queries, and with some, all visible tokens weigh the same."""
+    for zero in (True, False):
+        p = Problem([new, 3], [77, 20], 4, 2, 64, 32, cache, seed=44)
+        if zero:
+            p.q.zero_()
+        p.q[::2] *= 1e-30
+        got = attend(p, scale=scale).double().numpy()
+        ref, mag = p.attention(scale)
+        assert (np.abs(got - ref) <= (2.0 ** -8 + 1e-4) * mag).all()
