@@ -67,7 +67,8 @@ typedef struct {
  *   first rope_dim dims; pair i is (y[i], y[i + rope_dim / 2]), or (y[2 i], y[2 i + 1]) where interleaved.
  * Positions outside the rotation table give NaN.  Values are not normalised or rotated.  All of it is
  * computed in binary32 and rounded once: queries to bfloat16, keys and values to the cache's type.
- * S8: scale = amax / 127 over the head's dims of a token, code = rint(value * (127 / amax)). */
+ * S8: scale = amax / 127 over the head's dims of a token, code = rint(value * (127 / amax)).  Where these are not all
+ * finite, the scale is not either and all codes are 0, so that the token's head is NaN as a whole. */
 typedef struct {
     int32_t q_heads;            /* multiple of the cache's n_heads                               */
     spmm_out_t x_type;          /* F32, S8 or U8                                                 */

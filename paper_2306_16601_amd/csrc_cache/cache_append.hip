@@ -35,6 +35,16 @@ __device__ __forceinline__ float value_of(const AppendArgs& a, const X x)
     else return (float)((int)x - a.x_zero_point) * a.x_scale;
 }
 
+// the larger of two magnitudes: NaN where one of them is
+__device__ __forceinline__ float larger(const float a, const float b) { return __builtin_elementwise_maximum(a, b); }
+
+// The code of a value of a token's head; 0 where the head's values are not all finite, and so the scale is not (code times scale is NaN).
+__device__ __forceinline__ int8_t code_of(const float y, const float inv)
+{
+    const float c = rintf(y * inv);
+    return (int8_t)(fabsf(c) <= 127.0f ? c : 0.0f);
+}
+
 // largest and sum over the 16 lanes of a row
 __device__ __forceinline__ float row_sum(float v)
 {
@@ -43,7 +53,7 @@ __device__ __forceinline__ float row_sum(float v)
 }
 __device__ __forceinline__ float row_max(float v)
 {
-    for (int i = 1; i < 16; i <<= 1) v = fmaxf(v, __shfl_xor(v, i));
+    for (int i = 1; i < 16; i <<= 1) v = larger(v, __shfl_xor(v, i));
     return v;
 }
 
@@ -132,12 +142,12 @@ __global__ __launch_bounds__(THREADS) void cache_append(const AppendArgs a)
                 if constexpr (TYPE == SPMM_CACHE_S8) {
                     float most = 0.0f;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(y[j]));
+                    for (int j = 0; j < 8; ++j) most = larger(most, fabsf(y[j]));
                     most = row_max(most);
                     const float inv = most > 0.0f ? 127.0f / most : 0.0f;
                     uint32_t o[2] = {0, 0};
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) o[j / 4] |= (uint32_t)(uint8_t)(int8_t)rintf(y[j] * inv) << 8 * (j % 4);
+                    for (int j = 0; j < 8; ++j) o[j / 4] |= (uint32_t)(uint8_t)code_of(y[j], inv) << 8 * (j % 4);
                     if (p.page >= 0) {
                         if (mine) *(u32x2*)((int8_t*)a.pool.k + slot * D + d0) = u32x2{o[0], o[1]};
                         if (c == 0) a.pool.k_scale[slot] = most / 127.0f;
@@ -157,7 +167,7 @@ __global__ __launch_bounds__(THREADS) void cache_append(const AppendArgs a)
     if constexpr (TYPE == SPMM_CACHE_S8) {
         for (int t = tid / 16; t < TOKENS; t += THREADS / 16) {
             float most = 0.0f;
-            for (int d = tid % 16; d < D; d += 16) most = fmaxf(most, fabsf(tile[d * PITCH + t]));
+            for (int d = tid % 16; d < D; d += 16) most = larger(most, fabsf(tile[d * PITCH + t]));
             most = row_max(most);
             if (tid % 16 == 0) {
                 const Place p = places[t];
@@ -173,7 +183,7 @@ __global__ __launch_bounds__(THREADS) void cache_append(const AppendArgs a)
         if (p.page < 0) continue;
         const int64_t at = (((p.page * kv_heads + kv) * D + d) << shift) + p.offset;
         const float y = tile[d * PITCH + t];
-        if constexpr (TYPE == SPMM_CACHE_S8) ((int8_t*)a.pool.v)[at] = (int8_t)rintf(y * inverse[t]);
+        if constexpr (TYPE == SPMM_CACHE_S8) ((int8_t*)a.pool.v)[at] = code_of(y, inverse[t]);
         else ((__bf16*)a.pool.v)[at] = (__bf16)y;
     }
 }
@@ -190,7 +200,7 @@ __device__ __forceinline__ void store_key(const AppendArgs& a, const int64_t at,
     if constexpr (TYPE == SPMM_CACHE_S8) {
         uint32_t o[N / 4] = {};
 #pragma unroll
-        for (int i = 0; i < N; ++i) o[i / 4] |= (uint32_t)(uint8_t)(int8_t)rintf(y[i] * inv) << 8 * (i % 4);
+        for (int i = 0; i < N; ++i) o[i / 4] |= (uint32_t)(uint8_t)code_of(y[i], inv) << 8 * (i % 4);
         if constexpr (N == 16) *(u32x4*)((int8_t*)a.pool.k + at) = u32x4{o[0], o[1], o[2], o[3]};
         else *(u32x2*)((int8_t*)a.pool.k + at) = u32x2{o[0], o[1]};
     } else {
@@ -338,12 +348,12 @@ __global__ __launch_bounds__(THREADS) void cache_append_rows(const AppendArgs a)
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
-            for (int i = 0; i < N; ++i) most = fmaxf(most, fabsf(y[s][i]));
+            for (int i = 0; i < N; ++i) most = larger(most, fabsf(y[s][i]));
         __syncthreads();        // (the sums have been read)
         part[wave][lane] = most;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) most = fmaxf(most, part[w][lane]);
+        for (int w = 0; w < WAVES; ++w) most = larger(most, part[w][lane]);
         inv = most > 0.0f ? 127.0f / most : 0.0f;
         if (wave == 0 && p.page >= 0) (turned ? a.pool.k_scale : a.pool.v_scale)[((p.page * kv_heads + kv) << shift) + p.offset] = most / 127.0f;
     }
@@ -360,7 +370,7 @@ __global__ __launch_bounds__(THREADS) void cache_append_rows(const AppendArgs a)
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int64_t to = at + ((int64_t)(DIM / 2 * s + i) << shift);
-            if constexpr (TYPE == SPMM_CACHE_S8) ((int8_t*)a.pool.v)[to] = (int8_t)rintf(y[s][i] * inv);
+            if constexpr (TYPE == SPMM_CACHE_S8) ((int8_t*)a.pool.v)[to] = code_of(y[s][i], inv);
             else ((__bf16*)a.pool.v)[to] = (__bf16)y[s][i];
         }
 }
