@@ -38,6 +38,15 @@ __device__ __forceinline__ float value_of(const AppendArgs& a, const X x)
 // the larger of two magnitudes: NaN where one of them is
 __device__ __forceinline__ float larger(const float a, const float b) { return __builtin_elementwise_maximum(a, b); }
 
+// Values whose largest is below TINY are brought up by UP first: 127 over the largest would overflow.
+constexpr float TINY = 0x1p-120f, UP = 0x1p100f;
+
+// What a token's head's values become codes by.
+__device__ __forceinline__ float codes_by(const float most)
+{
+    return most > 0.0f ? 127.0f / (most < TINY ? most * UP : most) : 0.0f;
+}
+
 // The code of a value of a token's head; 0 where the head's values are not all finite, and so the scale is not (code times scale is NaN).
 __device__ __forceinline__ int8_t code_of(const float y, const float inv)
 {
@@ -62,7 +71,7 @@ __global__ __launch_bounds__(THREADS) void cache_append(const AppendArgs a)
 {
     __shared__ float tile[HEAD_DIM_MAX * PITCH];
     __shared__ Place places[TOKENS];
-    __shared__ float inverse[TOKENS];       // 127 / amax, of values in 8 bits
+    __shared__ float inverse[TOKENS];       // of codes_by, for values in 8 bits
 
     const int D = a.pool.head_dim, t0 = blockIdx.x * TOKENS, head = blockIdx.y, tid = threadIdx.x;
     const X* const x = (const X*)a.x + (int64_t)head * D * a.ldx;
@@ -144,7 +153,11 @@ __global__ __launch_bounds__(THREADS) void cache_append(const AppendArgs a)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) most = larger(most, fabsf(y[j]));
                     most = row_max(most);
-                    const float inv = most > 0.0f ? 127.0f / most : 0.0f;
+                    const float inv = codes_by(most);
+                    if (most < TINY) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) y[j] *= UP;
+                    }
                     uint32_t o[2] = {0, 0};
 #pragma unroll
                     for (int j = 0; j < 8; ++j) o[j / 4] |= (uint32_t)(uint8_t)code_of(y[j], inv) << 8 * (j % 4);
@@ -169,9 +182,12 @@ __global__ __launch_bounds__(THREADS) void cache_append(const AppendArgs a)
             float most = 0.0f;
             for (int d = tid % 16; d < D; d += 16) most = larger(most, fabsf(tile[d * PITCH + t]));
             most = row_max(most);
+            if (most < TINY) {
+                for (int d = tid % 16; d < D; d += 16) tile[d * PITCH + t] *= UP;
+            }
             if (tid % 16 == 0) {
                 const Place p = places[t];
-                inverse[t] = most > 0.0f ? 127.0f / most : 0.0f;
+                inverse[t] = codes_by(most);
                 if (p.page >= 0) a.pool.v_scale[((p.page * kv_heads + kv) << shift) + p.offset] = most / 127.0f;
             }
         }
@@ -354,7 +370,13 @@ __global__ __launch_bounds__(THREADS) void cache_append_rows(const AppendArgs a)
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) most = larger(most, part[w][lane]);
-        inv = most > 0.0f ? 127.0f / most : 0.0f;
+        inv = codes_by(most);
+        if (most < TINY) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int i = 0; i < N; ++i) y[s][i] *= UP;
+        }
         if (wave == 0 && p.page >= 0) (turned ? a.pool.k_scale : a.pool.v_scale)[((p.page * kv_heads + kv) << shift) + p.offset] = most / 127.0f;
     }
     if (p.page < 0) return;

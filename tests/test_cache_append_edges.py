@@ -67,3 +67,16 @@ def test_what_is_not_finite_is_not_lost_in_8_bits(norm, odd, dim):
         others = np.ones(scale.shape, bool)
         others[token, 0] = False
         assert (got[others] == ref[others]).all() and (scale[others] == ref_scale[others]).all()
+
+
+@pytest.mark.parametrize("dim", [64, 80, 128])
+@pytest.mark.parametrize("size", [1e-36, 2e-37, 1e-38, 1e-40, 1e-43])
+def test_tiny_values_have_codes_of_their_own(size, dim):
+    """Off by half a step of the scale, and by what binary32 holds of the scale itself (steps of 1.4e-45, for codes up to 127)."""
+    x = (random(dim) * np.float32(size)).astype(np.float32)
+    _, k, v, ks, vs = append(x, dim)
+    for got, scale, ref in ((k, ks, heads(x, dim)[0]), (v, vs, heads(x, dim)[1])):
+        ref = ref.astype(np.float64)
+        scale = scale.astype(np.float64)[..., None]
+        assert (np.abs(got * scale - ref) <= 0.501 * scale + 128 * 1.41e-45).all()
+        assert (np.abs(got).max(-1) <= 127).all()
