@@ -64,3 +64,94 @@ def test_small_scales(scale, new, cache):
         got = attend(p, scale=scale).double().numpy()
         ref, mag = p.attention(scale)
         assert (np.abs(got - ref) <= (2.0 ** -8 + 1e-4) * mag).all()
+
+
+def by_kind(p, causal=True, window=0):
+    """(result, sum of p |v|) as Problem.attention has them, for values that are not finite too: a sequence and a head at a time, their
+    sums and NaN, +inf and -inf apart from each other."""
+    out = np.full((p.q_heads, p.dim, p.tokens), np.nan)
+    mag = out.copy()
+    keys, values = p.k.double().numpy(), p.v.double().transpose(3, 4).numpy()
+    for b, n in enumerate(p.news):
+        at = p.lens[b] - n + np.arange(n)[:, None]
+        for h in range(p.q_heads if n else 0):
+            k, v = p._rows(b, h // p.group, keys, p.k_scale), p._rows(b, h // p.group, values, p.v_scale)
+            j = np.arange(len(k))
+            sees = np.broadcast_to(at >= 0, (n, len(k)))
+            if causal:
+                sees = sees & (j <= at)
+            if window:
+                sees = sees & (j > at - window)
+            t = slice(p.start[b], p.start[b] + n)
+            s = np.where(sees, p.q[t, h].double().numpy() @ k.T * p.dim ** -0.5, -np.inf)
+            lost = (sees & ~(s < np.inf)).any(1) | (sees.any(1) & (s == -np.inf).all(1))       # (NaN, or nothing but -inf, among the scores)
+            w = np.exp(s - np.where(np.isfinite(s), s, -1e300).max(1, keepdims=True))
+            w /= np.maximum(w.sum(1, keepdims=True), 1e-300)
+            w[lost] = 0
+            plus, minus, nan = (sees.astype(float) @ kind(v) > 0 for kind in (np.isposinf, np.isneginf, np.isnan))
+            finite = np.where(np.isfinite(v), v, 0)
+            y = w @ finite
+            y[plus], y[minus], y[nan | (plus & minus) | lost[:, None]] = np.inf, -np.inf, np.nan
+            out[h, :, t], mag[h, :, t] = y.T, (w @ np.abs(finite)).T
+    return out.reshape(-1, p.tokens), mag.reshape(-1, p.tokens)
+
+
+def as_defined(p, got, causal=True, window=0):
+    """Results that are not finite are NaN or infinities as the definition has them; the others are near it."""
+    with np.errstate(invalid="ignore", over="ignore"):
+        ref, mag = by_kind(p, causal, window)
+    got = got.double().numpy()
+    for kind in (np.isnan, np.isposinf, np.isneginf):
+        bad = kind(got) != kind(ref)
+        assert not bad.any(), (kind.__name__, int(bad.sum()), np.argwhere(bad)[:5], got[bad][:5], ref[bad][:5])
+    fine = np.isfinite(ref)
+    assert (np.abs(got[fine] - ref[fine]) <= (2.0 ** -8 + 1e-4) * mag[fine]).all()
+    return ref
+
+
+def test_the_definition_by_kind_is_the_definition():
+    p = Problem([8, 1, 20], [150, 40, 3], 4, 2, 64, 16, seed=60)
+    p.lens[2] = 9
+    for causal, window in ((True, 0), (False, 0), (True, 30), (False, 5)):
+        for x, y in zip(by_kind(p, causal, window), p.attention(p.dim ** -0.5, causal, window)):
+            assert np.allclose(x, y, rtol=1e-12, atol=1e-12)
+
+
+# new tokens and past of each sequence, table's width in pages of 16: heads that one workgroup takes, and runs that are joined; blocks
+# of 128 columns in parts, and whole; the same of 256 columns (8 bits)
+FORMS = {"whole": ([8, 1, 5], [150, 40, 0], None), "runs": ([8, 1, 5], [150, 40, 700], 90), "parts": ([70, 3, 260], [150, 40, 9], None),
+         "blocks": ([34] * 150, [70] * 150, None), "wide parts": ([70, 3, 250], [150, 40, 9], None), "wide blocks": ([120] * 70, [70] * 70, None)}
+
+
+def problem(form, cache, seed, dim=64):
+    news, pasts, width = FORMS[form]
+    p = Problem(news, pasts, 4, 2, dim, 16, cache, seed=seed, width=width)
+    p.q = (p.q.float() * 0.3).to(torch.bfloat16)        # (weights that neither type of the products' operands loses)
+    return p
+
+
+def plant(p, what, b, at, value, dim=5):
+    """A value of sequence b's token `at`, in one dim of its first head (of 8 bits: in the head's scale)."""
+    page, off = int(p.table[b, at // 16]), at % 16
+    if p.kind == "s8":
+        (p.k_scale if what == "k" else p.v_scale)[0, page, 0, off] = value
+    elif what == "k":
+        p.k[0, page, 0, off, dim] = value
+    else:
+        p.v[0, page, 0, dim, off] = value
+
+
+INF, NAN = float("inf"), float("nan")
+
+
+@pytest.mark.parametrize("cache", CACHES)
+@pytest.mark.parametrize("form", list(FORMS))
+@pytest.mark.parametrize("causal, window", [(True, 0), (False, 0), (True, 30)])
+@pytest.mark.parametrize("odd", [NAN, INF, -INF])
+def test_values_that_are_not_finite(odd, causal, window, form, cache):
+    """In tokens that all of a sequence's new ones see, and in tokens that some see."""
+    p = problem(form, cache, 61)
+    for b in range(len(p.news)):
+        plant(p, "v", b, (3, p.lens[b] // 2, p.lens[b] - p.news[b] // 2 - 1, p.lens[b] - 1)[b % 4], odd)
+    ref = as_defined(p, attend(p, causal=causal, window=window), causal, window)
+    assert not np.isfinite(ref).all()
