@@ -347,6 +347,16 @@ __global__ __launch_bounds__(THREADS, (PER_CU<DIM, NC>)) void cache_attend_few(c
 #pragma unroll
                 for (int i = 0; i < ROWS; ++i) vs[i] *= v_down;
             }
+            if constexpr (S8) {
+                // an infinite scale makes infinities of both signs of a key's codes, whose score is NaN
+                float most = 0.0f;
+#pragma unroll
+                for (int i = 0; i < ROWS; ++i) most = fmaxf(most, fabsf(ks[i]));
+                if (__any(most > FLT_MAX)) {
+#pragma unroll
+                    for (int i = 0; i < ROWS; ++i) ks[i] = fabsf(ks[i]) > FLT_MAX ? __builtin_nanf("") : ks[i];
+                }
+            }
             u32x4 p[NC][S8 ? 2 : 1];
             float x[NC][ROWS];
 #pragma unroll

@@ -155,3 +155,14 @@ def test_values_that_are_not_finite(odd, causal, window, form, cache):
         plant(p, "v", b, (3, p.lens[b] // 2, p.lens[b] - p.news[b] // 2 - 1, p.lens[b] - 1)[b % 4], odd)
     ref = as_defined(p, attend(p, causal=causal, window=window), causal, window)
     assert not np.isfinite(ref).all()
+
+
+@pytest.mark.parametrize("form", list(FORMS))
+@pytest.mark.parametrize("odd", [NAN, INF, -INF])
+@pytest.mark.parametrize("cache", CACHES)
+def test_keys_that_are_not_finite(cache, odd, form):
+    """(In 8 bits an infinite scale: dims of both signs, and so a score of NaN.)"""
+    p = problem(form, cache, 63)
+    for b, n in enumerate(p.lens):
+        plant(p, "k", b, min(n - 1, 4 + n // 3), odd, dim=9)
+    as_defined(p, attend(p))
