@@ -113,16 +113,15 @@ __device__ __forceinline__ float to_unit(const float most, float* const up)
 }
 
 // Values that are not finite, in steps of keys that not all columns see in full (all_from .. all_to are seen by all), are left
-// out of the products, where they would reach all columns.  This is their sum over the keys from .. to, of one dim; with any, it
-// is the result of the column (the weights are positive).
+// out of the products, where they would reach all columns.  This is their sum over the keys from .. to, of one dim, which is added to the
+// column's own: it is not finite if there are any (and their weights, which are positive, make no difference), else 0.
 template <spmm_cache_type_t TYPE, int STEP>
-__device__ __forceinline__ bool odd_sum(const AttendArgs& a, const int32_t* table, const int last_page, const int h, const int row, const int from, const int to,
-                                        const int all_from, const int all_to, float* const sum)
+__device__ __forceinline__ float odd_sum(const AttendArgs& a, const int32_t* table, const int last_page, const int h, const int row, const int from, const int to,
+                                         const int all_from, const int all_to)
 {
     const int shift = a.pool.page_shift, inside = (1 << shift) - 1;
     const int full_from = (all_from + STEP - 1) / STEP * STEP, full_to = (all_to + 1) / STEP * STEP - 1;
-    bool any = false;
-    *sum = 0.0f;
+    float sum = 0.0f;
 #pragma unroll 1
     for (int key = from; key <= to; ++key) {
         if (key >= full_from && key <= full_to) {
@@ -134,11 +133,9 @@ __device__ __forceinline__ bool odd_sum(const AttendArgs& a, const int32_t* tabl
         float v;
         if constexpr (TYPE == SPMM_CACHE_S8) v = (float)((const int8_t*)a.pool.v)[at] * a.pool.v_scale[(page << shift) + (key & inside)];
         else v = (float)((const __bf16*)a.pool.v)[at];
-        if (fabsf(v) <= 3.4e38f) continue;
-        any = true;
-        *sum += v;
+        if (!(fabsf(v) <= 3.4e38f)) sum += v;
     }
-    return any;
+    return sum;
 }
 
 // store(pointer to results of the call's type, function that makes one of a value)

@@ -478,6 +478,15 @@ __global__ __launch_bounds__(THREADS, (PER_CU<DIM, NC>)) void cache_attend_few(c
 #pragma unroll
                 for (int e = 0; e < 4; ++e) part[wave][d * 4 + e][lane] = o[c][d][e] * share;
             __syncthreads();
+            if (odd_found) {
+                const int k_first = (u_first + u0) * UNIT<TYPE>;
+                for (int i = tid; i < N * 4 * 64; i += THREADS) {
+                    const int reg = i / 64, row = 16 * (reg / 4) + 4 * (i % 64 / 16) + reg % 4, column = c * COLS + i % COLS, t = column / G;
+                    if (column < rows && row < D)
+                        part[0][reg][i % 64] += odd_sum<TYPE, STEP>(a, table, last_page, h, row, max(k_first, s.first_seen(a, t)), min(k_end, s.last_seen(a, t)), all_from, all_to);
+                }
+                __syncthreads();
+            }
             if (!whole && tid < COLS) {
                 slot[c * COLS + tid] = top;
                 slot[(NC + c) * COLS + tid] = all;
@@ -495,16 +504,6 @@ __global__ __launch_bounds__(THREADS, (PER_CU<DIM, NC>)) void cache_attend_few(c
                     store_out(a, ((int64_t)head[c] * D + row) * a.ldo + s.first + token[c], all == 0.0f ? 0.0f : y * inv);
             }
             __syncthreads();
-        }
-        if (odd_found) {
-            const int k_first = (u_first + u0) * UNIT<TYPE>;
-            for (int i = tid; i < NC * COLS * DIM; i += THREADS) {
-                const int row = i % DIM, c = i / DIM, t = c / G;
-                float sum;
-                if (c >= rows || row >= D || !odd_sum<TYPE, STEP>(a, table, last_page, h, row, max(k_first, s.first_seen(a, t)), min(k_end, s.last_seen(a, t)), all_from, all_to, &sum)) continue;
-                if (!whole) slot[2 * NC * COLS + (c / COLS * N * 4 + row / 16 * 4 + row % 4) * 64 + row % 16 / 4 * 16 + c % COLS] = sum;
-                else store_out(a, ((int64_t)(h * G + c % G) * D + row) * a.ldo + s.first + t, sum);
-            }
         }
         if constexpr (WHOLE) return;
         done += u1 - u0;

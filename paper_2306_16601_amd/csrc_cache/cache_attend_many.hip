@@ -588,16 +588,33 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void cache_attend_many(const Atten
     }
     lds_barrier();
     if (!odd_found) return;
+    uint64_t* const marks = (uint64_t*)keys0.at;        // of a thread's results: those that are +inf or NaN, and those that are -inf or NaN
+    if constexpr (!SPLIT) {
+        static_assert(sizeof(keys0) >= 2 * THREADS * sizeof(uint64_t) && DT * 16 <= 64, "a bit for each sum of each thread");
+        uint64_t plus = 0, minus = 0;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float y = o[d][r] + (l - l);
+                plus |= (uint64_t)!(y < -NONE) << (d * 16 + r);
+                minus |= (uint64_t)!(y > NONE) << (d * 16 + r);
+            }
+        marks[tid] = plus;
+        marks[THREADS + tid] = minus;
+    }
     __syncthreads();        // (the results are written)
     for (int i = tid; i < BLOCK<GROUPS> * DIM; i += THREADS) {
         const int row = i % DIM, c = blk.c0 + i / DIM, token = c / G;
-        float sum;
-        if (c >= blk.c1 || row >= D || !odd_sum<TYPE, TILE>(a, table, last_page, h, row, max(first, s.first_seen(a, token)), min(end - 1, s.last_seen(a, token)), all_from, all_to, &sum))
-            continue;
+        if (c >= blk.c1 || row >= D) continue;
+        float sum = odd_sum<TYPE, TILE>(a, table, last_page, h, row, max(first, s.first_seen(a, token)), min(end - 1, s.last_seen(a, token)), all_from, all_to);
+        if (fabsf(sum) <= 3.4e38f) continue;
+        const int w = i / DIM / 32, at = row / 32 * 16 + row % 32 / 8 * 4 + row % 4, from = row % 8 / 4 * 32 + i / DIM % 32;      // register and lane
         if constexpr (SPLIT) {
-            const int w = i / DIM / 32, r = row % 8;
-            slot[2 * BLOCK<GROUPS> + w * 32 * DIM + (row / 32 * 16 + row % 32 / 8 * 4 + r % 4) * 64 + r / 4 * 32 + i / DIM % 32] = sum;
+            slot[2 * BLOCK<GROUPS> + w * 32 * DIM + at * 64 + from] += sum;
         } else {
+            if (marks[w * 64 + from] >> at & 1) sum -= NONE;
+            if (marks[THREADS + w * 64 + from] >> at & 1) sum += NONE;
             store_out(a, ((int64_t)(h * G + c % G) * D + row) * a.ldo + s.first + token, sum);
         }
     }

@@ -166,3 +166,26 @@ def test_keys_that_are_not_finite(cache, odd, form):
     for b, n in enumerate(p.lens):
         plant(p, "k", b, min(n - 1, 4 + n // 3), odd, dim=9)
     as_defined(p, attend(p))
+
+
+@pytest.mark.parametrize("form", list(FORMS))
+@pytest.mark.parametrize("seen_by_all, seen_by_some", [(INF, -INF), (-INF, INF), (NAN, INF), (INF, INF), (INF, NAN)])
+@pytest.mark.parametrize("cache", CACHES)
+def test_values_of_both_signs(cache, seen_by_all, seen_by_some, form):
+    """An infinity that some columns see does not hide what they all see."""
+    p = problem(form, cache, 62)
+    for b, n in enumerate(p.lens):
+        plant(p, "v", b, 2, seen_by_all)
+        plant(p, "v", b, n - 1 - p.news[b] // 3, seen_by_some)
+    as_defined(p, attend(p))
+
+
+@pytest.mark.parametrize("form", list(FORMS))
+@pytest.mark.parametrize("cache", CACHES)
+def test_scores_of_nan_beside_infinite_values(cache, form):
+    """A column with a score of NaN is NaN as a whole, whatever else it sees."""
+    p = problem(form, cache, 64)
+    for b, n in enumerate(p.lens):
+        plant(p, "k", b, min(n - 1, 4 + n // 3), NAN, dim=9)
+        plant(p, "v", b, n - 1 - p.news[b] // 3, INF)
+    as_defined(p, attend(p))
