@@ -138,6 +138,9 @@ __device__ __forceinline__ float odd_sum(const AttendArgs& a, const int32_t* tab
     return sum;
 }
 
+// The result where the sum of the weights is 0: nothing is visible, or what is (from .. to) has scores of -inf alone, whose softmax is NaN.
+__device__ __forceinline__ float of_nothing(const int from, const int to) { return from <= to ? __builtin_nanf("") : 0.0f; }
+
 // store(pointer to results of the call's type, function that makes one of a value)
 template <typename F>
 __device__ __forceinline__ void store_type(const AttendArgs& a, const F& store)

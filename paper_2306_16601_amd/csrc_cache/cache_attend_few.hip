@@ -501,7 +501,7 @@ __global__ __launch_bounds__(THREADS, (PER_CU<DIM, NC>)) void cache_attend_few(c
                 const int row = 16 * (i / 4) + 4 * g_out + i % 4;
                 if (!whole) slot[2 * NC * COLS + (c * N * 4 + i) * 64 + lane] = y;
                 else if (c * COLS + col < rows && row < D)
-                    store_out(a, ((int64_t)head[c] * D + row) * a.ldo + s.first + token[c], all == 0.0f ? 0.0f : y * inv);
+                    store_out(a, ((int64_t)head[c] * D + row) * a.ldo + s.first + token[c], all == 0.0f ? of_nothing(lo[c], hi[c]) : y * inv);
             }
             __syncthreads();
         }
@@ -571,10 +571,11 @@ __global__ __launch_bounds__(THREADS) void cache_join(const AttendArgs a, const 
     const float all = sums[0][c * COLS + col], inv = all == 0.0f ? 0.0f : 1.0f / all;
     const int i0 = c * COLS + col, token = i0 / a.group, head = h * a.group + i0 % a.group;
     if (i0 >= rows) return;
+    const float nothing = of_nothing(s.first_seen(a, token), s.last_seen(a, token));
 #pragma unroll
     for (int i = 0; i < SLICE; ++i) {
         const int j = r0 % (N * 4) + i, row = 16 * (j / 4) + 4 * g + j % 4;
-        if (row < D) store_out(a, ((int64_t)head * D + row) * a.ldo + s.first + token, all == 0.0f ? 0.0f : y[i] * inv);
+        if (row < D) store_out(a, ((int64_t)head * D + row) * a.ldo + s.first + token, all == 0.0f ? nothing : y[i] * inv);
     }
 }
 

@@ -573,7 +573,7 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void cache_attend_many(const Atten
 #pragma unroll
             for (int r = 0; r < 16; ++r) slot[2 * BLOCK<GROUPS> + wave * 32 * DIM + (d * 16 + r) * 64 + lane] = o[d][r] * (S8 ? v_up : 1.0f);
     } else if (i < blk.c1) {
-        const float inv = l == 0.0f ? 0.0f : (S8 ? v_up : 1.0f) / l;
+        const float inv = l == 0.0f ? 0.0f : (S8 ? v_up : 1.0f) / l, nothing = of_nothing(lo, hi);
         const int64_t to = ((int64_t)(h * G + i % G) * D + 4 * half) * a.ldo + s.first + i / G;
         store_type(a, [&](auto* out, auto encode) INLINE {
             auto* const column = out + to;
@@ -582,7 +582,7 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void cache_attend_many(const Atten
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int row = 32 * d + 8 * (r / 4) + r % 4;
-                    if (EXACT || row + 4 * half < D) column[row * a.ldo] = encode(l == 0.0f ? 0.0f : o[d][r] * inv);
+                    if (EXACT || row + 4 * half < D) column[row * a.ldo] = encode(l == 0.0f ? nothing : o[d][r] * inv);
                 }
         });
     }
@@ -648,10 +648,11 @@ __global__ __launch_bounds__(64) void cache_join_many(const AttendArgs a, const 
     if (i >= blk.c1) return;
     const float inv = all == 0.0f ? 0.0f : 1.0f / all;
     const int token = i / a.group, head = h * a.group + i % a.group;
+    const float nothing = of_nothing(s.first_seen(a, token), s.last_seen(a, token));
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
         const int row = 32 * d + 8 * (r / 4) + 4 * half + r % 4;
-        if (row < a.pool.head_dim) store_out(a, ((int64_t)head * a.pool.head_dim + row) * a.ldo + s.first + token, all == 0.0f ? 0.0f : y[r] * inv);
+        if (row < a.pool.head_dim) store_out(a, ((int64_t)head * a.pool.head_dim + row) * a.ldo + s.first + token, all == 0.0f ? nothing : y[r] * inv);
     }
 }
 

@@ -189,3 +189,15 @@ def test_scores_of_nan_beside_infinite_values(cache, form):
         plant(p, "k", b, min(n - 1, 4 + n // 3), NAN, dim=9)
         plant(p, "v", b, n - 1 - p.news[b] // 3, INF)
     as_defined(p, attend(p))
+
+
+@pytest.mark.parametrize("form", list(FORMS))
+def test_nothing_but_scores_of_minus_infinity(form):
+    """The softmax of nothing but -inf is NaN; 0 is the result only where nothing is visible."""
+    p = problem(form, "bf16", 65)
+    p.q[:, :, 9] = p.q[:, :, 9].abs() + 0.1
+    for b, n in enumerate(p.lens):
+        for at in range(n if b % 2 else min(n, p.lens[b] - p.news[b] + 2)):
+            plant(p, "k", b, at, -INF, dim=9)
+    ref = as_defined(p, attend(p))
+    assert np.isnan(ref).any() and np.isfinite(ref).any()
