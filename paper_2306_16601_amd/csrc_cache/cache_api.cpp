@@ -1,6 +1,8 @@
 // C ABI of the paged cache (include/spmm_cache.h): argument checks, scratch layout, launches.
 #include "cache_internal.h"
 
+#include <algorithm>
+#include <cfloat>
 #include <cmath>
 
 using namespace spmm_cache;
@@ -193,7 +195,7 @@ spmm_status_t spmm_cache_attend(const spmm_cache_t* cache, int32_t layer, const 
     a.window = how->window;
     a.out_type = ot;
     a.out_zero_point = coded ? how->out_zero_point : 0;
-    a.scale_log2 = (float)((double)how->scale * 1.4426950408889634);
+    a.scale_log2 = (float)std::min((double)how->scale * 1.4426950408889634, (double)FLT_MAX);      // (finite: a score of 0 stays 0)
     a.out_inv = coded ? 1.0f / how->out_scale : 1.0f;
     return status_of(launch_attend(a, cache->type, hip_stream));
 }

@@ -201,3 +201,15 @@ def test_nothing_but_scores_of_minus_infinity(form):
             plant(p, "k", b, at, -INF, dim=9)
     ref = as_defined(p, attend(p))
     assert np.isnan(ref).any() and np.isfinite(ref).any()
+
+
+@pytest.mark.parametrize("cache", CACHES)
+@pytest.mark.parametrize("new", [1, 40, 300])
+def test_the_largest_scale(new, cache):
+    """log2(e) times it is beyond binary32; a zero query's scores are zero all the same."""
+    p = Problem([new, 3], [77, 20], 4, 2, 64, 32, cache, seed=45)
+    p.q.zero_()
+    scale = 3.4e38
+    got = attend(p, scale=scale).double().numpy()
+    ref, mag = p.attention(scale)
+    assert (np.abs(got - ref) <= (2.0 ** -8 + 1e-4) * mag).all()
