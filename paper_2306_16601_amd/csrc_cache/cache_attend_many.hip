@@ -103,22 +103,26 @@ __device__ __forceinline__ void scale_in_place(float& o, const float by)
     o = y;
 }
 
-// Eight codes times scales, in binary16, rounded once: (n + 128) s - 128 s is n s but for the last place of binary32.  `odd`: among the
-// scales are some that are not finite.
+// Eight codes times scales, in binary16, rounded once: (n + 128) s - 128 s is n s but for the last place of binary32, and for scales that
+// are not finite.
 template <typename F>
-__device__ __forceinline__ f16x8 scaled(uint32_t a, uint32_t b, const F& by, const bool odd)
+__device__ __forceinline__ f16x8 scaled(uint32_t a, uint32_t b, const F& by)
 {
-    if (odd) {
-        f16x8 r;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) r[j] = (_Float16)((float)(int8_t)((j < 4 ? a : b) >> 8 * (j % 4)) * by(j));
-        return r;
-    }
     a ^= 0x80808080u;
     b ^= 0x80808080u;
     f16x8 r;
 #pragma unroll
     for (int j = 0; j < 8; ++j) r[j] = (_Float16)__fmaf_rn((float)((j < 4 ? a : b) >> 8 * (j % 4) & 0xff), by(j), -128.0f * by(j));
+    return r;
+}
+
+// the same for any scales
+template <typename F>
+__device__ __forceinline__ f16x8 product(const uint32_t a, const uint32_t b, const F& by)
+{
+    f16x8 r;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r[j] = (_Float16)((float)(int8_t)((j < 4 ? a : b) >> 8 * (j % 4)) * by(j));
     return r;
 }
 
@@ -262,7 +266,6 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void cache_attend_many(const Atten
             if (!k_here) lane_k = 0.0f;     // (they may be anything)
             if (!v_here) lane_v = 0.0f;
             const float mk = wave_max(fabsf(lane_k) <= 3.4e38f ? fabsf(lane_k) : 0.0f), mv = wave_max(fabsf(lane_v) <= 3.4e38f ? fabsf(lane_v) : 0.0f);
-            const bool v_odd = __any(!(fabsf(lane_v) <= 3.4e38f));      // (such keys have scores of NaN)
             k_up_last = k_up;
             float up;
             const float k_down = to_unit(mk, &k_up);
@@ -282,13 +285,23 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void cache_attend_many(const Atten
                 if (is_key(i)) {
                     const float by = scales[wave][0][row];
                     const int c = u % UPR * 2;
-                    *(f16x8*)(tk.at + row * KC + turned<KC>(row, c)) = scaled(raw[i][0], raw[i][1], [&](int) { return by; }, false);
-                    *(f16x8*)(tk.at + row * KC + turned<KC>(row, c + 1)) = scaled(raw[i][2], raw[i][3], [&](int) { return by; }, false);
+                    *(f16x8*)(tk.at + row * KC + turned<KC>(row, c)) = scaled(raw[i][0], raw[i][1], [&](int) { return by; });
+                    *(f16x8*)(tk.at + row * KC + turned<KC>(row, c + 1)) = scaled(raw[i][2], raw[i][3], [&](int) { return by; });
                 } else {
                     const float* const by = scales[wave][1] + u % 4 * 16;
                     const int c = u % 4 * 2;
-                    *(f16x8*)(tv.at + row * 8 + turned<8>(row, c)) = scaled(raw[i][0], raw[i][1], [&](const int j) { return by[j]; }, v_odd);
-                    *(f16x8*)(tv.at + row * 8 + turned<8>(row, c + 1)) = scaled(raw[i][2], raw[i][3], [&](const int j) { return by[8 + j]; }, v_odd);
+                    *(f16x8*)(tv.at + row * 8 + turned<8>(row, c)) = scaled(raw[i][0], raw[i][1], [&](const int j) { return by[j]; });
+                    *(f16x8*)(tv.at + row * 8 + turned<8>(row, c + 1)) = scaled(raw[i][2], raw[i][3], [&](const int j) { return by[8 + j]; });
+                }
+            }
+            if (__any(!(fabsf(lane_v) <= 3.4e38f))) {       // (infinite values; such keys have scores of NaN)
+#pragma unroll
+                for (int i = 0; i < UNITS; ++i) {
+                    const int u = unit_of(i), row = u / 4, c = u % 4 * 2;
+                    const float* const by = scales[wave][1] + u % 4 * 16;
+                    if (is_key(i)) continue;
+                    *(f16x8*)(tv.at + row * 8 + turned<8>(row, c)) = product(raw[i][0], raw[i][1], [&](const int j) { return by[j]; });
+                    *(f16x8*)(tv.at + row * 8 + turned<8>(row, c + 1)) = product(raw[i][2], raw[i][3], [&](const int j) { return by[8 + j]; });
                 }
             }
         }
