@@ -95,7 +95,18 @@ spmm_status_t spmm_cache_append(const spmm_cache_t *cache, int32_t layer, const 
  * query head h reading key/value head h / (q_heads / n_heads).  Token j is visible to the token at position
  * i if j < kv_len, with `causal` j <= i, and with a window j > i - window.  Where nothing is visible the
  * result is 0.  What is not visible has no influence, whatever it holds (NaN and infinities too).
- * Softmax statistics and sums are held in binary32; weights are rounded to bfloat16 for the product with v. */
+ * Scores, softmax statistics and sums are held in binary32.  Operands of the products are rounded, whatever out_type is:
+ *   BF16 caches: weights to bfloat16; the sum of weights is that of the rounded ones.
+ *   S8 caches: queries, and weights, to binary16, over powers of two.  Up to 32 columns a key/value head (the query heads that
+ *   share it times max_new) codes are exact, weights are rounded with the values' scales in them, and the sum is of
+ *   the unrounded ones; with more columns keys and values, code * scale, are rounded too, and the sum is of the rounded weights.
+ *   What is below 2^-24 of the largest query, weight or scale it is multiplied beside is lost.
+ * Values that are not finite reach the columns that see them, as infinities or NaN (an infinity whose weight is rounded to 0 gives NaN);
+ * a score of NaN or +inf makes its column NaN, and so do scores of -inf alone.  A scale of keys that is not finite makes the
+ * token's scores NaN.
+ * One kernel is chosen for all sequences, by max_new: a batch that mixes prompts with single tokens of long contexts is
+ * faster in two calls (q_start, kv_len and table can be entered at any sequence, q and out are the same), and a max_new far above
+ * what there is costs as much as such a prompt would. */
 typedef struct {
     int32_t q_heads;            /* multiple of the cache's n_heads                               */
     int64_t max_new;            /* most new tokens of any sequence, or an upper bound (>= 1); of a sequence

@@ -9,9 +9,11 @@
 // operand are consecutive tokens, which V, whose tokens are contiguous, is loaded in 16 bytes at a time.
 //
 // bfloat16 caches are multiplied as they are, with weights in bfloat16; the sum of the weights is that of the rounded ones, so
-// that one that outweighs all others is exactly 1 (and half of the rounding's error cancels).  Codes of 8 bits are exact in
-// binary16 as well, which holds weights 8 times as exactly: they are widened to it.  Queries are brought to [1, 2) by a power
-// of two for each column before they are narrowed to binary16, and weights times the values' scales by a power of two that
+// that one that outweighs all others is exactly 1 (and half of the rounding's error cancels).  Codes of 8 bits are widened to
+// binary16, which holds weights 8 times as exactly: for few columns by themselves, which is exact, with the keys' scales on the scores and the
+// values' on the weights; for many columns times their scales, rounded once (results come out 1.07 times as far off as with one
+// rounding at the end): a product for each code, where scales on scores and weights would cost one for each column.  Queries are brought to [1, 2) by a power
+// of two for each column before they are narrowed to binary16, and scales, or weights times scales, by a power of two that
 // follows the largest scale, so that neither leaves its range; what is small beside the largest loses at most 2^-24 of that.
 #pragma once
 

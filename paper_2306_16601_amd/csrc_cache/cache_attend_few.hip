@@ -6,8 +6,8 @@
 // the keys of a unit in turn; a wave loads operands straight from the pages to registers, 16 bytes a lane, the next step's
 // keys and page numbers while it works on this one's: 64 KB on the way for each workgroup.  Where a run covers a whole head
 // the result is written; parts of a head go to scratch and are joined by cache_join, in the order of the keys.  64 tokens on
-// contexts of up to 8191, 32 heads on 8 of 128: 226 us, 5.2 TB/s; with a workgroup for each head 574 us, as long as the longest
-// takes.  4 x 3 tokens on 131 thousand keys in 8 bits: 213 us and 7 to join.
+// contexts of up to 8191, 32 heads on 8 of 128: 227 us, 5.2 TB/s; with a workgroup for each head 574 us, as long as the longest
+// takes.  4 x 3 tokens on 131 thousand keys in 8 bits: 216 us and 7 to join.
 #include "cache_attend.h"
 
 #include <cfloat>

@@ -9,20 +9,21 @@
 // (over a power of two for the tile) on the way.  Scores, weights and sums stay in registers: see cache_attend.h; with the
 // 32x32 instruction the lane's 16 scores of a tile of 32 keys are tokens 8 h .. 8 h + 7 of each half (h = lane / 32).
 // The running maximum moves only when a score exceeds it by 2^8: the weights have the room, and the sums need no scaling then
-// (two prompts of 4097 tokens 363 us, with every larger score 377; means of two runs, as below).
+// (two prompts of 4097 tokens 313 us, with every larger score 330; whole calls, means of two runs of 400, as below).
 //
 // A wave goes through two phases for a tile: products (values of tile i with its weights, then scores of tile i + 1), and
 // the softmax of tile i + 1.  Two waves share a SIMD, and the matrix unit stands still while both are in the second.  With
 // bfloat16 that is left to chance, between two workgroups of 128 columns: two prompts of 4097 tokens, 32 heads on 8 of 128,
-// 332 us (0.83 PFLOP/s, the matrix unit busy for 43 % of the cycles, at 1.9 GHz: the card's power bounds it as well).  With 256
-// columns, waves 4 to 7 held half a tile behind waves 0 to 3 by a barrier after each phase, it took 346 us; so that form is
-// taken for 8 bits only, whose widening twice the columns share (500 tokens behind 15000: 236 us, 128 columns 264).
+// 313 us (0.88 PFLOP/s, the matrix unit busy for 43 % of the cycles, at 2.0 GHz: the card's power bounds it as well).  With 256
+// columns, waves 4 to 7 held half a tile behind waves 0 to 3 by a barrier after each phase, the compiler spills 77 registers and it takes
+// 485 us (346 against 332 before results were stored by type); so that form is
+// taken for 8 bits only, whose widening twice the columns share (500 tokens behind 15000: 197 us, 128 columns 213).
 //
 // Blocks are dealt out head by head, the longest first, to one XCD after the other, so that blocks that read the same keys
-// share an L2 (in the order of their numbers 412 instead of 363 us, and 16 sequences of up to
-// 384 tokens 27.5 instead of 22.4).  Where the device could run twice as many workgroups as there are blocks, or more, the tiles
+// share an L2 (in the order of their numbers 360 instead of 313 us, and 16 sequences of up to
+// 384 tokens 24.3 instead of 19.4).  Where the device could run twice as many workgroups as there are blocks, or more, the tiles
 // of each block are dealt to `parts` workgroups, and cache_join_many joins what they write to scratch (500 tokens behind 15000,
-// 8 bits: 236 instead of 685 us).
+// 8 bits: 197 instead of 695 us).
 #include "cache_attend.h"
 
 #include <cfloat>
