@@ -11,6 +11,10 @@
  *   k        [n_layers][n_pages][n_heads][page_tokens][head_dim]    BF16 or S8
  *   v        [n_layers][n_pages][n_heads][head_dim][page_tokens]    (tokens contiguous, like activations)
  *   k_scale, v_scale  [n_layers][n_pages][n_heads][page_tokens]     binary32, S8 only:  value = code * scale
+ *   bounds   [n_layers][n_pages][n_heads][2][head_dim]              BF16: largest and smallest value of each dim of a page's keys
+ *   weight   [n_layers][n_pages][n_heads][page_tokens]              binary32: attention that a token has had so far
+ * The last two are there where long contexts are read in part (spmm_cache_score) or cut down (spmm_cache_evict); fork, compact
+ * and copy move all parts of a page.
  * One page table serves all layers: row b names the pages of sequence b in order, token p lies in page
  * table[b][p / page_tokens]; entries that are not in use are -1.
  *
@@ -43,6 +47,10 @@ typedef struct {
     int32_t head_dim;           /* multiple of 16, at most 128 (else SPMM_E_UNSUPPORTED)         */
     int32_t page_tokens;        /* 16, 32, 64, 128 or 256 (else SPMM_E_UNSUPPORTED)              */
     int64_t n_pages;            /* 1 .. 2^31 - 1                                                 */
+    void *bounds;               /* device, 16-byte aligned, or NULL: no call needs them but
+                                   spmm_cache_bounds and spmm_cache_score                        */
+    float *weight;              /* device, 16-byte aligned, or NULL: no call needs them but
+                                   spmm_cache_weigh and spmm_cache_evict                         */
 } spmm_cache_t;
 
 /* A batch of sequences and their new tokens.  The new tokens of sequence b are the columns q_start[b] ..
@@ -160,6 +168,99 @@ spmm_status_t spmm_cache_copy(const spmm_cache_t *cache, const int32_t *src, con
 
 /* Bytes of scratch of spmm_cache_fork (n_rows: of the new table) and spmm_cache_compact; *bytes is HOST memory. */
 spmm_status_t spmm_cache_work_bytes(const spmm_cache_t *cache, int64_t n_rows, int64_t *bytes);
+
+/* ---- Long contexts: reading the pages that matter, dropping the tokens that do not ----------------------------
+ *
+ * A step of new tokens   spmm_cache_append -> spmm_cache_bounds -> spmm_cache_score -> spmm_cache_select ->
+ * spmm_cache_attend_selected   reads the pages of a list for each new token and key/value head instead of all of them.
+ * spmm_cache_weigh adds up what attention each token gets, and spmm_cache_evict keeps the tokens that got most of it.
+ * "Visible" is what it is in spmm_cache_attend (kv_len, causal, window), token by token; columns at a negative position see nothing. */
+
+/* Bounds of the pages that the batch's new tokens lie in (of layer `layer`): of each head and dim the largest and the
+ * smallest of the keys' values (code * scale in S8 caches, in binary32, rounded to bfloat16) of all tokens of the page below kv_len;
+ * where one of them is not finite, both are NaN.  The call follows spmm_cache_append of the same batch.  A batch that says that all
+ * tokens of its sequences are new (q_start[b + 1] - q_start[b] = kv_len[b]) has all of their pages' bounds made again, as after an
+ * eviction.  T: columns of the batch; a number that is too small or too large costs time and nothing else. */
+spmm_status_t spmm_cache_bounds(const spmm_cache_t *cache, int32_t layer, const spmm_batch_t *batch, int64_t T, void *hip_stream);
+
+/* Which pages a new token reads. */
+typedef struct {
+    int32_t q_heads;            /* multiple of the cache's n_heads                               */
+    int32_t pages;              /* most pages of a list (>= 1)                                   */
+    int32_t first, last;        /* >= 0, together at most `pages`: so many of the first and of the last
+                                   pages with a visible token are taken whatever their scores are */
+    int32_t causal;
+    int32_t window;             /* 0: none                                                       */
+} spmm_select_t;
+
+/* scores[t][h][i] (device, binary32 [T][n_heads][lds], lds >= ld_table, 4-byte aligned): of every column t, key/value head h and
+ * page i of its sequence's row with a visible token, an upper bound of the products q . k of the page's keys:
+ *   max over the query heads of h of   sum_d q_d > 0 ? q_d hi_d : q_d lo_d,
+ * binary32 sums of products of the bounds hi, lo; NaN where a bound is.  Pages without a visible token, up to ld_table: -inf.  Columns of no
+ * sequence are left as they were.  q: as for spmm_cache_attend.  (pages, first and last are not read, but checked.) */
+spmm_status_t spmm_cache_score(const spmm_cache_t *cache, int32_t layer, const spmm_batch_t *batch, const void *q, int64_t T,
+                               const spmm_select_t *how, float *scores, int64_t lds, void *hip_stream);
+
+/* lists[t][h] (device, int32 [T][n_heads][pages]): of the pages of a column's row with a visible token the first `first`, the last
+ * `last`, and those of highest score, `pages` in all or as many as there are: in ascending order, then -1.  Of equal
+ * scores the lower page is taken; NaN counts as the highest.  Columns of no sequence are left as they were.  The scores may come from
+ * anywhere; those of spmm_cache_score are for the same causal and window. */
+spmm_status_t spmm_cache_select(const spmm_cache_t *cache, const spmm_batch_t *batch, const float *scores, int64_t T, int64_t lds,
+                                const spmm_select_t *how, int32_t *lists, void *hip_stream);
+
+/* Bytes of scratch that spmm_cache_attend_selected takes for such a call; *bytes is HOST memory. */
+spmm_status_t spmm_selected_work_bytes(const spmm_cache_t *cache, int64_t T, const spmm_attend_t *how, int64_t pages, int64_t *bytes);
+
+/* spmm_cache_attend over the pages of lists [T][n_heads][pages] (device, int32): column t's softmax for the query heads of h is over the visible
+ * tokens of the pages lists[t][h] of its row.  Numbers below 0 or not below ld_table name no page; pages may come in any order, and one that is
+ * named twice counts twice.  All columns of a sequence are computed (how->max_new is not read, but checked).  Results, rounding, out, ldo
+ * and work as for spmm_cache_attend, with S8 caches as for few columns there. */
+spmm_status_t spmm_cache_attend_selected(const spmm_cache_t *cache, int32_t layer, const spmm_batch_t *batch, const void *q, int64_t T,
+                                         const spmm_attend_t *how, const int32_t *lists, int64_t pages, void *out, int64_t ldo, void *work,
+                                         void *hip_stream);
+
+/* How attention is added up. */
+typedef struct {
+    int32_t q_heads;            /* multiple of the cache's n_heads                               */
+    int64_t max_new;            /* the last max_new new tokens of a sequence count (>= 1)        */
+    float scale;                /* > 0, finite: of the scores, as for spmm_cache_attend          */
+    int32_t causal;
+    int32_t window;             /* 0: none                                                       */
+    float decay;                /* 0 .. 1: what stays of the weights of earlier calls            */
+} spmm_weigh_t;
+
+/* Bytes of scratch that spmm_cache_weigh takes for such a call (of the batch its n_seqs and ld_table count); *bytes is HOST memory. */
+spmm_status_t spmm_weigh_work_bytes(const spmm_cache_t *cache, const spmm_batch_t *batch, int64_t T, const spmm_weigh_t *how, int64_t *bytes);
+
+/* The cache's weights of layer `layer`, for every token j < kv_len of every sequence with new tokens, and every key/value head h:
+ *   weight[j] = (j is one of the new tokens ? 0 : decay * weight[j]) + sum over the last max_new new tokens t and the query heads of h of
+ *               softmax over the visible tokens of scale * (q_t . k)   at j  (0 where j is not visible).
+ * So weights need no initialisation.  Sequences without a new token are left as they were.  Scores, statistics and sums are binary32, and nothing
+ * is rounded to less (codes of S8 caches are exact in the products, and scales are on the scores).  A score of NaN or +inf makes its column's weights NaN,
+ * and so do scores of -inf alone.  The order of the sums does not change from call to call.  A page that two rows name gets the weights of one of them
+ * (of a call with both; which one is not said).  q: as for spmm_cache_attend.  work: spmm_weigh_work_bytes bytes, as for attend. */
+spmm_status_t spmm_cache_weigh(const spmm_cache_t *cache, int32_t layer, const spmm_batch_t *batch, const void *q, int64_t T,
+                               const spmm_weigh_t *how, void *work, void *hip_stream);
+
+/* What stays. */
+typedef struct {
+    int32_t first, recent;      /* >= 0: so many of the first and of the last tokens stay, whatever their weights are */
+    int64_t most;               /* most tokens of a row that stay, or an upper bound (>= 1)      */
+} spmm_evict_t;
+
+/* Keeps n = min(keep[b], kv_len[b], most) tokens of every row b, in every layer and key/value head of their own: the first min(first, n), then
+ * the last ones, recent of them if n has room, and of the others those of the largest weight (of equal ones the earlier token; NaN counts as the largest).
+ * They go, in their order, to the first n tokens of row b of table_to: keys, values, scales and weights, as they are.
+ *   table, table_to  device [n_rows][ld_table].  table_to names the pages that take what stays: the same table (rows are then cut down in place, and
+ *                    pages behind them can be freed by spmm_cache_fork), or pages that fork has given out, which neither `table` nor another row
+ *                    names; no page may be in two rows that both write to it.  What table_to has no page for is lost.
+ *   kept             device, int32 [n_layers][n_rows][n_heads][most]: the tokens that stay, ascending, then -1
+ *   kv_len_out       device [n_rows], another buffer than kv_len: n
+ * What stays is rotated to where it was, so later tokens are appended with `positions` (spmm_append_t) that go on counting from where the
+ * sequence was before; a window of spmm_attend_t is one of places in the cache.  Bounds of the pages are not moved: see spmm_cache_bounds. */
+spmm_status_t spmm_cache_evict(const spmm_cache_t *cache, const int32_t *table, int64_t ld_table, const int32_t *kv_len, int64_t n_rows,
+                               const int32_t *keep, const spmm_evict_t *how, const int32_t *table_to, int32_t *kv_len_out, int32_t *kept,
+                               void *hip_stream);
 
 #ifdef __cplusplus
 }

@@ -18,6 +18,8 @@ __all__ = [
     "SPMM_CACHE_BF16", "SPMM_CACHE_S8", "SPMM_OUT_BF16", "CACHE_EXPORTS", "spmm_cache_t", "spmm_batch_t", "spmm_append_t", "spmm_attend_t",
     "make_cache", "make_batch", "make_append", "make_attend", "make_rope", "spmm_cache_append", "spmm_cache_attend", "spmm_attend_work_bytes",
     "spmm_cache_fork", "spmm_cache_compact", "spmm_cache_copy", "spmm_cache_work_bytes",
+    "spmm_select_t", "spmm_weigh_t", "spmm_evict_t", "make_select", "make_weigh", "make_evict", "spmm_cache_bounds", "spmm_cache_score", "spmm_cache_select",
+    "spmm_selected_work_bytes", "spmm_cache_attend_selected", "spmm_weigh_work_bytes", "spmm_cache_weigh", "spmm_cache_evict",
 ]
 
 SPMM_CACHE_BF16, SPMM_CACHE_S8 = 0, 1
@@ -26,14 +28,15 @@ ATTEND_OUT_TYPES = {"f32": SPMM_OUT_F32, "bf16": SPMM_OUT_BF16, "s8": SPMM_OUT_S
 _OUT_BYTES = {SPMM_OUT_F32: 4, SPMM_OUT_BF16: 2, SPMM_OUT_S8: 1, SPMM_OUT_U8: 1}
 
 CACHE_EXPORTS = ("spmm_cache_append", "spmm_cache_attend", "spmm_attend_work_bytes", "spmm_cache_fork", "spmm_cache_compact",
-                 "spmm_cache_copy", "spmm_cache_work_bytes")
+                 "spmm_cache_copy", "spmm_cache_work_bytes", "spmm_cache_bounds", "spmm_cache_score", "spmm_cache_select", "spmm_selected_work_bytes",
+                 "spmm_cache_attend_selected", "spmm_weigh_work_bytes", "spmm_cache_weigh", "spmm_cache_evict")
 
 _i64, _i32, _vp, _f32 = ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p, ctypes.c_float
 
 
 class spmm_cache_t(ctypes.Structure):
     _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp), ("type", ctypes.c_int), ("n_layers", _i32), ("n_heads", _i32),
-                ("head_dim", _i32), ("page_tokens", _i32), ("n_pages", _i64)]
+                ("head_dim", _i32), ("page_tokens", _i32), ("n_pages", _i64), ("bounds", _vp), ("weight", _vp)]
 
 
 class spmm_batch_t(ctypes.Structure):
@@ -48,6 +51,18 @@ class spmm_append_t(ctypes.Structure):
 class spmm_attend_t(ctypes.Structure):
     _fields_ = [("q_heads", _i32), ("max_new", _i64), ("scale", _f32), ("causal", _i32), ("window", _i32), ("out_type", _i32),
                 ("out_scale", _f32), ("out_zero_point", _i32)]
+
+
+class spmm_select_t(ctypes.Structure):
+    _fields_ = [("q_heads", _i32), ("pages", _i32), ("first", _i32), ("last", _i32), ("causal", _i32), ("window", _i32)]
+
+
+class spmm_weigh_t(ctypes.Structure):
+    _fields_ = [("q_heads", _i32), ("max_new", _i64), ("scale", _f32), ("causal", _i32), ("window", _i32), ("decay", _f32)]
+
+
+class spmm_evict_t(ctypes.Structure):
+    _fields_ = [("first", _i32), ("recent", _i32), ("most", _i64)]
 
 
 _bound = _native = None
@@ -66,12 +81,22 @@ def _functions() -> ctypes.CDLL:
                 ("spmm_cache_fork", [cache, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _vp, _vp, _vp, _vp]),
                 ("spmm_cache_compact", [cache, _vp, _i64, _i64, _vp, _vp, _vp, _vp]),
                 ("spmm_cache_copy", [cache, _vp, _vp, _i64, _vp]),
-                ("spmm_cache_work_bytes", [cache, _i64, ctypes.POINTER(_i64)])):
+                ("spmm_cache_work_bytes", [cache, _i64, ctypes.POINTER(_i64)]),
+                ("spmm_cache_bounds", [cache, _i32, batch, _i64, _vp]),
+                ("spmm_cache_score", [cache, _i32, batch, _vp, _i64, ctypes.POINTER(spmm_select_t), _vp, _i64, _vp]),
+                ("spmm_cache_select", [cache, batch, _vp, _i64, _i64, ctypes.POINTER(spmm_select_t), _vp, _vp]),
+                ("spmm_selected_work_bytes", [cache, _i64, ctypes.POINTER(spmm_attend_t), _i64, ctypes.POINTER(_i64)]),
+                ("spmm_cache_attend_selected", [cache, _i32, batch, _vp, _i64, ctypes.POINTER(spmm_attend_t), _vp, _i64, _vp, _i64, _vp, _vp]),
+                ("spmm_weigh_work_bytes", [cache, batch, _i64, ctypes.POINTER(spmm_weigh_t), ctypes.POINTER(_i64)]),
+                ("spmm_cache_weigh", [cache, _i32, batch, _vp, _i64, ctypes.POINTER(spmm_weigh_t), _vp, _vp]),
+                ("spmm_cache_evict", [cache, _vp, _i64, _vp, _i64, _vp, ctypes.POINTER(spmm_evict_t), _vp, _vp, _vp, _vp])):
             f = getattr(L, name)
             f.restype, f.argtypes = ctypes.c_int, args
         if _native is not None:
             _native.bind(*(ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in (
-                "spmm_cache_append", "spmm_cache_attend", "spmm_attend_work_bytes", "spmm_cache_fork", "spmm_cache_compact", "spmm_cache_work_bytes")))
+                "spmm_cache_append", "spmm_cache_attend", "spmm_attend_work_bytes", "spmm_cache_fork", "spmm_cache_compact", "spmm_cache_work_bytes",
+                "spmm_cache_bounds", "spmm_cache_score", "spmm_cache_select", "spmm_selected_work_bytes", "spmm_cache_attend_selected",
+                "spmm_weigh_work_bytes", "spmm_cache_weigh", "spmm_cache_evict")))
         _bound = L
     return _bound
 
@@ -101,9 +126,10 @@ def _address(t, what: str):
     return t.data_ptr()
 
 
-def make_cache(k, v, k_scale=None, v_scale=None) -> spmm_cache_t:
+def make_cache(k, v, k_scale=None, v_scale=None, bounds=None, weight=None) -> spmm_cache_t:
     """A cache over the caller's tensors: k [layers, pages, heads, page_tokens, head_dim], v [layers, pages, heads, head_dim, page_tokens],
-    bfloat16, or int8 with scales [layers, pages, heads, page_tokens] in float32."""
+    bfloat16, or int8 with scales [layers, pages, heads, page_tokens] in float32; for long contexts the keys' bounds
+    [layers, pages, heads, 2, head_dim] in bfloat16 and the tokens' weights [layers, pages, heads, page_tokens] in float32."""
     layers, pages, heads, tokens, dim = k.shape
     kind = _name(k)
     if kind not in ("bfloat16", "int8"):
@@ -112,8 +138,9 @@ def make_cache(k, v, k_scale=None, v_scale=None) -> spmm_cache_t:
         raise ValueError("make_cache: int8 caches have scales, others have none")
     scales = (layers, pages, heads, tokens)
     c = spmm_cache_t(_tensor(k, "k", kind), _tensor(v, "v", kind, (layers, pages, heads, dim, tokens)), _tensor(k_scale, "k_scale", "float32", scales),
-                     _tensor(v_scale, "v_scale", "float32", scales), SPMM_CACHE_S8 if kind == "int8" else SPMM_CACHE_BF16, layers, heads, dim, tokens, pages)
-    c._keepalive = (k, v, k_scale, v_scale)
+                     _tensor(v_scale, "v_scale", "float32", scales), SPMM_CACHE_S8 if kind == "int8" else SPMM_CACHE_BF16, layers, heads, dim, tokens, pages,
+                     _tensor(bounds, "bounds", "bfloat16", (layers, pages, heads, 2, dim)), _tensor(weight, "weight", "float32", scales))
+    c._keepalive = (k, v, k_scale, v_scale, bounds, weight)
     return c
 
 
@@ -233,8 +260,94 @@ def spmm_cache_copy(cache: spmm_cache_t, src, dst, n: int, stream=None) -> None:
     _check(_functions().spmm_cache_copy(cache, _tensor(src, "src", "int32", need=n), _tensor(dst, "dst", "int32", need=n), n, stream), "spmm_cache_copy")
 
 
+def make_select(q_heads: int, pages: int, first: int = 1, last: int = 1, causal: bool = True, window: int = 0) -> spmm_select_t:
+    """Lists of at most `pages` pages, the first `first` and the last `last` visible ones among them."""
+    return spmm_select_t(q_heads, pages, first, last, bool(causal), window)
+
+
+def make_weigh(q_heads: int, max_new: int, scale: float, causal: bool = True, window: int = 0, decay: float = 1.0) -> spmm_weigh_t:
+    """The last max_new new tokens of a sequence count; what earlier calls added up is multiplied by decay."""
+    return spmm_weigh_t(q_heads, max_new, scale, bool(causal), window, decay)
+
+
+def make_evict(first: int, recent: int, most: int) -> spmm_evict_t:
+    """The first and the most recent tokens stay, and at most `most` of a row in all."""
+    return spmm_evict_t(first, recent, most)
+
+
+def _scratch(work, need: int):
+    if work is not None and not isinstance(work, int) and _nbytes(work) < need:
+        raise ValueError("work holds %d bytes, %d are wanted" % (_nbytes(work), need))
+    return work if work is None or isinstance(work, int) else _address(work, "work")
+
+
+def spmm_cache_bounds(cache: spmm_cache_t, layer: int, batch: spmm_batch_t, T: int, stream=None) -> None:
+    """Bounds of the keys of the pages that the batch's new tokens lie in."""
+    cache, batch = _struct(cache, spmm_cache_t), _struct(batch, spmm_batch_t)
+    _check(_functions().spmm_cache_bounds(cache, layer, batch, T, stream), "spmm_cache_bounds")
+
+
+def spmm_cache_score(cache: spmm_cache_t, layer: int, batch: spmm_batch_t, q, T: int, how: spmm_select_t, scores, lds: int, stream=None) -> None:
+    """scores [T][n_heads][lds] (float32) = upper bounds of the new tokens' products with the keys of each page."""
+    cache, batch, how = _struct(cache, spmm_cache_t), _struct(batch, spmm_batch_t), _struct(how, spmm_select_t)
+    _check(_functions().spmm_cache_score(cache, layer, batch, _tensor(q, "q", "bfloat16", need=T * how.q_heads * cache.head_dim), T, how,
+                                         _tensor(scores, "scores", "float32", need=T * cache.n_heads * lds), lds, stream), "spmm_cache_score")
+
+
+def spmm_cache_select(cache: spmm_cache_t, batch: spmm_batch_t, scores, T: int, lds: int, how: spmm_select_t, lists, stream=None) -> None:
+    """lists [T][n_heads][pages] (int32) = the pages that each new token reads, of scores [T][n_heads][lds]."""
+    cache, batch, how = _struct(cache, spmm_cache_t), _struct(batch, spmm_batch_t), _struct(how, spmm_select_t)
+    _check(_functions().spmm_cache_select(cache, batch, _tensor(scores, "scores", "float32", need=T * cache.n_heads * lds), T, lds, how,
+                                          _tensor(lists, "lists", "int32", need=T * cache.n_heads * how.pages), stream), "spmm_cache_select")
+
+
+def spmm_selected_work_bytes(cache: spmm_cache_t, T: int, how: spmm_attend_t, pages: int) -> int:
+    n = _i64()
+    cache, how = _struct(cache, spmm_cache_t), _struct(how, spmm_attend_t)
+    _check(_functions().spmm_selected_work_bytes(cache, T, how, pages, n), "spmm_selected_work_bytes")
+    return n.value
+
+
+def spmm_cache_attend_selected(cache: spmm_cache_t, layer: int, batch: spmm_batch_t, q, T: int, how: spmm_attend_t, lists, pages: int, out, ldo: int, work, stream=None) -> None:
+    """spmm_cache_attend over the pages of lists [T][n_heads][pages] (int32); work: a tensor of spmm_selected_work_bytes bytes."""
+    cache, batch, how = _struct(cache, spmm_cache_t), _struct(batch, spmm_batch_t), _struct(how, spmm_attend_t)
+    values = how.q_heads * cache.head_dim
+    need = 0 if work is None or isinstance(work, int) else _in_python["spmm_selected_work_bytes"](cache, T, how, pages)
+    _check(_functions().spmm_cache_attend_selected(
+        cache, layer, batch, _tensor(q, "q", "bfloat16", need=T * values), T, how, _tensor(lists, "lists", "int32", need=T * cache.n_heads * pages), pages,
+        _matrix(out, "out", _O_TYPES.get(how.out_type), values, T, ldo), ldo, _scratch(work, need), stream), "spmm_cache_attend_selected")
+
+
+def spmm_weigh_work_bytes(cache: spmm_cache_t, batch: spmm_batch_t, T: int, how: spmm_weigh_t) -> int:
+    n = _i64()
+    cache, batch, how = _struct(cache, spmm_cache_t), _struct(batch, spmm_batch_t), _struct(how, spmm_weigh_t)
+    _check(_functions().spmm_weigh_work_bytes(cache, batch, T, how, n), "spmm_weigh_work_bytes")
+    return n.value
+
+
+def spmm_cache_weigh(cache: spmm_cache_t, layer: int, batch: spmm_batch_t, q, T: int, how: spmm_weigh_t, work, stream=None) -> None:
+    """The new tokens' attention added to the cache's weights; work: a tensor of spmm_weigh_work_bytes bytes."""
+    cache, batch, how = _struct(cache, spmm_cache_t), _struct(batch, spmm_batch_t), _struct(how, spmm_weigh_t)
+    need = 0 if work is None or isinstance(work, int) else _in_python["spmm_weigh_work_bytes"](cache, batch, T, how)
+    _check(_functions().spmm_cache_weigh(cache, layer, batch, _tensor(q, "q", "bfloat16", need=T * how.q_heads * cache.head_dim), T, how,
+                                         _scratch(work, need), stream), "spmm_cache_weigh")
+
+
+def spmm_cache_evict(cache: spmm_cache_t, table, kv_len, keep, how: spmm_evict_t, table_to, kv_len_out, kept, stream=None) -> None:
+    """What stays of each row of table [rows, width] goes to the front of the row of table_to (which may be table); int32 tensors kv_len, keep,
+    kv_len_out [rows], kept [layers, rows, n_heads, how.most]."""
+    cache, how = _struct(cache, spmm_cache_t), _struct(how, spmm_evict_t)
+    rows, width = table.shape
+    i = "int32"
+    _check(_functions().spmm_cache_evict(
+        cache, _tensor(table, "table", i), width, _tensor(kv_len, "kv_len", i, (rows,)), rows, _tensor(keep, "keep", i, (rows,)), how,
+        _tensor(table_to, "table_to", i, (rows, width)), _tensor(kv_len_out, "kv_len_out", i, (rows,)),
+        _tensor(kept, "kept", i, need=cache.n_layers * rows * cache.n_heads * how.most), stream), "spmm_cache_evict")
+
+
 _FAST = ("make_cache", "make_batch", "make_append", "make_attend", "spmm_cache_append", "spmm_cache_attend", "spmm_attend_work_bytes", "spmm_cache_fork",
-         "spmm_cache_compact", "spmm_cache_work_bytes")
+         "spmm_cache_compact", "spmm_cache_work_bytes", "make_select", "make_weigh", "make_evict", "spmm_cache_bounds", "spmm_cache_score", "spmm_cache_select",
+         "spmm_selected_work_bytes", "spmm_cache_attend_selected", "spmm_weigh_work_bytes", "spmm_cache_weigh", "spmm_cache_evict")
 NATIVE_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "_native_cache.so")
 _in_python = {n: globals()[n] for n in _FAST}       # (the tests of the checks call these too)
 

@@ -17,6 +17,8 @@ constexpr int HEAD_DIM_STEP = 16;
 struct Pool {
     void *k, *v;
     float *k_scale, *v_scale;
+    __bf16* bounds;
+    float* weight;
     int32_t n_pages, n_heads, head_dim, page_shift;
 };
 
@@ -49,10 +51,12 @@ struct AttendArgs {
     float scale_log2, out_inv;      // scale * log2(e); 1 / out_scale
 };
 
+constexpr int PARTS = 6;
+
 // pages of all layers that are copied: src[i] -> dst[i], i < *count
 struct CopyArgs {
-    uint4* parts[4];                // keys, values and their scales; nullptr where there are none
-    int64_t part_pages[4];          // 16-byte units of a page in that part
+    uint4* parts[PARTS];            // keys, values and their scales, bounds, weights; nullptr where there are none
+    int64_t part_pages[PARTS];      // 16-byte units of a page in that part
     const int32_t *src, *dst, *count;
     int64_t n_layers;
     int32_t n_pages, most;          // most: bound of *count (and the number where count is nullptr)
@@ -74,6 +78,51 @@ struct CompactArgs {
     int32_t n_pages;
 };
 
+struct BoundsArgs {
+    Pool pool;
+    Batch batch;
+};
+
+struct ScoreArgs {
+    Pool pool;
+    Batch batch;
+    const __bf16* q;
+    float* scores;
+    int64_t lds;
+    int32_t T, group, causal, window;
+};
+
+struct SelectArgs {
+    Batch batch;
+    const float* scores;
+    int32_t* lists;
+    int64_t lds;
+    int32_t T, n_heads, page_shift, pages, first, last, causal, window;
+};
+
+struct SelectedArgs {
+    AttendArgs attend;
+    const int32_t* lists;
+    int32_t pages, parts;           // of a list; workgroups that share one
+};
+
+struct WeighArgs {
+    Pool pool;
+    Batch batch;
+    const __bf16* q;
+    float* work;
+    int32_t T, group, max_new, causal, window, parts;
+    float scale_log2, decay;
+};
+
+struct EvictArgs {
+    Pool pool;                      // of the first layer
+    const int32_t *table, *kv_len, *keep, *table_to;
+    int32_t *kv_len_out, *kept;
+    int64_t ld_table, most, layer_slots;        // layer_slots: tokens of a layer's pages, times heads
+    int32_t n_rows, n_layers, first, recent;
+};
+
 // launches; a HIP status
 int launch_append(const AppendArgs& a, spmm_out_t x_type, spmm_cache_type_t type, void* stream);
 int launch_attend(const AttendArgs& a, spmm_cache_type_t type, void* stream);
@@ -83,6 +132,14 @@ int launch_attend_many(const AttendArgs& a, spmm_cache_type_t type, void* stream
 int64_t many_work_bytes(spmm_cache_type_t type, int64_t n_seqs, int n_heads, int dim, int64_t cols);
 int64_t attend_work_bytes(spmm_cache_type_t type, int64_t n_seqs, int32_t n_heads, int32_t group, int32_t head_dim, int64_t max_new);
 int launch_copy(const CopyArgs& a, void* stream);
+int launch_bounds(const BoundsArgs& a, spmm_cache_type_t type, int64_t T, void* stream);
+int launch_score(const ScoreArgs& a, void* stream);
+int launch_select(const SelectArgs& a, void* stream);
+int64_t selected_work_bytes(spmm_cache_type_t type, int page_tokens, int64_t T, int n_heads, int group, int dim, int64_t pages);
+int launch_attend_selected(const SelectedArgs& a, spmm_cache_type_t type, void* stream);
+int64_t weigh_work_bytes(int page_tokens, int64_t n_seqs, int64_t ld_table, int n_heads, int64_t cols);
+int launch_weigh(const WeighArgs& a, spmm_cache_type_t type, void* stream);
+int launch_evict(const EvictArgs& a, spmm_cache_type_t type, void* stream);
 int launch_fork(const ForkArgs& a, const CopyArgs& c, void* stream);
 int launch_compact(const CompactArgs& a, const CopyArgs& c, void* stream);
 
@@ -123,6 +180,22 @@ __host__ __device__ __forceinline__ int tokens_of(const Batch& s, const int b, c
     const int64_t most = s.ld_table << page_shift;
     const int n = s.kv_len[b];
     return n < 0 ? 0 : (int64_t)n < most ? n : (int)most;
+}
+
+// The tokens that a column sees: from .. to of its sequence's row (none: from > to).
+struct Span {
+    int from, to;
+};
+__host__ __device__ __forceinline__ Span span_of(const Batch& s, const int b, const int t, const int page_shift, const int causal, const int window)
+{
+    const int len = tokens_of(s, b, page_shift);
+    const int64_t at = (int64_t)s.kv_len[b] - ((int64_t)s.q_start[b + 1] - t);
+    if (at < 0 || len == 0) return Span{0, -1};
+    Span r;
+    r.to = causal && at < len ? (int)at : len - 1;
+    const int64_t from = window ? at + 1 - window : 0;
+    r.from = from <= 0 ? 0 : from < len ? (int)from : len;
+    return r;
 }
 
 // A page number that lies in the pool, whatever the table holds.

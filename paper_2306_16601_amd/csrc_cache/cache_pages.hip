@@ -226,9 +226,9 @@ __global__ __launch_bounds__(THREADS) void cache_compact(const CompactArgs a)
 __global__ __launch_bounds__(COPY_THREADS) void cache_copy_pages(const CopyArgs a)
 {
     const int64_t count = a.count ? min(*a.count, a.most) : a.most;
-    uint32_t pieces[4], sum = 0;
+    uint32_t pieces[PARTS], sum = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sum += pieces[i] = a.parts[i] ? (uint32_t)((a.part_pages[i] + PIECE - 1) / PIECE) : 0;
+    for (int i = 0; i < PARTS; ++i) sum += pieces[i] = a.parts[i] ? (uint32_t)((a.part_pages[i] + PIECE - 1) / PIECE) : 0;
     const int64_t all = count * a.n_layers * sum;
     for (int64_t w = blockIdx.x; w < all; w += gridDim.x) {
         // (page, layer, piece): in 32 bits where they suffice
@@ -248,7 +248,7 @@ __global__ __launch_bounds__(COPY_THREADS) void cache_copy_pages(const CopyArgs 
         int64_t units = a.part_pages[0];
         u32x4* part = (u32x4*)a.parts[0];
 #pragma unroll
-        for (int i = 0; i < 3; ++i)
+        for (int i = 0; i < PARTS - 1; ++i)
             if (part == (u32x4*)a.parts[i] && piece >= pieces[i]) {
                 piece -= pieces[i];
                 part = (u32x4*)a.parts[i + 1];
@@ -273,7 +273,7 @@ __global__ __launch_bounds__(COPY_THREADS) void cache_copy_pages(const CopyArgs 
 int launch_copy(const CopyArgs& a, void* stream)
 {
     int64_t pieces = 0;
-    for (int i = 0; i < 4; ++i) pieces += a.parts[i] ? (a.part_pages[i] + PIECE - 1) / PIECE : 0;
+    for (int i = 0; i < PARTS; ++i) pieces += a.parts[i] ? (a.part_pages[i] + PIECE - 1) / PIECE : 0;
     const int64_t all = a.most * a.n_layers * pieces;
     return launch(cache_copy_pages, dim3((unsigned)(all < COPY_GRID ? all : COPY_GRID)), dim3(COPY_THREADS), a, stream);
 }

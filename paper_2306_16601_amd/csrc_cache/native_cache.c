@@ -14,8 +14,9 @@
 
 #include "spmm_cache.h"
 
-enum { CACHE, BATCH, APPEND, ATTEND, KINDS };
-static const Py_ssize_t sizes[KINDS] = {sizeof(spmm_cache_t), sizeof(spmm_batch_t), sizeof(spmm_append_t), sizeof(spmm_attend_t)};
+enum { CACHE, BATCH, APPEND, ATTEND, SELECT, WEIGH, EVICT, KINDS };
+static const Py_ssize_t sizes[KINDS] = {sizeof(spmm_cache_t), sizeof(spmm_batch_t), sizeof(spmm_append_t), sizeof(spmm_attend_t),
+                                        sizeof(spmm_select_t), sizeof(spmm_weigh_t), sizeof(spmm_evict_t)};
 
 typedef struct {
     PyObject_HEAD
@@ -26,6 +27,9 @@ typedef struct {
         spmm_batch_t batch;
         spmm_append_t append;
         spmm_attend_t attend;
+        spmm_select_t select;
+        spmm_weigh_t weigh;
+        spmm_evict_t evict;
     } u;
 } Record;
 
@@ -53,9 +57,11 @@ static PyTypeObject RecordType = {
     .tp_as_buffer = &record_as_buffer, .tp_getset = record_attributes, .tp_flags = Py_TPFLAGS_DEFAULT,
     .tp_doc = "A cache, a batch or a call of include/spmm_cache.h, described"};
 
-enum { F_APPEND, F_ATTEND, F_ATTEND_WORK, F_FORK, F_COMPACT, F_CACHE_WORK, FUNCTIONS };
+enum { F_APPEND, F_ATTEND, F_ATTEND_WORK, F_FORK, F_COMPACT, F_CACHE_WORK, F_BOUNDS, F_SCORE, F_SELECT, F_SELECTED_WORK, F_SELECTED, F_WEIGH_WORK, F_WEIGH, F_EVICT,
+       FUNCTIONS };
 static void *functions[FUNCTIONS];
-enum { S_MAKE_CACHE, S_MAKE_BATCH, S_MAKE_APPEND, S_MAKE_ATTEND, S_APPEND, S_ATTEND, S_ATTEND_WORK, S_FORK, S_COMPACT, S_CACHE_WORK, SLOW };
+enum { S_MAKE_CACHE, S_MAKE_BATCH, S_MAKE_APPEND, S_MAKE_ATTEND, S_APPEND, S_ATTEND, S_ATTEND_WORK, S_FORK, S_COMPACT, S_CACHE_WORK,
+       S_MAKE_SELECT, S_MAKE_WEIGH, S_MAKE_EVICT, S_BOUNDS, S_SCORE, S_SELECT, S_SELECTED_WORK, S_SELECTED, S_WEIGH_WORK, S_WEIGH, S_EVICT, SLOW };
 static PyObject *slow[SLOW], *py_check;
 static PyObject *s_data_ptr, *s_nbytes, *s_is_contiguous, *s_dtype, *s_is_cuda, *s_shape;
 
@@ -195,13 +201,17 @@ static PyObject *make_cache(PyObject *self, PyObject *const *args, Py_ssize_t na
 {
     int64_t ks[5], vs[5], ss[4];
     (void)self;
-    if (kwnames || nargs < 2 || nargs > 4 || !shape_of(args[0], 5, ks) || !shape_of(args[1], 5, vs)) return instead(S_MAKE_CACHE, args, nargs, kwnames);
+    if (kwnames || nargs < 2 || nargs > 6 || !shape_of(args[0], 5, ks) || !shape_of(args[1], 5, vs)) return instead(S_MAKE_CACHE, args, nargs, kwnames);
     const int type = type_of(args[0]);
     PyObject *const scale[2] = {nargs > 2 ? args[2] : Py_None, nargs > 3 ? args[3] : Py_None};
     int ok = (type == BF16 || type == S8) && ks[0] == vs[0] && ks[1] == vs[1] && ks[2] == vs[2] && ks[3] == vs[4] && ks[4] == vs[3] &&
              ks[0] <= INT32_MAX && ks[2] <= INT32_MAX && ks[3] <= INT32_MAX && ks[4] <= INT32_MAX;
-    void *p[4] = {0};
+    void *p[6] = {0};
     ok = ok && operand(args[0], type, 0, p) && operand(args[1], type, 0, p + 1);
+    if (ok && nargs > 4 && args[4] != Py_None)
+        ok = shape_of(args[4], 5, vs) && vs[0] == ks[0] && vs[1] == ks[1] && vs[2] == ks[2] && vs[3] == 2 && vs[4] == ks[4] && operand(args[4], BF16, 0, p + 4);
+    if (ok && nargs > 5 && args[5] != Py_None)
+        ok = shape_of(args[5], 4, ss) && ss[0] == ks[0] && ss[1] == ks[1] && ss[2] == ks[2] && ss[3] == ks[3] && operand(args[5], F32, 0, p + 5);
     for (int i = 0; i < 2 && ok; ++i) {
         if (type == S8)
             ok = scale[i] != Py_None && shape_of(scale[i], 4, ss) && ss[0] == ks[0] && ss[1] == ks[1] && ss[2] == ks[2] && ss[3] == ks[3] &&
@@ -212,7 +222,7 @@ static PyObject *make_cache(PyObject *self, PyObject *const *args, Py_ssize_t na
     if (!ok) return instead(S_MAKE_CACHE, args, nargs, kwnames);
     Record *r = record(CACHE, args, nargs);
     if (r) r->u.cache = (spmm_cache_t){p[0], p[1], p[2], p[3], type == S8 ? SPMM_CACHE_S8 : SPMM_CACHE_BF16, (int32_t)ks[0], (int32_t)ks[2],
-                                       (int32_t)ks[4], (int32_t)ks[3], ks[1]};
+                                       (int32_t)ks[4], (int32_t)ks[3], ks[1], p[4], p[5]};
     return (PyObject *)r;
 }
 
@@ -434,7 +444,254 @@ static PyObject *cache_compact(PyObject *self, PyObject *const *args, Py_ssize_t
     return ok ? done(st, "spmm_cache_compact") : instead(S_COMPACT, args, nargs, kwnames);
 }
 
-/* hooks(_check, the ten slow functions) */
+static int narrow(PyObject *v, int64_t *out) { return number(v, out) && *out >= INT32_MIN && *out <= INT32_MAX; }
+static int narrow_all(PyObject *const *args, int n, int64_t *out)
+{
+    for (int i = 0; i < n; ++i)
+        if (!narrow(args[i], out + i)) return 0;
+    return 1;
+}
+static int stream_of(PyObject *const *args, Py_ssize_t nargs, Py_ssize_t at, int64_t *out)
+{
+    *out = 0;
+    return nargs <= at || args[at] == Py_None || number(args[at], out);
+}
+
+/* make_select(q_heads, pages, first, last, causal, window): all six */
+static PyObject *make_select(PyObject *self, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    int64_t v[6];
+    (void)self;
+    if (kwnames || nargs != 6 || !narrow_all(args, 6, v)) return instead(S_MAKE_SELECT, args, nargs, kwnames);
+    Record *r = record(SELECT, args, nargs);
+    if (r) r->u.select = (spmm_select_t){(int32_t)v[0], (int32_t)v[1], (int32_t)v[2], (int32_t)v[3], v[4] != 0, (int32_t)v[5]};
+    return (PyObject *)r;
+}
+
+/* make_weigh(q_heads, max_new, scale, causal, window, decay): all six */
+static PyObject *make_weigh(PyObject *self, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    int64_t heads, most, causal, window;
+    float scale, decay;
+    (void)self;
+    if (kwnames || nargs != 6 || !narrow(args[0], &heads) || !number(args[1], &most) || !real(args[2], &scale) || !number(args[3], &causal) || !narrow(args[4], &window) ||
+        !real(args[5], &decay))
+        return instead(S_MAKE_WEIGH, args, nargs, kwnames);
+    Record *r = record(WEIGH, args, nargs);
+    if (r) r->u.weigh = (spmm_weigh_t){(int32_t)heads, most, scale, causal != 0, (int32_t)window, decay};
+    return (PyObject *)r;
+}
+
+/* make_evict(first, recent, most) */
+static PyObject *make_evict(PyObject *self, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    int64_t v[2], most;
+    (void)self;
+    if (kwnames || nargs != 3 || !narrow_all(args, 2, v) || !number(args[2], &most)) return instead(S_MAKE_EVICT, args, nargs, kwnames);
+    Record *r = record(EVICT, args, nargs);
+    if (r) r->u.evict = (spmm_evict_t){(int32_t)v[0], (int32_t)v[1], most};
+    return (PyObject *)r;
+}
+
+/* spmm_cache_bounds(cache, layer, batch, T, stream) */
+static PyObject *cache_bounds(PyObject *self, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    Py_buffer cb = {0}, bb = {0};
+    int64_t layer, T, stream;
+    (void)self;
+    if (kwnames || nargs < 4 || nargs > 5 || !functions[F_BOUNDS] || !narrow(args[1], &layer) || !number(args[3], &T) || !stream_of(args, nargs, 4, &stream))
+        return instead(S_BOUNDS, args, nargs, kwnames);
+    const spmm_cache_t *const c = description(args[0], CACHE, &cb);
+    const spmm_batch_t *const b = c ? description(args[2], BATCH, &bb) : NULL;
+    int st = 0;
+    if (b) {
+        Py_BEGIN_ALLOW_THREADS
+        st = ((spmm_status_t (*)(const spmm_cache_t *, int32_t, const spmm_batch_t *, int64_t, void *))functions[F_BOUNDS])(c, (int32_t)layer, b, T, (void *)(uintptr_t)stream);
+        Py_END_ALLOW_THREADS
+    }
+    const int ok = b != NULL;
+    release(&cb);
+    release(&bb);
+    return ok ? done(st, "spmm_cache_bounds") : instead(S_BOUNDS, args, nargs, kwnames);
+}
+
+/* spmm_cache_score(cache, layer, batch, q, T, how, scores, lds, stream) */
+static PyObject *cache_score(PyObject *self, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    Py_buffer cb = {0}, bb = {0}, hb = {0};
+    int64_t layer, T, lds, stream;
+    void *q, *scores;
+    (void)self;
+    if (kwnames || nargs < 8 || nargs > 9 || !functions[F_SCORE] || !narrow(args[1], &layer) || !number(args[4], &T) || !number(args[7], &lds) || !stream_of(args, nargs, 8, &stream))
+        return instead(S_SCORE, args, nargs, kwnames);
+    const spmm_cache_t *const c = description(args[0], CACHE, &cb);
+    const spmm_batch_t *const b = c ? description(args[2], BATCH, &bb) : NULL;
+    const spmm_select_t *const a = b ? description(args[5], SELECT, &hb) : NULL;
+    const int ok = a && operand(args[3], BF16, covered(T, (int64_t)a->q_heads * c->head_dim, (int64_t)a->q_heads * c->head_dim, 2), &q) &&
+                   operand(args[6], F32, covered((__int128)T * c->n_heads, lds, lds, 4), &scores);
+    int st = 0;
+    if (ok) {
+        Py_BEGIN_ALLOW_THREADS
+        st = ((spmm_status_t (*)(const spmm_cache_t *, int32_t, const spmm_batch_t *, const void *, int64_t, const spmm_select_t *, void *, int64_t, void *))functions[F_SCORE])(
+            c, (int32_t)layer, b, q, T, a, scores, lds, (void *)(uintptr_t)stream);
+        Py_END_ALLOW_THREADS
+    }
+    release(&cb);
+    release(&bb);
+    release(&hb);
+    return ok ? done(st, "spmm_cache_score") : instead(S_SCORE, args, nargs, kwnames);
+}
+
+/* spmm_cache_select(cache, batch, scores, T, lds, how, lists, stream) */
+static PyObject *cache_select(PyObject *self, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    Py_buffer cb = {0}, bb = {0}, hb = {0};
+    int64_t T, lds, stream;
+    void *scores, *lists;
+    (void)self;
+    if (kwnames || nargs < 7 || nargs > 8 || !functions[F_SELECT] || !number(args[3], &T) || !number(args[4], &lds) || !stream_of(args, nargs, 7, &stream))
+        return instead(S_SELECT, args, nargs, kwnames);
+    const spmm_cache_t *const c = description(args[0], CACHE, &cb);
+    const spmm_batch_t *const b = c ? description(args[1], BATCH, &bb) : NULL;
+    const spmm_select_t *const a = b ? description(args[5], SELECT, &hb) : NULL;
+    const int ok = a && operand(args[2], F32, covered((__int128)T * c->n_heads, lds, lds, 4), &scores) &&
+                   operand(args[6], S32, covered((__int128)T * c->n_heads, a->pages, a->pages, 4), &lists);
+    int st = 0;
+    if (ok) {
+        Py_BEGIN_ALLOW_THREADS
+        st = ((spmm_status_t (*)(const spmm_cache_t *, const spmm_batch_t *, const void *, int64_t, int64_t, const spmm_select_t *, void *, void *))functions[F_SELECT])(
+            c, b, scores, T, lds, a, lists, (void *)(uintptr_t)stream);
+        Py_END_ALLOW_THREADS
+    }
+    release(&cb);
+    release(&bb);
+    release(&hb);
+    return ok ? done(st, "spmm_cache_select") : instead(S_SELECT, args, nargs, kwnames);
+}
+
+typedef spmm_status_t (*selected_work_fn)(const spmm_cache_t *, int64_t, const spmm_attend_t *, int64_t, int64_t *);
+
+/* spmm_selected_work_bytes(cache, T, how, pages) */
+static PyObject *selected_work(PyObject *self, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    Py_buffer cb = {0}, hb = {0};
+    int64_t T, pages, bytes = 0;
+    (void)self;
+    if (kwnames || nargs != 4 || !functions[F_SELECTED_WORK] || !number(args[1], &T) || !number(args[3], &pages)) return instead(S_SELECTED_WORK, args, nargs, kwnames);
+    const spmm_cache_t *const c = description(args[0], CACHE, &cb);
+    const spmm_attend_t *const a = c ? description(args[2], ATTEND, &hb) : NULL;
+    const int st = a ? (int)((selected_work_fn)functions[F_SELECTED_WORK])(c, T, a, pages, &bytes) : -1;
+    release(&cb);
+    release(&hb);
+    return st == SPMM_OK ? PyLong_FromLongLong(bytes) : instead(S_SELECTED_WORK, args, nargs, kwnames);
+}
+
+/* spmm_cache_attend_selected(cache, layer, batch, q, T, how, lists, pages, out, ldo, work, stream) */
+static PyObject *cache_selected(PyObject *self, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    Py_buffer cb = {0}, bb = {0}, hb = {0};
+    int64_t layer, T, pages, ldo, stream, need = 0;
+    void *q, *lists, *out, *work;
+    (void)self;
+    if (kwnames || nargs < 11 || nargs > 12 || !functions[F_SELECTED] || !narrow(args[1], &layer) || !number(args[4], &T) || !number(args[7], &pages) || !number(args[9], &ldo) ||
+        !stream_of(args, nargs, 11, &stream))
+        return instead(S_SELECTED, args, nargs, kwnames);
+    const spmm_cache_t *const c = description(args[0], CACHE, &cb);
+    const spmm_batch_t *const b = c ? description(args[2], BATCH, &bb) : NULL;
+    const spmm_attend_t *const a = b ? description(args[5], ATTEND, &hb) : NULL;
+    int ok = a != NULL;
+    if (ok) {
+        static const int of[] = {-1, F32, S8, U8, BF16};
+        const int known = a->out_type >= 1 && a->out_type <= 4;
+        const int64_t each = a->out_type == SPMM_OUT_F32 ? 4 : a->out_type == SPMM_OUT_BF16 ? 2 : 1, values = (int64_t)a->q_heads * c->head_dim;
+        ok = known && ((selected_work_fn)functions[F_SELECTED_WORK])(c, T, a, pages, &need) == SPMM_OK && operand(args[3], BF16, covered(T, values, values, 2), &q) &&
+             operand(args[6], S32, covered((__int128)T * c->n_heads, pages, pages, 4), &lists) && operand(args[8], of[known ? a->out_type : 0], covered(values, T, ldo, each), &out) &&
+             operand(args[10], -1, need, &work);
+    }
+    int st = 0;
+    if (ok) {
+        Py_BEGIN_ALLOW_THREADS
+        st = ((spmm_status_t (*)(const spmm_cache_t *, int32_t, const spmm_batch_t *, const void *, int64_t, const spmm_attend_t *, const void *, int64_t, void *, int64_t, void *,
+                                 void *))functions[F_SELECTED])(c, (int32_t)layer, b, q, T, a, lists, pages, out, ldo, work, (void *)(uintptr_t)stream);
+        Py_END_ALLOW_THREADS
+    }
+    release(&cb);
+    release(&bb);
+    release(&hb);
+    return ok ? done(st, "spmm_cache_attend_selected") : instead(S_SELECTED, args, nargs, kwnames);
+}
+
+typedef spmm_status_t (*weigh_work_fn)(const spmm_cache_t *, const spmm_batch_t *, int64_t, const spmm_weigh_t *, int64_t *);
+
+/* spmm_weigh_work_bytes(cache, batch, T, how) */
+static PyObject *weigh_work(PyObject *self, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    Py_buffer cb = {0}, bb = {0}, hb = {0};
+    int64_t T, bytes = 0;
+    (void)self;
+    if (kwnames || nargs != 4 || !functions[F_WEIGH_WORK] || !number(args[2], &T)) return instead(S_WEIGH_WORK, args, nargs, kwnames);
+    const spmm_cache_t *const c = description(args[0], CACHE, &cb);
+    const spmm_batch_t *const b = c ? description(args[1], BATCH, &bb) : NULL;
+    const spmm_weigh_t *const a = b ? description(args[3], WEIGH, &hb) : NULL;
+    const int st = a ? (int)((weigh_work_fn)functions[F_WEIGH_WORK])(c, b, T, a, &bytes) : -1;
+    release(&cb);
+    release(&bb);
+    release(&hb);
+    return st == SPMM_OK ? PyLong_FromLongLong(bytes) : instead(S_WEIGH_WORK, args, nargs, kwnames);
+}
+
+/* spmm_cache_weigh(cache, layer, batch, q, T, how, work, stream) */
+static PyObject *cache_weigh(PyObject *self, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    Py_buffer cb = {0}, bb = {0}, hb = {0};
+    int64_t layer, T, stream, need = 0;
+    void *q, *work;
+    (void)self;
+    if (kwnames || nargs < 7 || nargs > 8 || !functions[F_WEIGH] || !narrow(args[1], &layer) || !number(args[4], &T) || !stream_of(args, nargs, 7, &stream))
+        return instead(S_WEIGH, args, nargs, kwnames);
+    const spmm_cache_t *const c = description(args[0], CACHE, &cb);
+    const spmm_batch_t *const b = c ? description(args[2], BATCH, &bb) : NULL;
+    const spmm_weigh_t *const a = b ? description(args[5], WEIGH, &hb) : NULL;
+    const int ok = a && ((weigh_work_fn)functions[F_WEIGH_WORK])(c, b, T, a, &need) == SPMM_OK &&
+                   operand(args[3], BF16, covered(T, (int64_t)a->q_heads * c->head_dim, (int64_t)a->q_heads * c->head_dim, 2), &q) && operand(args[6], -1, need, &work);
+    int st = 0;
+    if (ok) {
+        Py_BEGIN_ALLOW_THREADS
+        st = ((spmm_status_t (*)(const spmm_cache_t *, int32_t, const spmm_batch_t *, const void *, int64_t, const spmm_weigh_t *, void *, void *))functions[F_WEIGH])(
+            c, (int32_t)layer, b, q, T, a, work, (void *)(uintptr_t)stream);
+        Py_END_ALLOW_THREADS
+    }
+    release(&cb);
+    release(&bb);
+    release(&hb);
+    return ok ? done(st, "spmm_cache_weigh") : instead(S_WEIGH, args, nargs, kwnames);
+}
+
+/* spmm_cache_evict(cache, table, kv_len, keep, how, table_to, kv_len_out, kept, stream) */
+static PyObject *cache_evict(PyObject *self, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    Py_buffer cb = {0}, hb = {0};
+    int64_t in[2], to[2], stream;
+    void *p[6];
+    (void)self;
+    if (kwnames || nargs < 8 || nargs > 9 || !functions[F_EVICT] || !stream_of(args, nargs, 8, &stream)) return instead(S_EVICT, args, nargs, kwnames);
+    const spmm_cache_t *const c = description(args[0], CACHE, &cb);
+    const spmm_evict_t *const a = c ? description(args[4], EVICT, &hb) : NULL;
+    const int ok = a && table_of(args[1], in, p) && table_of(args[5], to, p + 3) && in[0] == to[0] && in[1] == to[1] && row_of(args[2], in[0], p + 1) && row_of(args[3], in[0], p + 2) &&
+                   row_of(args[6], in[0], p + 4) && a->most >= 0 && operand(args[7], S32, covered((__int128)c->n_layers * c->n_heads * in[0], a->most, a->most, 4), p + 5);
+    int st = 0;
+    if (ok) {
+        Py_BEGIN_ALLOW_THREADS
+        st = ((spmm_status_t (*)(const spmm_cache_t *, const void *, int64_t, const void *, int64_t, const void *, const spmm_evict_t *, const void *, void *, void *, void *))functions[F_EVICT])(
+            c, p[0], in[1], p[1], in[0], p[2], a, p[3], p[4], p[5], (void *)(uintptr_t)stream);
+        Py_END_ALLOW_THREADS
+    }
+    release(&cb);
+    release(&hb);
+    return ok ? done(st, "spmm_cache_evict") : instead(S_EVICT, args, nargs, kwnames);
+}
+
+/* hooks(_check, the slow functions) */
 static PyObject *native_hooks(PyObject *self, PyObject *args)
 {
     (void)self;
@@ -444,13 +701,16 @@ static PyObject *native_hooks(PyObject *self, PyObject *args)
     Py_RETURN_NONE;
 }
 
-/* bind(addresses of the six functions) */
+/* bind(addresses of the functions) */
 static PyObject *native_bind(PyObject *self, PyObject *args)
 {
-    unsigned long long p[FUNCTIONS];
     (void)self;
-    if (!PyArg_ParseTuple(args, "KKKKKK", p, p + 1, p + 2, p + 3, p + 4, p + 5)) return NULL;
-    for (int i = 0; i < FUNCTIONS; ++i) functions[i] = (void *)(uintptr_t)p[i];
+    if (PyTuple_GET_SIZE(args) != FUNCTIONS) return PyErr_Format(PyExc_TypeError, "bind() takes %d addresses", FUNCTIONS);
+    for (int i = 0; i < FUNCTIONS; ++i) {
+        const unsigned long long p = PyLong_AsUnsignedLongLong(PyTuple_GET_ITEM(args, i));
+        if (PyErr_Occurred()) return NULL;
+        functions[i] = (void *)(uintptr_t)p;
+    }
     Py_RETURN_NONE;
 }
 
@@ -459,6 +719,10 @@ static PyMethodDef methods[] = {
     FAST("make_cache", make_cache), FAST("make_batch", make_batch), FAST("make_append", make_append), FAST("make_attend", make_attend),
     FAST("spmm_cache_append", cache_append), FAST("spmm_cache_attend", cache_attend), FAST("spmm_attend_work_bytes", attend_work),
     FAST("spmm_cache_fork", cache_fork), FAST("spmm_cache_compact", cache_compact), FAST("spmm_cache_work_bytes", cache_work),
+    FAST("make_select", make_select), FAST("make_weigh", make_weigh), FAST("make_evict", make_evict), FAST("spmm_cache_bounds", cache_bounds),
+    FAST("spmm_cache_score", cache_score), FAST("spmm_cache_select", cache_select), FAST("spmm_selected_work_bytes", selected_work),
+    FAST("spmm_cache_attend_selected", cache_selected), FAST("spmm_weigh_work_bytes", weigh_work), FAST("spmm_cache_weigh", cache_weigh),
+    FAST("spmm_cache_evict", cache_evict),
     {"hooks", native_hooks, METH_VARARGS, NULL}, {"bind", native_bind, METH_VARARGS, NULL}, {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native_cache", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
