@@ -18,9 +18,9 @@ struct Row {
 };
 
 // false: a column of no sequence
-__device__ __forceinline__ bool row_of(const SelectArgs& a, const int64_t i, Row* const r)
+__device__ __forceinline__ bool row_of(const SelectArgs& a, const int i, Row* const r)      // (there are at most 2^22)
 {
-    const int t = (int)(i / a.n_heads), b = sequence_of(a.batch, t);
+    const int t = i / a.n_heads, b = sequence_of(a.batch, t);
     if (b < 0) return false;
     const Span s = span_of(a.batch, b, t, a.page_shift, a.causal, a.window);
     r->first = s.from <= s.to ? s.from >> a.page_shift : 0;
@@ -29,8 +29,8 @@ __device__ __forceinline__ bool row_of(const SelectArgs& a, const int64_t i, Row
     r->from = r->first + a.first;
     r->n = r->pages - a.first - a.last;
     r->need = a.pages - a.first - a.last;
-    r->scores = a.scores + i * a.lds;
-    r->list = a.lists + i * a.pages;
+    r->scores = a.scores + (int64_t)i * a.lds;
+    r->list = a.lists + (int64_t)i * a.pages;
     return true;
 }
 
@@ -52,10 +52,10 @@ __device__ __forceinline__ void ends_of(const SelectArgs& a, const Row& r, const
 template <int REGS>
 __global__ __launch_bounds__(64 * SMALL_WAVES) void cache_select(const SelectArgs a)
 {
-    const int lane = threadIdx.x % 64;
-    const int64_t i = (int64_t)blockIdx.x * SMALL_WAVES + threadIdx.x / 64;
+    __shared__ Bins<1> bins[SMALL_WAVES];
+    const int lane = threadIdx.x % 64, i = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * SMALL_WAVES + threadIdx.x / 64));
     Row r;
-    if (i >= (int64_t)a.T * a.n_heads || !row_of(a, i, &r) || all_of(a, r, lane, 64)) return;
+    if (i >= a.T * a.n_heads || !row_of(a, i, &r) || all_of(a, r, lane, 64)) return;
     ends_of(a, r, lane, 64);
     if (r.need == 0) return;
     uint32_t v[REGS];
@@ -64,16 +64,16 @@ __global__ __launch_bounds__(64 * SMALL_WAVES) void cache_select(const SelectArg
         const int j = k * 64 + lane;
         v[k] = j < r.n ? rank_of(r.scores[r.from + j]) : 0;
     }
-    const Border border = border_of<1>(v, r.need, (int*)nullptr);
-    put_chosen<1>(v, border, (int (*)[2])nullptr, [&](const int j, const int place) { r.list[r.head + place] = r.from + j; });
+    choose<1>(v, r.need, bins[threadIdx.x / 64], (int (*)[2])nullptr, [&](const int j, const int place) { r.list[r.head + place] = r.from + j; });
 }
 
 template <int WAVES, int REGS>
 __global__ __launch_bounds__(64 * WAVES) void cache_select_long(const SelectArgs a)
 {
-    __shared__ int counts[2 * WAVES], totals[(REGS ? REGS : 1) * WAVES][2];
+    __shared__ Bins<WAVES> bins;
+    __shared__ int totals[(REGS ? REGS : 1) * WAVES][2];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    for (int64_t i = blockIdx.x; i < (int64_t)a.T * a.n_heads; i += gridDim.x) {
+    for (int i = blockIdx.x; i < a.T * a.n_heads; i += gridDim.x) {
         Row r;
         if (!row_of(a, i, &r) || all_of(a, r, threadIdx.x, 64 * WAVES)) continue;
         ends_of(a, r, threadIdx.x, 64 * WAVES);
@@ -87,10 +87,9 @@ __global__ __launch_bounds__(64 * WAVES) void cache_select_long(const SelectArgs
                 const int j = (k * WAVES + wave) * 64 + lane;
                 v[k] = j < r.n ? rank_of(r.scores[r.from + j]) : 0;
             }
-            const Border border = border_of<WAVES>(v, r.need, counts);
-            put_chosen<WAVES>(v, border, totals, put);
+            choose<WAVES>(v, r.need, bins, totals, put);
         } else {
-            choose_long<WAVES>(r.n, r.need, counts, totals, [&](const int j) { return rank_of(r.scores[r.from + j]); }, put);
+            choose_long<WAVES>(r.n, r.need, bins, totals, [&](const int j) { return rank_of(r.scores[r.from + j]); }, put);
         }
     }
 }

@@ -2,10 +2,12 @@
 //
 // The softmax of a column (a new token's query head) needs the largest of its scores and the sum of their powers before any key can be
 // given its share, so there are two passes over the keys.  cache_weigh_stats: a workgroup has columns in its registers and a part of
-// the keys goes by, with a running maximum and sum; cache_weigh_join puts the parts' statistics together; cache_weigh_add: a wave has keys in its
-// registers, the columns go by, and each key's shares are summed up, first in a lane, then over the lanes of its row: every weight is
-// one wave's, so that there are no atomics, and sums have one order.  Products are exact: queries are bfloat16, and so are codes of 8 bits
-// once they are widened (integers up to 256 have 8 bits).
+// the keys goes by, with a running maximum and sum.  Where a key/value head has up to 16 columns (single tokens, drafts) that pass reads the
+// cache once and memory bounds it; it keeps the scores, four bytes where the key has 2 head_dim, and cache_weigh_kept makes shares of them.  With
+// more columns the scores would be more than the keys are: cache_weigh_join puts the parts' statistics together, and in
+// cache_weigh_add a wave has keys in its registers, the columns go by, and each key's shares are summed up, first in a lane, then over the lanes of
+// its row.  Every weight is one thread's, so that there are no atomics, and sums have one order.  Products are exact: queries are bfloat16, and so are
+// codes of 8 bits once they are widened (integers up to 256 have 8 bits).
 #include "cache_attend.h"
 
 namespace spmm_cache {
@@ -13,8 +15,11 @@ namespace spmm_cache {
 constexpr int WAVES = 4;
 constexpr int THREADS = 64 * WAVES;
 constexpr int COLS = 16;            // columns of a tile
-constexpr int KEYS = 32;            // of a wave's step
-constexpr int STEP = KEYS * WAVES;
+constexpr int MANY = 4;             // tiles of columns of a workgroup of cache_weigh_stats, where there are many
+constexpr int NEAR = 2, FAR = 4;    // tiles of 16 keys of a wave's step, in cache_weigh_stats and cache_weigh_add
+constexpr int STEP = 16 * NEAR * WAVES;
+constexpr int LISTED = 512;         // columns whose numbers are in LDS at a time
+constexpr double KEPT = 1 << 30;    // most bytes of scores that are kept
 
 // A sequence's columns that count, and its tokens.
 struct Counted {
@@ -47,11 +52,19 @@ __device__ __forceinline__ void join(float& m, float& l, const float mo, const f
     m = mn;
 }
 
-// statistics: of column (t, query head) and part; behind them, of columns
+// scratch: statistics of column (t, query head) and part; behind them scores that are kept, or statistics of columns
 __device__ __forceinline__ float* stat_of(const WeighArgs& a, const int64_t column, const int part) { return a.work + (column * a.parts + part) * 2; }
-__device__ __forceinline__ float* joined_of(const WeighArgs& a, const int64_t column)
+__device__ __forceinline__ float* behind_stats(const WeighArgs& a) { return a.work + ((int64_t)a.T * a.group * a.pool.n_heads * a.parts + 1) / 2 * 4; }
+__device__ __forceinline__ float* joined_of(const WeighArgs& a, const int64_t column) { return behind_stats(a) + column * 2; }
+__host__ __device__ __forceinline__ int64_t kept_keys(const int64_t keys) { return (keys + STEP - 1) / STEP * STEP; }
+// scores of column c of a sequence's head, all keys
+__device__ __forceinline__ float* kept_of(const WeighArgs& a, const int b, const int h, const int c)
 {
-    return a.work + ((int64_t)a.T * a.group * a.pool.n_heads * a.parts + column) * 2;
+    return behind_stats(a) + (((int64_t)b * a.pool.n_heads + h) * (a.max_new * a.group) + c) * kept_keys(a.batch.ld_table << a.pool.page_shift);
+}
+__device__ __forceinline__ int64_t column_of(const WeighArgs& a, const Counted& s, const int h, const int c)
+{
+    return ((int64_t)(s.first + c / a.group) * a.pool.n_heads + h) * a.group + c % a.group;
 }
 
 // Operands of 32 dims of a product: queries' and keys'.  bfloat16: step s holds dims 32 s + 8 g ..; 8 bits: dims 64 (s / 2) + 16 g + 8 (s % 2) ..
@@ -80,62 +93,67 @@ __device__ __forceinline__ bf16x8 codes(const uint32_t lo, const uint32_t hi)
     return v;
 }
 
-// Keys k0 + 16 t + row of tile t, in registers; their scales (8 bits) for the rows that the lane has scores of.
-template <int KS, spmm_cache_type_t TYPE>
+// Keys k0 + 16 t + row of tile t < N, as they lie in the cache; their scales (8 bits) for the rows that the lane has scores of.
+template <int KS, spmm_cache_type_t TYPE, int N>
 struct Keys {
-    bf16x8 v[2][KS];
-    float scale[2][4];
+    static constexpr bool S8 = TYPE == SPMM_CACHE_S8;
+    static constexpr int PARTS = S8 ? (KS + 1) / 2 : KS;       // of 16 bytes
+    u32x4 v[N][PARTS];
+    f32x4 scale[S8 ? N : 1];
     __device__ __forceinline__ void load(const WeighArgs& a, const int32_t* const table, const int h, const int k0, const int last)
     {
         const int lane = threadIdx.x % 64, row = lane % 16, g = lane / 16, shift = a.pool.page_shift, inside = (1 << shift) - 1, D = a.pool.head_dim;
-        const auto slot_of = [&](const int at) {
-            const int key = min(at, last);
-            return (((int64_t)page_in_pool(table[key >> shift], a.pool.n_pages) * a.pool.n_heads + h) << shift) + (key & inside);
-        };
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const int64_t slot = slot_of(k0 + 16 * t + row);
-            if constexpr (TYPE == SPMM_CACHE_S8) {
-                const int8_t* const src = (const int8_t*)a.pool.k + slot * D;
+        for (int t = 0; t < N; ++t) {
+            // (16 tokens that start at a multiple of 16 are in one page; those beyond the last lie in its page too)
+            const int at = min(k0 + 16 * t, last) & ~15;
+            const int64_t slot = (((int64_t)page_in_pool(table[at >> shift], a.pool.n_pages) * a.pool.n_heads + h) << shift) + (at & inside);
+            const char* const src = (const char*)a.pool.k + (slot + row) * D * (S8 ? 1 : 2) + 16 * g;
 #pragma unroll
-                for (int s = 0; s < KS; s += 2) {
-                    const int d = dim_of<TYPE>(s, g);
-                    const u32x4 x = d < D ? *(const u32x4*)(src + d) : u32x4{0, 0, 0, 0};
-                    v[t][s] = codes(x[0], x[1]);
-                    v[t][s + 1] = codes(x[2], x[3]);
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float f = a.pool.k_scale[slot_of(k0 + 16 * t + 4 * g + i)];
-                    scale[t][i] = fabsf(f) <= 3.4028235e38f ? f : __builtin_nanf("");
-                }
-            } else {
-                const __bf16* const src = (const __bf16*)a.pool.k + slot * D;
-#pragma unroll
-                for (int s = 0; s < KS; ++s) {
-                    const int d = dim_of<TYPE>(s, g);
-                    v[t][s] = d < D ? *(const bf16x8*)(src + d) : bf16x8{};
-                }
-            }
+            for (int s = 0; s < PARTS; ++s) v[t][s] = 64 * s + 16 * g < D * (S8 ? 1 : 2) ? *(const u32x4*)(src + 64 * s) : u32x4{0, 0, 0, 0};
+            if constexpr (S8) scale[t] = *(const f32x4*)(a.pool.k_scale + slot + 4 * g);
         }
     }
-    // scores of the lane's column: of key k0 + 16 t + 4 g + i
-    __device__ __forceinline__ void scores(const bf16x8 (&q)[KS], float (&x)[2][4]) const
+    // what is not finite among the scales makes scores NaN
+    __device__ __forceinline__ void ready()
     {
+        if constexpr (S8)
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            f32x4 sc = {0, 0, 0, 0};
+            for (int t = 0; t < N; ++t)
 #pragma unroll
-            for (int s = 0; s < KS; ++s) sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[t][s], q[s], sc, 0, 0, 0);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[t][i] = TYPE == SPMM_CACHE_S8 ? sc[i] * scale[t][i] : sc[i];
-        }
+                for (int i = 0; i < 4; ++i) scale[t][i] = fabsf(scale[t][i]) <= 3.4028235e38f ? scale[t][i] : __builtin_nanf("");
+    }
+    __device__ __forceinline__ bf16x8 operand(const int t, const int s) const
+    {
+        if constexpr (S8) return s % 2 ? codes(v[t][s / 2][2], v[t][s / 2][3]) : codes(v[t][s / 2][0], v[t][s / 2][1]);
+        else return __builtin_bit_cast(bf16x8, v[t][s]);
     }
 };
+
+// Scores of TILES tiles of columns: of the lane's column and key k0 + 16 t + 4 g + i.
+template <int KS, spmm_cache_type_t TYPE, int N, int TILES>
+__device__ __forceinline__ void scores_of(const Keys<KS, TYPE, N>& k, const bf16x8 (&q)[TILES][KS], f32x4 (&x)[TILES][N])
+{
+#pragma unroll
+    for (int t = 0; t < N; ++t) {
+#pragma unroll
+        for (int c = 0; c < TILES; ++c) x[c][t] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            const bf16x8 w = k.operand(t, s);
+#pragma unroll
+            for (int c = 0; c < TILES; ++c) x[c][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, q[c][s], x[c][t], 0, 0, 0);
+        }
+        if constexpr (TYPE == SPMM_CACHE_S8)
+#pragma unroll
+            for (int c = 0; c < TILES; ++c) x[c][t] *= k.scale[t];
+    }
+}
 
 template <int KS, spmm_cache_type_t TYPE, int TILES>
 __global__ __launch_bounds__(THREADS) void cache_weigh_stats(const WeighArgs a)
 {
+    constexpr int KEYS = 16 * NEAR;     // of a wave's step
     __shared__ float stat[WAVES][2][TILES * COLS];
     const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, col = lane % 16, g = lane / 16;
     const int H = a.pool.n_heads, G = a.group, part = blockIdx.x % a.parts, h = blockIdx.x / a.parts, b = blockIdx.y;
@@ -143,45 +161,62 @@ __global__ __launch_bounds__(THREADS) void cache_weigh_stats(const WeighArgs a)
     const int cols = s.tokens * G;
     const int32_t* const table = a.batch.table + b * a.batch.ld_table;
     for (int c0 = blockIdx.z * TILES * COLS; c0 < cols; c0 += gridDim.z * TILES * COLS) {
-        const int token_last = min(c0 + TILES * COLS, cols) - 1;
-        const Span first = span_of(a, b, s.first + c0 / G), last = span_of(a, b, s.first + token_last / G);
-        // keys that some column of these sees, and this part of them
+        const Span first = span_of(a, b, s.first + c0 / G), last = span_of(a, b, s.first + (min(c0 + TILES * COLS, cols) - 1) / G);
+        // keys that some column of these sees, and this part of them; keys that all see
         const int from = first.from <= first.to ? min(first.from, last.from) : last.from, to = last.to;
-        const int steps = to < from ? 0 : to / STEP + 1 - from / STEP, step0 = from / STEP + (int)((int64_t)steps * part / a.parts),
-                  step1 = from / STEP + (int)((int64_t)steps * (part + 1) / a.parts);
+        const int steps = to < from ? 0 : to / STEP + 1 - from / STEP;
+        const int key0 = (from / STEP + (int)((int64_t)steps * part / a.parts)) * STEP, key1 = (from / STEP + (int)((int64_t)steps * (part + 1) / a.parts)) * STEP;
+        const int all_from = last.from, all_to = first.to;
         bf16x8 q[TILES][KS];
         Span span[TILES];
         float m[TILES], l[TILES];
 #pragma unroll
         for (int x = 0; x < TILES; ++x) {
-            const int c = min(c0 + x * COLS + col, cols - 1), t = s.first + c / G;
-            load_q<KS, TYPE>(a, ((int64_t)t * H + h) * G + c % G, g, q[x]);
-            span[x] = span_of(a, b, t);
+            const int c = min(c0 + x * COLS + col, cols - 1);
+            load_q<KS, TYPE>(a, column_of(a, s, h, c), g, q[x]);
+            span[x] = span_of(a, b, s.first + c / G);
             m[x] = NONE;
             l[x] = 0.0f;
         }
-        for (int k0 = step0 * STEP + wave * KEYS; k0 < step1 * STEP && k0 <= to; k0 += STEP) {
-            Keys<KS, TYPE> k;
-            k.load(a, table, h, k0, max(s.len - 1, 0));
+        const int end = min(key1 - 1, to), last_key = max(s.len - 1, 0);
+        int k0 = key0 + wave * KEYS;
+        Keys<KS, TYPE, NEAR> k, next;
+        if (k0 <= end) next.load(a, table, h, k0, last_key);
+        for (; k0 <= end; k0 += STEP) {
+            k = next;
+            if (k0 + STEP <= end) next.load(a, table, h, k0 + STEP, last_key);
+            __builtin_amdgcn_sched_barrier(0);
+            k.ready();
+            f32x4 sc[TILES][NEAR];
+            scores_of(k, q, sc);
+            if (k0 < all_from || k0 + KEYS - 1 > all_to) {
+#pragma unroll
+                for (int x = 0; x < TILES; ++x)
+#pragma unroll
+                    for (int t = 0; t < NEAR; ++t)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int key = k0 + 16 * t + 4 * g + i;
+                            sc[x][t][i] = key >= span[x].from && key <= span[x].to ? sc[x][t][i] : NONE;
+                        }
+            }
+            if (TILES == 1 && a.keep && c0 + col < cols) {
+#pragma unroll
+                for (int t = 0; t < NEAR; ++t) *(f32x4*)(kept_of(a, b, h, c0 + col) + k0 + 16 * t + 4 * g) = sc[0][t];
+            }
 #pragma unroll
             for (int x = 0; x < TILES; ++x) {
-                float sc[2][4];
-                k.scores(q[x], sc);
                 float top = NONE;
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+                for (int t = 0; t < NEAR; ++t)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int key = k0 + 16 * t + 4 * g + i;
-                        sc[t][i] = key >= span[x].from && key <= span[x].to ? sc[t][i] : NONE;
-                        top = fmaxf(top, sc[t][i]);
-                    }
+                    for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[x][t][i]);
                 const float mn = fmaxf(m[x], top), ms = mn == NONE ? 0.0f : mn * a.scale_log2;
                 float sum = 0.0f;
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+                for (int t = 0; t < NEAR; ++t)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) sum += __builtin_amdgcn_exp2f(__fmaf_rn(sc[t][i], a.scale_log2, -ms));
+                    for (int i = 0; i < 4; ++i) sum += __builtin_amdgcn_exp2f(__fmaf_rn(sc[x][t][i], a.scale_log2, -ms));
                 l[x] = l[x] * __builtin_amdgcn_exp2f(m[x] * a.scale_log2 - ms) + sum;
                 m[x] = mn;
             }
@@ -202,13 +237,66 @@ __global__ __launch_bounds__(THREADS) void cache_weigh_stats(const WeighArgs a)
             float top = NONE, sum = 0.0f;
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) join(top, sum, stat[w][0][c], stat[w][1][c]);
-            const int i = c0 + c;
-            float* const out = stat_of(a, ((int64_t)(s.first + i / G) * H + h) * G + i % G, part);
+            float* const out = stat_of(a, column_of(a, s, h, c0 + c), part);
             out[0] = top;
             out[1] = sum;
         }
         __syncthreads();
     }
+}
+
+// What a key's weight is before this call's shares.
+__device__ __forceinline__ float faded(const WeighArgs& a, const Counted& s, const int key, const float weight)
+{
+    return key >= s.fresh || a.decay == 0.0f ? 0.0f : a.decay * weight;
+}
+
+// Shares of kept scores: a thread has four keys, in one page.
+__global__ __launch_bounds__(THREADS) void cache_weigh_kept(const WeighArgs a)
+{
+    constexpr int EACH = THREADS / COLS;
+    __shared__ float tops[EACH][COLS], sums[EACH][COLS], most[COLS], inv[COLS];
+    __shared__ Span spans[COLS];
+    const int tid = threadIdx.x, h = blockIdx.y, b = blockIdx.z, shift = a.pool.page_shift, inside = (1 << shift) - 1;
+    const Counted s = counted(a, b);
+    const int cols = s.tokens * a.group, first = blockIdx.x * THREADS * 4;
+    if (cols <= 0 || first >= s.len) return;
+    const int key = first + tid * 4;
+    // statistics of the columns, of all parts
+    const int c = tid % COLS, p0 = tid / COLS;
+    float top = NONE, sum = 0.0f;
+    if (c < cols) {
+        const int64_t column = column_of(a, s, h, c);
+        for (int p = p0; p < a.parts; p += EACH) join(top, sum, stat_of(a, column, p)[0], stat_of(a, column, p)[1]);
+        if (p0 == 0) spans[c] = span_of(a, b, s.first + c / a.group);
+    }
+    tops[p0][c] = top;
+    sums[p0][c] = sum;
+    __syncthreads();
+    if (tid < COLS) {
+        for (int i = 1; i < EACH; ++i) join(top, sum, tops[i][c], sums[i][c]);
+        most[c] = top;
+        inv[c] = 1.0f / sum;
+    }
+    __syncthreads();
+    if (key >= s.len) return;
+    const int page = a.batch.table[b * a.batch.ld_table + (key >> shift)];
+    if ((uint32_t)page >= (uint32_t)a.pool.n_pages) return;
+    float* const out = a.pool.weight + (((int64_t)page * a.pool.n_heads + h) << shift) + (key & inside);
+    f32x4 w = *(const f32x4*)out, add = {0, 0, 0, 0};
+    for (int i = 0; i < cols; ++i) {
+        const f32x4 x = *(const f32x4*)(kept_of(a, b, h, i) + key);
+        const Span span = spans[i];
+        const float m = most[i], f = inv[i];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float p = __builtin_amdgcn_exp2f(__fmaf_rn(x[j], a.scale_log2, -m)) * f;
+            add[j] += key + j >= span.from && key + j <= span.to ? p : 0.0f;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = key + j < s.len ? faded(a, s, key + j, w[j]) + add[j] : w[j];
+    *(f32x4*)out = w;
 }
 
 // A column's largest score, in units of the exponent, and 1 / the sum of powers.
@@ -226,92 +314,138 @@ __global__ __launch_bounds__(THREADS) void cache_weigh_join(const WeighArgs a)
     out[1] = 1.0f / sum;
 }
 
+// What a column goes by with, in LDS.
+struct Column {
+    int64_t id;
+    float most, inv;
+    Span span;
+};
+
 template <int KS, spmm_cache_type_t TYPE>
 __global__ __launch_bounds__(THREADS) void cache_weigh_add(const WeighArgs a)
 {
+    constexpr int KEYS = 16 * FAR;      // of a wave's step
+    __shared__ Column columns[LISTED];
     const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, col = lane % 16, g = lane / 16;
-    const int H = a.pool.n_heads, G = a.group, part = blockIdx.x % a.parts, h = blockIdx.x / a.parts, b = blockIdx.y;
-    const int shift = a.pool.page_shift, inside = (1 << shift) - 1;
+    const int H = a.pool.n_heads, G = a.group, h = blockIdx.y, b = blockIdx.z, shift = a.pool.page_shift, inside = (1 << shift) - 1;
     const Counted s = counted(a, b);
     const int cols = s.tokens * G;
     if (cols <= 0) return;
     const int32_t* const table = a.batch.table + b * a.batch.ld_table;
-    const int steps = (s.len + STEP - 1) / STEP, step0 = (int)((int64_t)steps * part / a.parts), step1 = (int)((int64_t)steps * (part + 1) / a.parts);
-    for (int k0 = step0 * STEP + wave * KEYS; k0 < step1 * STEP && k0 < s.len; k0 += STEP) {
-        Keys<KS, TYPE> k;
+    for (int block = blockIdx.x * KEYS * WAVES; block < s.len; block += gridDim.x * KEYS * WAVES) {
+        const int k0 = block + wave * KEYS;
+        Keys<KS, TYPE, FAR> k;
         k.load(a, table, h, k0, s.len - 1);
-        float sum[2][4] = {};
-        for (int c0 = 0; c0 < cols; c0 += COLS) {
-            const int c = min(c0 + col, cols - 1), t = s.first + c / G;
-            const int64_t column = ((int64_t)t * H + h) * G + c % G;
-            bf16x8 q[KS];
-            load_q<KS, TYPE>(a, column, g, q);
-            const Span span = span_of(a, b, t);
-            const float* const joined = joined_of(a, column);
-            const float most = joined[0], inv = joined[1];
-            float sc[2][4];
-            k.scores(q, sc);
-#pragma unroll
-            for (int t2 = 0; t2 < 2; ++t2)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int key = k0 + 16 * t2 + 4 * g + i;
-                    const float p = __builtin_amdgcn_exp2f(__fmaf_rn(sc[t2][i], a.scale_log2, -most)) * inv;
-                    if (key >= span.from && key <= span.to && c0 + col < cols) sum[t2][i] += p;
+        float sum[4 * FAR] = {};
+        for (int c0 = 0; c0 < cols; c0 += LISTED) {
+            const int n = min(cols - c0, LISTED), rounded = (n + COLS - 1) / COLS * COLS;
+            if (cols > LISTED || block == (int)blockIdx.x * KEYS * WAVES) {
+                __syncthreads();        // (the last ones have been read)
+                for (int i = tid; i < rounded; i += THREADS) {
+                    // (columns that fill the last tile up are the last one, with no share)
+                    const int c = c0 + min(i, n - 1);
+                    const int64_t id = column_of(a, s, h, c);
+                    columns[i] = Column{id, joined_of(a, id)[0], i < n ? joined_of(a, id)[1] : 0.0f, span_of(a, b, s.first + c / G)};
                 }
-        }
-#pragma unroll
-        for (int t2 = 0; t2 < 2; ++t2)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                for (int o = 1; o < 16; o <<= 1) sum[t2][i] += __shfl_xor(sum[t2][i], o);
-                const int key = k0 + 16 * t2 + 4 * g + i;
-                if (col == 0 && key < s.len) {
-                    const int page = table[key >> shift];
-                    if ((uint32_t)page >= (uint32_t)a.pool.n_pages) continue;
-                    float* const w = a.pool.weight + (((int64_t)page * H + h) << shift) + (key & inside);
-                    *w = (key >= s.fresh || a.decay == 0.0f ? 0.0f : a.decay * *w) + sum[t2][i];
-                }
+                __syncthreads();
             }
+            if (c0 == 0) k.ready();
+            bf16x8 q[1][KS], next[KS];
+            load_q<KS, TYPE>(a, columns[col].id, g, next);
+            for (int i = 0; i < rounded; i += COLS) {
+#pragma unroll
+                for (int x = 0; x < KS; ++x) q[0][x] = next[x];
+                if (i + COLS < rounded) load_q<KS, TYPE>(a, columns[i + COLS + col].id, g, next);
+                const Span first = columns[i].span, last = columns[i + COLS - 1].span;
+                if (k0 > last.to || k0 + KEYS <= first.from) continue;      // (no column of the tile sees any of the keys)
+                const Column c = columns[i + col];
+                f32x4 sc[1][FAR];
+                scores_of(k, q, sc);
+                const bool all = k0 >= last.from && k0 + KEYS - 1 <= first.to;
+#pragma unroll
+                for (int t = 0; t < FAR; ++t)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float p = __builtin_amdgcn_exp2f(__fmaf_rn(sc[0][t][j], a.scale_log2, -c.most));
+                        if (all) {
+                            sum[4 * t + j] = __fmaf_rn(p, c.inv, sum[4 * t + j]);
+                        } else {
+                            const int key = k0 + 16 * t + 4 * g + j;
+                            sum[4 * t + j] += key >= c.span.from && key <= c.span.to ? p * c.inv : 0.0f;
+                        }
+                    }
+            }
+        }
+        // over the 16 lanes of a key: each hands the others half of what it has, and is left with the sum of one key
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                if (j >= o) continue;
+                const bool high = col & o;
+                const float give = high ? sum[j] : sum[j + o], keep = high ? sum[j + o] : sum[j];
+                sum[j] = keep + __shfl_xor(give, o);
+            }
+        const int key = k0 + 16 * (col / 4) + 4 * g + col % 4;
+        if (key < s.len) {
+            const int page = table[key >> shift];
+            if ((uint32_t)page < (uint32_t)a.pool.n_pages) {
+                float* const w = a.pool.weight + (((int64_t)page * H + h) << shift) + (key & inside);
+                *w = faded(a, s, key, *w) + sum[0];
+            }
+        }
     }
 }
 
-constexpr int MANY = 4;             // tiles of columns of a workgroup, where there are many
-
-static int64_t blocks_of(const int64_t cols) { return cols <= COLS ? 1 : (cols + MANY * COLS - 1) / (MANY * COLS); }
-
-static int parts_of(const int page_tokens, const int64_t n_seqs, const int64_t ld_table, const int n_heads, const int64_t cols)
+// How a call is cut up: parts of the keys that statistics are taken of, and whether scores are kept.
+struct WeighShape {
+    int parts, keep;
+    int64_t bytes;
+};
+static WeighShape shape_of(const int page_tokens, const int64_t n_seqs, const int64_t ld_table, const int n_heads, const int64_t cols, const int64_t columns)
 {
-    const int64_t most = (ld_table * page_tokens + STEP - 1) / STEP, want = 2048 / (n_seqs * n_heads * blocks_of(cols));
-    return (int)(want < 1 ? 1 : want < most ? want : most);
+    const int64_t keys = ld_table * page_tokens, most = (keys + STEP - 1) / STEP, blocks = cols <= COLS ? 1 : (cols + MANY * COLS - 1) / (MANY * COLS);
+    const int64_t want = (cols <= COLS ? 2048 : 1024) / (n_seqs * n_heads * blocks);
+    WeighShape f;
+    f.parts = (int)(want < 1 ? 1 : want < most ? want : most);
+    const double kept = 4.0 * n_seqs * n_heads * cols * kept_keys(keys);
+    f.keep = cols <= COLS && kept <= KEPT;
+    f.bytes = (columns * f.parts + 1) / 2 * 16 + (f.keep ? (int64_t)kept : 8 * columns);
+    return f;
 }
 
-int64_t weigh_work_bytes(const int page_tokens, const int64_t n_seqs, const int64_t ld_table, const int n_heads, const int64_t cols)
+int64_t weigh_work_bytes(const int page_tokens, const int64_t n_seqs, const int64_t ld_table, const int n_heads, const int64_t cols, const int64_t columns)
 {
-    return 8 * (int64_t)(parts_of(page_tokens, n_seqs, ld_table, n_heads, cols) + 1);     // of a column
+    return shape_of(page_tokens, n_seqs, ld_table, n_heads, cols, columns).bytes;
 }
 
 template <int KS, spmm_cache_type_t TYPE>
-static int launch_steps(const WeighArgs& a, const int64_t blocks, void* stream)
+static int launch_steps(const WeighArgs& a, const int64_t cols, void* stream)
 {
-    const dim3 grid((unsigned)(a.parts * a.pool.n_heads), (unsigned)a.batch.n_seqs, (unsigned)(blocks < 65535 ? blocks : 65535));
-    const bool few = (int64_t)a.max_new * a.group <= COLS;
-    if (const int rc = few ? launch(cache_weigh_stats<KS, TYPE, 1>, grid, dim3(THREADS), a, stream) : launch(cache_weigh_stats<KS, TYPE, MANY>, grid, dim3(THREADS), a, stream)) return rc;
+    const int64_t blocks = cols <= COLS ? 1 : (cols + MANY * COLS - 1) / (MANY * COLS), keys = a.batch.ld_table << a.pool.page_shift;
+    const dim3 grid((unsigned)(a.parts * a.pool.n_heads), (unsigned)a.batch.n_seqs, (unsigned)(blocks < 65535 ? blocks : 65535)), threads(THREADS);
+    if (const int rc = cols <= COLS ? launch(cache_weigh_stats<KS, TYPE, 1>, grid, threads, a, stream) : launch(cache_weigh_stats<KS, TYPE, MANY>, grid, threads, a, stream)) return rc;
+    const auto blocks_of = [&](const int each) { return dim3((unsigned)((keys + each - 1) / each), (unsigned)a.pool.n_heads, (unsigned)a.batch.n_seqs); };
+    if (a.keep) return launch(cache_weigh_kept, blocks_of(4 * THREADS), threads, a, stream);
     const int64_t columns = (int64_t)a.T * a.group * a.pool.n_heads;
-    if (const int rc = launch(cache_weigh_join, dim3((unsigned)((columns + THREADS - 1) / THREADS)), dim3(THREADS), a, stream)) return rc;
-    return launch(cache_weigh_add<KS, TYPE>, dim3(grid.x, grid.y), dim3(THREADS), a, stream);
+    if (const int rc = launch(cache_weigh_join, dim3((unsigned)((columns + THREADS - 1) / THREADS)), threads, a, stream)) return rc;
+    dim3 all = blocks_of(16 * FAR * WAVES);
+    if (all.x > 4096) all.x = 4096;
+    return launch(cache_weigh_add<KS, TYPE>, all, threads, a, stream);
 }
 
 int launch_weigh(const WeighArgs& args, const spmm_cache_type_t type, void* stream)
 {
     WeighArgs a = args;
-    const int64_t cols = (int64_t)a.max_new * a.group, blocks = blocks_of(cols);
-    a.parts = parts_of(1 << a.pool.page_shift, a.batch.n_seqs, a.batch.ld_table, a.pool.n_heads, cols);
+    const int64_t cols = (int64_t)a.max_new * a.group;
+    const WeighShape f = shape_of(1 << a.pool.page_shift, a.batch.n_seqs, a.batch.ld_table, a.pool.n_heads, cols, (int64_t)a.T * a.group * a.pool.n_heads);
+    a.parts = f.parts;
+    a.keep = f.keep;
     const int dim = a.pool.head_dim;
-    if (type == SPMM_CACHE_S8) return dim > 64 ? launch_steps<4, SPMM_CACHE_S8>(a, blocks, stream) : launch_steps<2, SPMM_CACHE_S8>(a, blocks, stream);
-    return dim > 96 ? launch_steps<4, SPMM_CACHE_BF16>(a, blocks, stream)
-         : dim > 64 ? launch_steps<3, SPMM_CACHE_BF16>(a, blocks, stream)
-         : dim > 32 ? launch_steps<2, SPMM_CACHE_BF16>(a, blocks, stream) : launch_steps<1, SPMM_CACHE_BF16>(a, blocks, stream);
+    if (type == SPMM_CACHE_S8) return dim > 64 ? launch_steps<4, SPMM_CACHE_S8>(a, cols, stream) : launch_steps<2, SPMM_CACHE_S8>(a, cols, stream);
+    return dim > 96 ? launch_steps<4, SPMM_CACHE_BF16>(a, cols, stream)
+         : dim > 64 ? launch_steps<3, SPMM_CACHE_BF16>(a, cols, stream)
+         : dim > 32 ? launch_steps<2, SPMM_CACHE_BF16>(a, cols, stream) : launch_steps<1, SPMM_CACHE_BF16>(a, cols, stream);
 }
 
 }  // namespace spmm_cache
