@@ -33,7 +33,8 @@ __global__ __launch_bounds__(THREADS) void cache_bounds(const BoundsArgs a)
     const int first = past > 0 ? (int)(past >> shift) : 0, pages = ((len - 1) >> shift) + 1 - first;
     const int wide = D / N, deep = 64 / wide, c = lane % wide, r = lane / wide;
     const int64_t all = (int64_t)pages * H;
-    for (int64_t w = (int64_t)blockIdx.x * WAVES + threadIdx.x / 64; w < all; w += (int64_t)gridDim.x * WAVES) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    for (int64_t w = (int64_t)blockIdx.x * WAVES + wave; w < all; w += (int64_t)gridDim.x * WAVES) {
         const int i = first + (int)(w / H), h = (int)(w % H);
         const int page = a.batch.table[b * a.batch.ld_table + i];
         if ((uint32_t)page >= (uint32_t)a.pool.n_pages) continue;

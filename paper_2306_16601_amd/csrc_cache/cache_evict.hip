@@ -12,15 +12,12 @@
 
 namespace spmm_cache {
 
-constexpr int CHOOSE_WAVES = 16, CHOOSE_REGS = 32;
 constexpr int MOVE_THREADS = 256;
 constexpr int PIECE = 1024;         // tokens that are moved with one list of places
-constexpr int KEYS_AHEAD = 8, VALUES_AHEAD = 4;
-constexpr int VALUE_DIMS = 4;       // of a wave
-
-struct MoveShape {
-    int keys, values;       // slices of a head's keys, and of its values
-};
+constexpr int KEYS_AHEAD = 8;       // steps whose loads are under way together
+constexpr int VALUE_DIMS = 16;      // of a workgroup
+template <int BYTES>
+constexpr int SPAN = 1024 / BYTES;  // tokens whose values are in LDS at a time
 
 // How many tokens of a row there are, and how many stay: all of them, the first, the last.
 struct Stay {
@@ -37,11 +34,10 @@ __device__ __forceinline__ Stay stay_of(const EvictArgs& a, const int b)
     return s;
 }
 
-// (two workgroups on a CU where the registers allow it)
-template <int REGS>
-__global__ __launch_bounds__(64 * CHOOSE_WAVES, (REGS > 16 ? 4 : 8)) void cache_evict_choose(const EvictArgs a)
+// W: waves of a row's head, REGS: values of a lane (0: any number, read again at each pass)
+template <int W, int REGS>
+__global__ __launch_bounds__(64 * W, (REGS > 16 ? 4 : 8)) void cache_evict_choose(const EvictArgs a)
 {
-    constexpr int W = CHOOSE_WAVES;
     __shared__ Bins<W> bins;
     __shared__ int totals[(REGS ? REGS : 1) * W][2];
     const int H = a.pool.n_heads, h = blockIdx.x % H, layer = blockIdx.x / H, b = blockIdx.y;
@@ -78,130 +74,225 @@ __global__ __launch_bounds__(64 * CHOOSE_WAVES, (REGS > 16 ? 4 : 8)) void cache_
     }
 }
 
-// Where a piece of the tokens that stay are and go to: bytes from the first of a layer's keys, values or numbers, -1: nowhere.
-struct Piece {
-    int64_t from[PIECE], to[PIECE / 16];        // `to` of every 16 tokens, which lie in one page
+// The place of a token of a row among all of a layer's, times heads; -1: nowhere.
+__device__ __forceinline__ int64_t slot_of(const EvictArgs& a, const int32_t* const pages, const int h, const int at)
+{
+    const int shift = a.pool.page_shift, page = pages[at >> shift];
+    return (uint32_t)page < (uint32_t)a.pool.n_pages ? (((int64_t)page * a.pool.n_heads + h) << shift) + (at & ((1 << shift) - 1)) : -1;
+}
+
+// What a workgroup moves: a slice of a row's head of a layer.
+struct Moved {
+    int slice, h, layer, b;
+    Stay stay;
+    const int32_t *table, *table_to, *kept;
+};
+__device__ __forceinline__ Moved moved(const EvictArgs& a, const int slices)
+{
+    Moved m;
+    const int lh = blockIdx.x / slices, H = a.pool.n_heads;
+    m.slice = blockIdx.x % slices;
+    m.h = lh % H;
+    m.layer = lh / H;
+    m.b = blockIdx.y;
+    m.stay = stay_of(a, m.b);
+    m.table = a.table + m.b * a.ld_table;
+    m.table_to = a.table_to + m.b * a.ld_table;
+    m.kept = a.kept + (((int64_t)m.layer * a.n_rows + m.b) * H + m.h) * a.most;
+    return m;
+}
+
+// LDS of a workgroup: a piece of the tokens, and where every 16 of them go, which lie in one page
+struct ForKeys {
+    int64_t from[PIECE], to[PIECE / 16];
+};
+template <int BYTES>
+struct ForValues {
+    alignas(16) char tokens[VALUE_DIMS * SPAN<BYTES> * BYTES * 5 / 4];
+    alignas(16) uint16_t at[PIECE]; // where a token is in `tokens`, once its pages are there (of the first dim)
+    int ids[PIECE], found;
+    int64_t to[PIECE / 16];
 };
 
-// A workgroup moves a slice of a row's head: dims of its keys, dims of its values, or its scales and weights.
-template <spmm_cache_type_t TYPE>
-__global__ __launch_bounds__(MOVE_THREADS, 5) void cache_evict_move(const EvictArgs a, const MoveShape f)
+// Keys: slices of the dims, 16 bytes of a token a lane; and, as the last slice, what is a number a token: weights and scales.
+template <int BYTES>
+__device__ __forceinline__ void move_keys(const EvictArgs& a, const Moved& m, const int slices, ForKeys& lds)
 {
-    constexpr int BYTES = TYPE == SPMM_CACHE_S8 ? 1 : 2;
-    __shared__ Piece piece;
-    const int H = a.pool.n_heads, D = a.pool.head_dim, shift = a.pool.page_shift, inside = (1 << shift) - 1, tid = threadIdx.x;
-    const int slices = f.keys + f.values + 1, slice = blockIdx.x % slices, lh = blockIdx.x / slices, h = lh % H, layer = lh / H, b = blockIdx.y;
-    const Stay s = stay_of(a, b);
-    if (s.n == 0) return;
-    const bool keys = slice < f.keys, values = !keys && slice < f.keys + f.values;
-    const int32_t *const table = a.table + b * a.ld_table, *const table_to = a.table_to + b * a.ld_table;
-    const int32_t* const kept = a.kept + (((int64_t)layer * a.n_rows + b) * H + h) * a.most;
-    const int64_t layer_slots = layer * a.layer_slots;
-    const auto place = [&](const int32_t* const pages, const int at) {
-        const int page = pages[at >> shift];
-        if ((uint32_t)page >= (uint32_t)a.pool.n_pages) return (int64_t)-1;
-        const int64_t head = ((int64_t)page * H + h) << shift;
-        const int off = at & inside;
-        return keys ? (head + off) * D * BYTES : values ? (head * D + off) * BYTES : (head + off) * 4;
-    };
-    for (int i0 = 0; i0 < s.n; i0 += PIECE) {
-        const int n = min(s.n - i0, PIECE);
+    int64_t *const from = lds.from, *const to = lds.to;
+    const int tid = threadIdx.x, row = a.pool.head_dim * BYTES;
+    const int64_t layer_slots = m.layer * a.layer_slots;
+    for (int i0 = 0; i0 < m.stay.n; i0 += PIECE) {
+        const int n = min(m.stay.n - i0, PIECE);
         __syncthreads();        // (the last piece has been read)
         for (int i = tid; i < n; i += MOVE_THREADS) {
-            piece.from[i] = max(place(table, kept[i0 + i]), (int64_t)0);
-            if (i % 16 == 0) piece.to[i / 16] = place(table_to, i0 + i);
+            from[i] = max(slot_of(a, m.table, m.h, m.kept[i0 + i]), (int64_t)0);
+            if (i % 16 == 0) to[i / 16] = slot_of(a, m.table_to, m.h, i0 + i);
         }
         __syncthreads();
-        if (keys) {
-            // a lane has 16 bytes of a token
-            const int row = D * BYTES, per = row / 16 / f.keys, c = tid % per, rows = MOVE_THREADS / per, r = tid / per;
-            char* const pool = (char*)a.pool.k + layer_slots * row + (slice * per + c) * 16;
+        if (m.slice < slices) {
+            const int per = row / 16 / slices, c = tid % per, rows = MOVE_THREADS / per, r = tid / per;
+            char* const pool = (char*)a.pool.k + layer_slots * row + (m.slice * per + c) * 16;
             for (int i1 = 0; i1 < n; i1 += rows * KEYS_AHEAD) {
-                u32x4 v[KEYS_AHEAD] = {};
+                u32x4 v[KEYS_AHEAD];
 #pragma unroll
-                for (int k = 0; k < KEYS_AHEAD; ++k) {
-                    const int i = i1 + k * rows + r;
-                    if (r < rows && i < n) v[k] = *(const u32x4*)(pool + piece.from[i]);
-                }
+                for (int k = 0; k < KEYS_AHEAD; ++k) v[k] = *(const u32x4*)(pool + from[min(i1 + k * rows + r, n - 1)] * row);
 #pragma unroll
                 for (int k = 0; k < KEYS_AHEAD; ++k) asm volatile("" : "+v"(v[k]));       // (loads are back, not only under way, before anyone stores)
                 __syncthreads();
+                if (r >= rows) continue;
 #pragma unroll
                 for (int k = 0; k < KEYS_AHEAD; ++k) {
                     const int i = i1 + k * rows + r;
-                    if (r < rows && i < n && piece.to[i / 16] >= 0) *(u32x4*)(pool + piece.to[i / 16] + i % 16 * row) = v[k];
-                }
-            }
-        } else if (values) {
-            // a wave has VALUE_DIMS dims and no other wave has them, a lane four tokens of one
-            using E = typename std::conditional<TYPE == SPMM_CACHE_S8, uint8_t, uint16_t>::type;
-            constexpr int LANES = 64 / VALUE_DIMS, TOKENS = LANES * 4;       // of a dim; tokens of a wave's step
-            const int dims = D / f.values, lane = tid % 64, j = lane % LANES * 4;
-            for (int d = (slice - f.keys) * dims + tid / 64 * VALUE_DIMS + lane / LANES; d < (slice - f.keys + 1) * dims; d += MOVE_THREADS / 64 * VALUE_DIMS) {
-                char* const pool = (char*)a.pool.v + (layer_slots * D + ((int64_t)d << shift)) * BYTES;
-                for (int i1 = j; i1 - j < n; i1 += TOKENS * VALUES_AHEAD) {
-                    uint32_t v[VALUES_AHEAD][BYTES] = {};
-#pragma unroll
-                    for (int k = 0; k < VALUES_AHEAD; ++k)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            v[k][e * BYTES / 4] |= (uint32_t) * (const E*)(pool + piece.from[min(i1 + k * TOKENS + e, n - 1)]) << (e * 8 * BYTES % 32);
-                    // (a wave's loads are back before its first store, which waits for the last of them)
-#pragma unroll
-                    for (int k = 0; k < VALUES_AHEAD; ++k)
-#pragma unroll
-                        for (int w = 0; w < BYTES; ++w) asm volatile("" : "+v"(v[k][w]));
-#pragma unroll
-                    for (int k = 0; k < VALUES_AHEAD; ++k) {
-                        const int i = i1 + k * TOKENS;
-                        if (i >= n || piece.to[i / 16] < 0) continue;
-                        char* const out = pool + piece.to[i / 16] + i % 16 * BYTES;
-                        if (i + 4 <= n) {
-                            if constexpr (BYTES == 1) *(uint32_t*)out = v[k][0];
-                            else *(u32x2*)out = u32x2{v[k][0], v[k][BYTES - 1]};
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 3; ++e)
-                                if (i + e < n) ((E*)out)[e] = (E)(v[k][e * BYTES / 4] >> (e * 8 * BYTES % 32));
-                        }
-                    }
+                    if (i >= n) break;
+                    const int64_t slot = to[i / 16];
+                    if (slot >= 0) *(u32x4*)(pool + (slot + i % 16) * row) = v[k];
                 }
             }
         } else {
-            char* const parts[3] = {(char*)a.pool.weight, (char*)a.pool.k_scale, (char*)a.pool.v_scale};
+            float* const parts[3] = {a.pool.weight, a.pool.k_scale, a.pool.v_scale};
             for (int i1 = 0; i1 < n; i1 += MOVE_THREADS) {
                 const int i = i1 + tid;
                 float v[3] = {0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int p = 0; p < 3; ++p)
-                    if (i < n && parts[p]) v[p] = *(const float*)(parts[p] + layer_slots * 4 + piece.from[i]);
+                    if (i < n && parts[p]) v[p] = parts[p][layer_slots + from[i]];
 #pragma unroll
                 for (int p = 0; p < 3; ++p) asm volatile("" : "+v"(v[p]));
                 __syncthreads();
 #pragma unroll
                 for (int p = 0; p < 3; ++p)
-                    if (i < n && parts[p] && piece.to[i / 16] >= 0) *(float*)(parts[p] + layer_slots * 4 + piece.to[i / 16] + i % 16 * 4) = v[p];
+                    if (i < n && parts[p] && to[i / 16] >= 0) parts[p][layer_slots + to[i / 16] + i % 16] = v[p];
             }
         }
+    }
+}
+
+// Values: VALUE_DIMS dims, whose tokens of a page are one run of memory.  Pages go through LDS, SPAN tokens at a time from the first that has one that
+// stays; the tokens that stay are picked out there, 16 bytes of them a lane, and lanes side by side write a page's dims one after the other.
+template <int BYTES>
+__device__ __forceinline__ void move_values(const EvictArgs& a, const Moved& m, ForValues<BYTES>& lds)
+{
+    constexpr int LOADS = VALUE_DIMS * SPAN<BYTES> * BYTES / 16 / MOVE_THREADS, GROUP = 16 / BYTES, LOG = BYTES == 1 ? 4 : 3;
+    using E = typename std::conditional<BYTES == 1, uint8_t, uint16_t>::type;
+    typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+    E* const tokens = (E*)lds.tokens;
+    int *const ids = lds.ids, &found = lds.found;
+    uint16_t* const place = lds.at;
+    int64_t* const to = lds.to;
+    const int tid = threadIdx.x, shift = a.pool.page_shift, inside = (1 << shift) - 1, D = a.pool.head_dim, H = a.pool.n_heads, d0 = m.slice * VALUE_DIMS;
+    const int last_page = max(m.stay.len - 1, 0) >> shift;
+    const int pitch = (1 << shift) + (BYTES << shift >= 64 ? GROUP : 0);       // of a dim's row in LDS, so that dims begin at different banks
+    E* const pool = (E*)a.pool.v + m.layer * a.layer_slots * D;
+    for (int i = tid; i < PIECE; i += MOVE_THREADS) place[i] = 0;      // (a place that is there, for tokens whose own is not known yet)
+    for (int i0 = 0; i0 < m.stay.n; i0 += PIECE) {
+        const int n = min(m.stay.n - i0, PIECE);
+        __syncthreads();        // (the last piece has been read)
+        for (int i = tid; i < n; i += MOVE_THREADS) {
+            ids[i] = m.kept[i0 + i];
+            if (i % 16 == 0) {
+                // (of the slice's first dim: pages hold a head's dims one after the other)
+                const int64_t slot = slot_of(a, m.table_to, m.h, i0 + i);
+                to[i / 16] = slot < 0 ? -1 : (slot >> shift << shift) * D + ((int64_t)d0 << shift) + (slot & inside);
+            }
+        }
+        __syncthreads();
+        u32x4 v[LOADS];
+        const auto load = [&](const int start) {
+#pragma unroll
+            for (int k = 0; k < LOADS; ++k) {
+                const int off = (k * MOVE_THREADS + tid) * GROUP, page = (start >> shift) + (off >> shift) / VALUE_DIMS;
+                const int number = page_in_pool(m.table[min(page, last_page)], a.pool.n_pages);
+                v[k] = *(const u32x4*)(pool + ((((int64_t)number * H + m.h) * D + d0) << shift) + (off & ((VALUE_DIMS << shift) - 1)));
+            }
+        };
+        int start = ids[0] & ~inside;
+        load(start);
+        for (int begin = 0; begin < n;) {
+#pragma unroll
+            for (int k = 0; k < LOADS; ++k) {
+                const int off = (k * MOVE_THREADS + tid) * GROUP;
+                *(u32x4*)&tokens[(off >> shift) * pitch + (off & inside)] = v[k];
+            }
+            for (int i = begin + tid; i < min(n, begin + SPAN<BYTES>); i += MOVE_THREADS) {
+                const int at = ids[i] - start;
+                if (at >= SPAN<BYTES>) break;
+                place[i] = (uint16_t)((at >> shift) * VALUE_DIMS * pitch + (at & inside));
+                if (i + 1 == n || ids[i + 1] - start >= SPAN<BYTES>) found = i + 1;
+            }
+            __syncthreads();
+            // whole groups go, and the tokens behind them with the next pages, unless there is no group
+            const int here = found, end = here == n || (here & ~15) <= begin ? here : here & ~15, next = end < n ? ids[end] & ~inside : start;
+            if (end < n) load(next);
+            // (what is stored lies before what is loaded and needed: a token goes to no later place than its own)
+            const int first_page = begin >> shift, items = (((end - 1) >> shift) + 1 - first_page) << (shift - LOG + 4);
+            for (int x = tid; x < items; x += MOVE_THREADS) {
+                const int i = ((first_page + (x >> (shift - LOG + 4))) << shift) + (x & (inside >> LOG)) * GROUP, d = x >> (shift - LOG) & (VALUE_DIMS - 1);
+                if (i >= end || i + GROUP <= begin) continue;
+                const int64_t first = to[i / 16];
+                if (first < 0) continue;
+                // (of a group's tokens those that do not go now have another place, or none yet)
+                E v[GROUP];
+#pragma unroll
+                for (int e = 0; e < GROUP; e += 8) {
+                    const u16x8 from = *(const u16x8*)&place[i + e];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[e + j] = tokens[from[j] + d * pitch];
+                }
+                E* const out = pool + first + ((int64_t)d << shift) + i % 16;
+                if (i >= begin && i + GROUP <= end) {
+                    u32x4 w;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        w[j] = BYTES == 1 ? v[GROUP / 4 * j] | v[GROUP / 4 * j + 1] << 8 | v[GROUP / 4 * j + GROUP / 4 - 2] << 16 | (uint32_t)v[GROUP / 4 * j + GROUP / 4 - 1] << 24
+                                          : v[2 * j] | (uint32_t)v[2 * j + 1] << 16;
+                    *(u32x4*)out = w;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < GROUP; ++e)
+                        if (i + e >= begin && i + e < end) out[e] = v[e];
+                }
+            }
+            __syncthreads();
+            begin = end;
+            start = next;
+        }
+    }
+}
+
+// Slices of a head, each of which a workgroup moves: VALUE_DIMS dims of the values, `keys` parts of the keys' dims, weights and scales.
+template <int BYTES>
+__global__ __launch_bounds__(MOVE_THREADS, 5) void cache_evict_move(const EvictArgs a, const int keys)
+{
+    __shared__ union {
+        ForKeys keys;
+        ForValues<BYTES> values;
+    } lds;
+    const int values = a.pool.head_dim / VALUE_DIMS;
+    Moved m = moved(a, values + keys + 1);
+    if (m.slice < values) {
+        move_values<BYTES>(a, m, lds.values);
+    } else {
+        m.slice -= values;
+        move_keys<BYTES>(a, m, keys, lds.keys);
     }
 }
 
 int launch_evict(const EvictArgs& a, const spmm_cache_type_t type, void* stream)
 {
     const int64_t most = a.ld_table << a.pool.page_shift, heads = (int64_t)a.n_layers * a.pool.n_heads;
-    const dim3 rows((unsigned)heads, (unsigned)a.n_rows), threads(64 * CHOOSE_WAVES);
+    const dim3 rows((unsigned)heads, (unsigned)a.n_rows);
     int rc;
-    if (most <= 64 * CHOOSE_WAVES * 8) rc = launch(cache_evict_choose<8>, rows, threads, a, stream);
-    else if (most <= 64 * CHOOSE_WAVES * 16) rc = launch(cache_evict_choose<16>, rows, threads, a, stream);
-    else if (most <= 64 * CHOOSE_WAVES * CHOOSE_REGS) rc = launch(cache_evict_choose<CHOOSE_REGS>, rows, threads, a, stream);
-    else rc = launch(cache_evict_choose<0>, rows, threads, a, stream);
+    if (most <= 64 * 4 * 4) rc = launch(cache_evict_choose<4, 4>, rows, dim3(64 * 4), a, stream);
+    else if (most <= 64 * 4 * 16) rc = launch(cache_evict_choose<4, 16>, rows, dim3(64 * 4), a, stream);
+    else if (most <= 64 * 16 * 16) rc = launch(cache_evict_choose<16, 16>, rows, dim3(64 * 16), a, stream);
+    else if (most <= 64 * 16 * 32) rc = launch(cache_evict_choose<16, 32>, rows, dim3(64 * 16), a, stream);
+    else rc = launch(cache_evict_choose<16, 0>, rows, dim3(64 * 16), a, stream);
     if (rc) return rc;
-    // a slice has 128 bytes of a key at least, and 16 dims of values, one step of four waves
-    MoveShape f = {1, a.pool.head_dim / 16};
-    if (type == SPMM_CACHE_BF16 && a.pool.head_dim == 128) f.keys = 2;
-    void* args[] = {const_cast<EvictArgs*>(&a), &f};
-    return (int)hipLaunchKernel(type == SPMM_CACHE_S8 ? (const void*)cache_evict_move<SPMM_CACHE_S8> : (const void*)cache_evict_move<SPMM_CACHE_BF16>,
-                                dim3((unsigned)(heads * (f.keys + f.values + 1)), (unsigned)a.n_rows), dim3(MOVE_THREADS), args, 0, (hipStream_t)stream);
+    // (keys in slices of 128 bytes where they have that many)
+    int keys = type == SPMM_CACHE_BF16 && a.pool.head_dim == 128 ? 2 : 1;
+    void* args[] = {const_cast<EvictArgs*>(&a), &keys};
+    return (int)hipLaunchKernel(type == SPMM_CACHE_S8 ? (const void*)cache_evict_move<1> : (const void*)cache_evict_move<2>,
+                                dim3((unsigned)(heads * (a.pool.head_dim / VALUE_DIMS + keys + 1)), (unsigned)a.n_rows), dim3(MOVE_THREADS), args, 0, (hipStream_t)stream);
 }
 
 }  // namespace spmm_cache

@@ -29,7 +29,7 @@ struct ScoreShape {
 template <int KS, int TILES>
 __global__ __launch_bounds__(THREADS, (TILES > 1 ? 2 : 3)) void cache_score(const ScoreArgs a, const ScoreShape f)
 {
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, col = lane % 16, g = lane / 16;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 16, g = lane / 16;
     constexpr int D = 16 * KS;
     const int H = a.pool.n_heads, G = a.group, h = blockIdx.x % H, per = ROWS / f.padded;
     const int width = (int)a.batch.ld_table;
@@ -49,6 +49,7 @@ __global__ __launch_bounds__(THREADS, (TILES > 1 ? 2 : 3)) void cache_score(cons
         // position of column t: of the others it is so many more (they lie between -2^30 and 2^30)
         const int at0 = (int)max((int64_t)a.batch.kv_len[b] - ((int64_t)a.batch.q_start[b + 1] - t), (int64_t)-(1 << 30));
         const int seen = span_of(a.batch, b, end - 1, shift, a.causal, a.window).to >> shift;      // (no column before sees a later page)
+#pragma unroll 1
         for (int turn = 0; turn < f.turns; ++turn) {
             // queries: row r of tile x is token (x * 16 + r) / padded, head r % padded (of this turn), or another of it where there is none
             bf16x8 q[TILES][KS];
@@ -68,29 +69,15 @@ __global__ __launch_bounds__(THREADS, (TILES > 1 ? 2 : 3)) void cache_score(cons
                 __builtin_amdgcn_sched_barrier(0);
             }
             const auto load = [&](const int p, bf16x8 (&v)[KS]) {
-                const int page = page_in_pool(table[min(p + col, seen)], a.pool.n_pages);
+                const int page = page_in_pool(table[max(min(p + col, seen), 0)], a.pool.n_pages);
                 const bf16x8* const src = (const bf16x8*)(a.pool.bounds + ((int64_t)page * H + h) * 2 * D) + g;
 #pragma unroll
                 for (int s = 0; s < KS; ++s) v[s] = src[4 * s];
             };
-            bf16x8 v[KS];
-            if (p0 < p1 && p0 <= seen) load(p0, v);
-            for (int p = p0; p < p1; p += PAGES) {
-                f32x4 sc[TILES];
-#pragma unroll
-                for (int x = 0; x < TILES; ++x) sc[x] = f32x4{0, 0, 0, 0};
-                if (p <= seen) {
-#pragma unroll
-                    for (int s = 0; s < KS; ++s)
-#pragma unroll
-                        for (int x = 0; x < TILES; ++x) sc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[x][s], v[s], sc[x], 0, 0, 0);
-                    __builtin_amdgcn_sched_barrier(0);
-                    if (p + PAGES < p1 && p + PAGES <= seen) load(p + PAGES, v);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
+            const auto store = [&](const int p, const f32x4 (&sc)[TILES]) {
                 int g_out = g;
                 asm volatile("" : "+v"(g_out));     // (or what the stores need of each tile is worked out before the loop, and spilled)
-                if (p + col >= width) continue;
+                if (p + col >= width) return;
 #pragma unroll
                 for (int x = 0; x < TILES; ++x) {
                     // rows 4 g .. 4 g + 3 of the lane's page: the highest of each token's
@@ -113,7 +100,29 @@ __global__ __launch_bounds__(THREADS, (TILES > 1 ? 2 : 3)) void cache_score(cons
                         *out = y;
                     }
                 }
+            };
+            f32x4 sc[TILES];
+            bf16x8 v[KS];
+            load(p0, v);
+            int p = p0;
+#pragma unroll 1
+            for (; p < p1 && p <= seen; p += PAGES) {
+#pragma unroll
+                for (int x = 0; x < TILES; ++x) sc[x] = f32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int s = 0; s < KS; ++s)
+#pragma unroll
+                    for (int x = 0; x < TILES; ++x) sc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[x][s], v[s], sc[x], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+                load(p + PAGES, v);         // (of the last step: pages that are there, and are not used)
+                __builtin_amdgcn_sched_barrier(0);
+                store(p, sc);
             }
+            // what lies behind the visible pages
+#pragma unroll
+            for (int x = 0; x < TILES; ++x) sc[x] = f32x4{0, 0, 0, 0};
+#pragma unroll 1
+            for (; p < p1; p += PAGES) store(p, sc);
         }
         t = end;
     }

@@ -18,7 +18,7 @@ constexpr int COLS = 16;            // columns of a tile
 constexpr int MANY = 4;             // tiles of columns of a workgroup of cache_weigh_stats, where there are many
 constexpr int NEAR = 2, FAR = 4;    // tiles of 16 keys of a wave's step, in cache_weigh_stats and cache_weigh_add
 constexpr int STEP = 16 * NEAR * WAVES;
-constexpr int LISTED = 512;         // columns whose numbers are in LDS at a time
+constexpr int LISTED = 128;         // columns that are in LDS at a time
 constexpr double KEPT = 1 << 30;    // most bytes of scores that are kept
 
 // A sequence's columns that count, and its tokens.
@@ -44,6 +44,8 @@ __device__ __forceinline__ Counted counted(const WeighArgs& a, const int b)
 
 __device__ __forceinline__ Span span_of(const WeighArgs& a, const int b, const int t) { return span_of(a.batch, b, t, a.pool.page_shift, a.causal, a.window); }
 
+__device__ __forceinline__ int uniform(const int v) { return __builtin_amdgcn_readfirstlane(v); }
+
 // Another part's largest score and sum of powers into m and l.
 __device__ __forceinline__ void join(float& m, float& l, const float mo, const float lo)
 {
@@ -52,10 +54,16 @@ __device__ __forceinline__ void join(float& m, float& l, const float mo, const f
     m = mn;
 }
 
+// Of a column: its largest score, in units of the exponent, 1 / the sum of powers, and what it sees.
+struct Joined {
+    float most, inv;
+    Span span;
+};
+
 // scratch: statistics of column (t, query head) and part; behind them scores that are kept, or statistics of columns
 __device__ __forceinline__ float* stat_of(const WeighArgs& a, const int64_t column, const int part) { return a.work + (column * a.parts + part) * 2; }
 __device__ __forceinline__ float* behind_stats(const WeighArgs& a) { return a.work + ((int64_t)a.T * a.group * a.pool.n_heads * a.parts + 1) / 2 * 4; }
-__device__ __forceinline__ float* joined_of(const WeighArgs& a, const int64_t column) { return behind_stats(a) + column * 2; }
+__device__ __forceinline__ Joined* joined_of(const WeighArgs& a, const int64_t column) { return (Joined*)behind_stats(a) + column; }
 __host__ __device__ __forceinline__ int64_t kept_keys(const int64_t keys) { return (keys + STEP - 1) / STEP * STEP; }
 // scores of column c of a sequence's head, all keys
 __device__ __forceinline__ float* kept_of(const WeighArgs& a, const int b, const int h, const int c)
@@ -74,14 +82,16 @@ __device__ __forceinline__ int dim_of(const int s, const int g)
     return TYPE == SPMM_CACHE_S8 ? 64 * (s / 2) + 16 * g + 8 * (s % 2) : 32 * s + 8 * g;
 }
 
-template <int KS, spmm_cache_type_t TYPE>
+template <int KS, spmm_cache_type_t TYPE, bool EXACT>
 __device__ __forceinline__ void load_q(const WeighArgs& a, const int64_t column, const int g, bf16x8 (&q)[KS])
 {
-    const __bf16* const src = a.q + column * a.pool.head_dim;
+    const int D = EXACT ? 32 * KS : a.pool.head_dim;
+    const __bf16* const src = a.q + column * D;
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
         const int d = dim_of<TYPE>(s, g);
-        q[s] = d < a.pool.head_dim ? *(const bf16x8*)(src + d) : bf16x8{};
+        q[s] = *(const bf16x8*)(src + (EXACT || d < D ? d : 0));
+        if (!EXACT && d >= D) q[s] = bf16x8{};
     }
 }
 
@@ -94,7 +104,7 @@ __device__ __forceinline__ bf16x8 codes(const uint32_t lo, const uint32_t hi)
 }
 
 // Keys k0 + 16 t + row of tile t < N, as they lie in the cache; their scales (8 bits) for the rows that the lane has scores of.
-template <int KS, spmm_cache_type_t TYPE, int N>
+template <int KS, spmm_cache_type_t TYPE, bool EXACT, int N>
 struct Keys {
     static constexpr bool S8 = TYPE == SPMM_CACHE_S8;
     static constexpr int PARTS = S8 ? (KS + 1) / 2 : KS;       // of 16 bytes
@@ -102,15 +112,19 @@ struct Keys {
     f32x4 scale[S8 ? N : 1];
     __device__ __forceinline__ void load(const WeighArgs& a, const int32_t* const table, const int h, const int k0, const int last)
     {
-        const int lane = threadIdx.x % 64, row = lane % 16, g = lane / 16, shift = a.pool.page_shift, inside = (1 << shift) - 1, D = a.pool.head_dim;
+        const int lane = threadIdx.x % 64, row = lane % 16, g = lane / 16, shift = a.pool.page_shift, inside = (1 << shift) - 1, D = EXACT ? 32 * KS : a.pool.head_dim;
 #pragma unroll
         for (int t = 0; t < N; ++t) {
             // (16 tokens that start at a multiple of 16 are in one page; those beyond the last lie in its page too)
             const int at = min(k0 + 16 * t, last) & ~15;
             const int64_t slot = (((int64_t)page_in_pool(table[at >> shift], a.pool.n_pages) * a.pool.n_heads + h) << shift) + (at & inside);
-            const char* const src = (const char*)a.pool.k + (slot + row) * D * (S8 ? 1 : 2) + 16 * g;
+            const char* const src = (const char*)a.pool.k + (slot + row) * D * (S8 ? 1 : 2) + (EXACT || 16 * g < D * (S8 ? 1 : 2) ? 16 * g : 0);
 #pragma unroll
-            for (int s = 0; s < PARTS; ++s) v[t][s] = 64 * s + 16 * g < D * (S8 ? 1 : 2) ? *(const u32x4*)(src + 64 * s) : u32x4{0, 0, 0, 0};
+            for (int s = 0; s < PARTS; ++s) {
+                const bool there = EXACT || 64 * s + 16 * g < D * (S8 ? 1 : 2);
+                v[t][s] = *(const u32x4*)(src + (there ? 64 * s : 0));
+                if (!there) v[t][s] = u32x4{0, 0, 0, 0};
+            }
             if constexpr (S8) scale[t] = *(const f32x4*)(a.pool.k_scale + slot + 4 * g);
         }
     }
@@ -131,8 +145,8 @@ struct Keys {
 };
 
 // Scores of TILES tiles of columns: of the lane's column and key k0 + 16 t + 4 g + i.
-template <int KS, spmm_cache_type_t TYPE, int N, int TILES>
-__device__ __forceinline__ void scores_of(const Keys<KS, TYPE, N>& k, const bf16x8 (&q)[TILES][KS], f32x4 (&x)[TILES][N])
+template <int KS, spmm_cache_type_t TYPE, bool EXACT, int N, int TILES>
+__device__ __forceinline__ void scores_of(const Keys<KS, TYPE, EXACT, N>& k, const bf16x8 (&q)[TILES][KS], f32x4 (&x)[TILES][N])
 {
 #pragma unroll
     for (int t = 0; t < N; ++t) {
@@ -150,12 +164,12 @@ __device__ __forceinline__ void scores_of(const Keys<KS, TYPE, N>& k, const bf16
     }
 }
 
-template <int KS, spmm_cache_type_t TYPE, int TILES>
-__global__ __launch_bounds__(THREADS) void cache_weigh_stats(const WeighArgs a)
+template <int KS, spmm_cache_type_t TYPE, bool EXACT, int TILES>
+__global__ __launch_bounds__(THREADS, 2) void cache_weigh_stats(const WeighArgs a)
 {
     constexpr int KEYS = 16 * NEAR;     // of a wave's step
     __shared__ float stat[WAVES][2][TILES * COLS];
-    const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, col = lane % 16, g = lane / 16;
+    const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64), col = lane % 16, g = lane / 16;
     const int H = a.pool.n_heads, G = a.group, part = blockIdx.x % a.parts, h = blockIdx.x / a.parts, b = blockIdx.y;
     const Counted s = counted(a, b);
     const int cols = s.tokens * G;
@@ -173,14 +187,14 @@ __global__ __launch_bounds__(THREADS) void cache_weigh_stats(const WeighArgs a)
 #pragma unroll
         for (int x = 0; x < TILES; ++x) {
             const int c = min(c0 + x * COLS + col, cols - 1);
-            load_q<KS, TYPE>(a, column_of(a, s, h, c), g, q[x]);
+            load_q<KS, TYPE, EXACT>(a, column_of(a, s, h, c), g, q[x]);
             span[x] = span_of(a, b, s.first + c / G);
             m[x] = NONE;
             l[x] = 0.0f;
         }
         const int end = min(key1 - 1, to), last_key = max(s.len - 1, 0);
         int k0 = key0 + wave * KEYS;
-        Keys<KS, TYPE, NEAR> k, next;
+        Keys<KS, TYPE, EXACT, NEAR> k, next;
         if (k0 <= end) next.load(a, table, h, k0, last_key);
         for (; k0 <= end; k0 += STEP) {
             k = next;
@@ -299,95 +313,118 @@ __global__ __launch_bounds__(THREADS) void cache_weigh_kept(const WeighArgs a)
     *(f32x4*)out = w;
 }
 
-// A column's largest score, in units of the exponent, and 1 / the sum of powers.
 __global__ __launch_bounds__(THREADS) void cache_weigh_join(const WeighArgs a)
 {
     const int64_t column = (int64_t)blockIdx.x * THREADS + threadIdx.x;
     if (column >= (int64_t)a.T * a.group * a.pool.n_heads) return;
+    const int t = (int)(column / (a.group * a.pool.n_heads)), b = sequence_of(a.batch, t);
+    if (b < 0) return;
     float top = NONE, sum = 0.0f;
     for (int p = 0; p < a.parts; ++p) {
         const float* const in = stat_of(a, column, p);
         join(top, sum, in[0], in[1]);
     }
-    float* const out = joined_of(a, column);
-    out[0] = top;
-    out[1] = 1.0f / sum;
+    *joined_of(a, column) = Joined{top, 1.0f / sum, span_of(a, b, t)};
 }
 
-// What a column goes by with, in LDS.
-struct Column {
-    int64_t id;
-    float most, inv;
-    Span span;
+// What columns go by with, in LDS: queries (16 bytes between rows, so that the lanes of a tile read from all banks), and numbers.
+template <int KS>
+struct Columns {
+    static constexpr int PITCH = 32 * KS + 8;
+    __bf16 q[LISTED][PITCH];
+    Joined joined[LISTED];
+    int64_t id[LISTED];
 };
 
-template <int KS, spmm_cache_type_t TYPE>
-__global__ __launch_bounds__(THREADS) void cache_weigh_add(const WeighArgs a)
+template <int KS, spmm_cache_type_t TYPE, bool EXACT>
+__global__ __launch_bounds__(THREADS, 2) void cache_weigh_add(const WeighArgs a)
 {
     constexpr int KEYS = 16 * FAR;      // of a wave's step
-    __shared__ Column columns[LISTED];
-    const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, col = lane % 16, g = lane / 16;
+    __shared__ Columns<KS> columns;
+    const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64), col = lane % 16, g = lane / 16;
     const int H = a.pool.n_heads, G = a.group, h = blockIdx.y, b = blockIdx.z, shift = a.pool.page_shift, inside = (1 << shift) - 1;
+    const int D = EXACT ? 32 * KS : a.pool.head_dim;
     const Counted s = counted(a, b);
     const int cols = s.tokens * G;
     if (cols <= 0) return;
     const int32_t* const table = a.batch.table + b * a.batch.ld_table;
-    for (int block = blockIdx.x * KEYS * WAVES; block < s.len; block += gridDim.x * KEYS * WAVES) {
+    const int stride = gridDim.x * KEYS * WAVES;
+    Keys<KS, TYPE, EXACT, FAR> k, next;
+    next.load(a, table, h, blockIdx.x * KEYS * WAVES + wave * KEYS, s.len - 1);
+    for (int block = blockIdx.x * KEYS * WAVES; block < s.len; block += stride) {
         const int k0 = block + wave * KEYS;
-        Keys<KS, TYPE, FAR> k;
-        k.load(a, table, h, k0, s.len - 1);
+        k = next;
+        next.load(a, table, h, block + stride < s.len ? k0 + stride : k0, s.len - 1);
+        __builtin_amdgcn_sched_barrier(0);
         float sum[4 * FAR] = {};
         for (int c0 = 0; c0 < cols; c0 += LISTED) {
             const int n = min(cols - c0, LISTED), rounded = (n + COLS - 1) / COLS * COLS;
             if (cols > LISTED || block == (int)blockIdx.x * KEYS * WAVES) {
+                // (columns that fill the last tile up are the last one, with no share)
                 __syncthreads();        // (the last ones have been read)
-                for (int i = tid; i < rounded; i += THREADS) {
-                    // (columns that fill the last tile up are the last one, with no share)
-                    const int c = c0 + min(i, n - 1);
-                    const int64_t id = column_of(a, s, h, c);
-                    columns[i] = Column{id, joined_of(a, id)[0], i < n ? joined_of(a, id)[1] : 0.0f, span_of(a, b, s.first + c / G)};
+                if (tid < rounded) {
+                    const int64_t id = column_of(a, s, h, c0 + min(tid, n - 1));
+                    Joined x = *joined_of(a, id);
+                    if (tid >= n) x.inv = 0.0f;
+                    columns.joined[tid] = x;
+                    columns.id[tid] = id;
                 }
+                __syncthreads();
+                constexpr int PIECES = 4 * KS;
+                const int d = tid % PIECES * 8;
+                for (int row = tid / PIECES; row < rounded; row += THREADS / PIECES)
+                    *(bf16x8*)&columns.q[row][d] = EXACT || d < D ? *(const bf16x8*)(a.q + columns.id[row] * D + d) : bf16x8{};
                 __syncthreads();
             }
             if (c0 == 0) k.ready();
-            bf16x8 q[1][KS], next[KS];
-            load_q<KS, TYPE>(a, columns[col].id, g, next);
             for (int i = 0; i < rounded; i += COLS) {
+                // what the first and the last column see (no column sees less far than one before it)
+                const int first_from = uniform(columns.joined[i].span.from), first_to = uniform(columns.joined[i].span.to);
+                const int last_from = uniform(columns.joined[i + COLS - 1].span.from), last_to = uniform(columns.joined[i + COLS - 1].span.to);
+                if (k0 > last_to || k0 + KEYS <= first_from) continue;      // (no column of the tile sees any of the keys)
+                bf16x8 q[1][KS];
 #pragma unroll
-                for (int x = 0; x < KS; ++x) q[0][x] = next[x];
-                if (i + COLS < rounded) load_q<KS, TYPE>(a, columns[i + COLS + col].id, g, next);
-                const Span first = columns[i].span, last = columns[i + COLS - 1].span;
-                if (k0 > last.to || k0 + KEYS <= first.from) continue;      // (no column of the tile sees any of the keys)
-                const Column c = columns[i + col];
+                for (int x = 0; x < KS; ++x) q[0][x] = *(const bf16x8*)&columns.q[i + col][dim_of<TYPE>(x, g)];
+                const float most = columns.joined[i + col].most, inv = columns.joined[i + col].inv;
                 f32x4 sc[1][FAR];
                 scores_of(k, q, sc);
-                const bool all = k0 >= last.from && k0 + KEYS - 1 <= first.to;
+                if (k0 >= last_from && k0 + KEYS - 1 <= first_to) {
 #pragma unroll
-                for (int t = 0; t < FAR; ++t)
+                    for (int t = 0; t < FAR; ++t)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float p = __builtin_amdgcn_exp2f(__fmaf_rn(sc[0][t][j], a.scale_log2, -c.most));
-                        if (all) {
-                            sum[4 * t + j] = __fmaf_rn(p, c.inv, sum[4 * t + j]);
-                        } else {
+                        for (int j = 0; j < 4; ++j)
+                            sum[4 * t + j] = __fmaf_rn(__builtin_amdgcn_exp2f(__fmaf_rn(sc[0][t][j], a.scale_log2, -most)), inv, sum[4 * t + j]);
+                } else {
+                    const Span span = columns.joined[i + col].span;
+#pragma unroll
+                    for (int t = 0; t < FAR; ++t)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
                             const int key = k0 + 16 * t + 4 * g + j;
-                            sum[4 * t + j] += key >= c.span.from && key <= c.span.to ? p * c.inv : 0.0f;
+                            const bool sees = key >= span.from && key <= span.to;
+                            const float p = __builtin_amdgcn_exp2f(__fmaf_rn(sc[0][t][j], a.scale_log2, -most));
+                            sum[4 * t + j] = __fmaf_rn(sees ? p : 0.0f, sees ? inv : 0.0f, sum[4 * t + j]);
                         }
-                    }
+                }
             }
         }
-        // over the 16 lanes of a key: each hands the others half of what it has, and is left with the sum of one key
+        // over the 16 lanes of a key: each hands another half of what it has, until it is left with the sum of one key
+        constexpr int SHARED = COLS / (4 * FAR);        // lanes that are left with the same
 #pragma unroll
-        for (int o = 8; o > 0; o >>= 1)
+        for (int o = COLS / 2; o > 0; o >>= 1) {
+            if (o >= SHARED) {
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                if (j >= o) continue;
-                const bool high = col & o;
-                const float give = high ? sum[j] : sum[j + o], keep = high ? sum[j + o] : sum[j];
-                sum[j] = keep + __shfl_xor(give, o);
+                for (int j = 0; j < o / SHARED; ++j) {
+                    const bool high = col & o;
+                    const float give = high ? sum[j] : sum[j + o / SHARED], keep = high ? sum[j + o / SHARED] : sum[j];
+                    sum[j] = keep + __shfl_xor(give, o);
+                }
+            } else {
+                sum[0] += __shfl_xor(sum[0], o);
             }
-        const int key = k0 + 16 * (col / 4) + 4 * g + col % 4;
-        if (key < s.len) {
+        }
+        const int j = col / SHARED, key = k0 + 16 * (j / 4) + 4 * g + j % 4;
+        if (key < s.len && col % SHARED == 0) {
             const int page = table[key >> shift];
             if ((uint32_t)page < (uint32_t)a.pool.n_pages) {
                 float* const w = a.pool.weight + (((int64_t)page * H + h) << shift) + (key & inside);
@@ -405,12 +442,12 @@ struct WeighShape {
 static WeighShape shape_of(const int page_tokens, const int64_t n_seqs, const int64_t ld_table, const int n_heads, const int64_t cols, const int64_t columns)
 {
     const int64_t keys = ld_table * page_tokens, most = (keys + STEP - 1) / STEP, blocks = cols <= COLS ? 1 : (cols + MANY * COLS - 1) / (MANY * COLS);
-    const int64_t want = (cols <= COLS ? 2048 : 1024) / (n_seqs * n_heads * blocks);
+    const int64_t want = (cols <= COLS ? 2048 : 512) / (n_seqs * n_heads * blocks);
     WeighShape f;
     f.parts = (int)(want < 1 ? 1 : want < most ? want : most);
     const double kept = 4.0 * n_seqs * n_heads * cols * kept_keys(keys);
     f.keep = cols <= COLS && kept <= KEPT;
-    f.bytes = (columns * f.parts + 1) / 2 * 16 + (f.keep ? (int64_t)kept : 8 * columns);
+    f.bytes = (columns * f.parts + 1) / 2 * 16 + (f.keep ? (int64_t)kept : (int64_t)sizeof(Joined) * columns);
     return f;
 }
 
@@ -419,19 +456,29 @@ int64_t weigh_work_bytes(const int page_tokens, const int64_t n_seqs, const int6
     return shape_of(page_tokens, n_seqs, ld_table, n_heads, cols, columns).bytes;
 }
 
-template <int KS, spmm_cache_type_t TYPE>
-static int launch_steps(const WeighArgs& a, const int64_t cols, void* stream)
+template <int KS, spmm_cache_type_t TYPE, bool EXACT>
+static int launch_exact(const WeighArgs& a, const int64_t cols, void* stream)
 {
     const int64_t blocks = cols <= COLS ? 1 : (cols + MANY * COLS - 1) / (MANY * COLS), keys = a.batch.ld_table << a.pool.page_shift;
     const dim3 grid((unsigned)(a.parts * a.pool.n_heads), (unsigned)a.batch.n_seqs, (unsigned)(blocks < 65535 ? blocks : 65535)), threads(THREADS);
-    if (const int rc = cols <= COLS ? launch(cache_weigh_stats<KS, TYPE, 1>, grid, threads, a, stream) : launch(cache_weigh_stats<KS, TYPE, MANY>, grid, threads, a, stream)) return rc;
+    if (const int rc = cols <= COLS ? launch(cache_weigh_stats<KS, TYPE, EXACT, 1>, grid, threads, a, stream)
+                                    : launch(cache_weigh_stats<KS, TYPE, EXACT, MANY>, grid, threads, a, stream))
+        return rc;
     const auto blocks_of = [&](const int each) { return dim3((unsigned)((keys + each - 1) / each), (unsigned)a.pool.n_heads, (unsigned)a.batch.n_seqs); };
     if (a.keep) return launch(cache_weigh_kept, blocks_of(4 * THREADS), threads, a, stream);
     const int64_t columns = (int64_t)a.T * a.group * a.pool.n_heads;
     if (const int rc = launch(cache_weigh_join, dim3((unsigned)((columns + THREADS - 1) / THREADS)), threads, a, stream)) return rc;
+    // (a workgroup takes several blocks of keys with the columns it has put together, where there are more blocks than it takes to fill the device)
     dim3 all = blocks_of(16 * FAR * WAVES);
-    if (all.x > 4096) all.x = 4096;
-    return launch(cache_weigh_add<KS, TYPE>, all, threads, a, stream);
+    const int64_t enough = (512 + (int64_t)all.y * all.z - 1) / ((int64_t)all.y * all.z);
+    if (all.x > enough) all.x = (unsigned)enough;
+    return launch(cache_weigh_add<KS, TYPE, EXACT>, all, threads, a, stream);
+}
+
+template <int KS, spmm_cache_type_t TYPE>
+static int launch_steps(const WeighArgs& a, const int64_t cols, void* stream)
+{
+    return a.pool.head_dim == 32 * KS ? launch_exact<KS, TYPE, true>(a, cols, stream) : launch_exact<KS, TYPE, false>(a, cols, stream);
 }
 
 int launch_weigh(const WeighArgs& args, const spmm_cache_type_t type, void* stream)
@@ -441,11 +488,8 @@ int launch_weigh(const WeighArgs& args, const spmm_cache_type_t type, void* stre
     const WeighShape f = shape_of(1 << a.pool.page_shift, a.batch.n_seqs, a.batch.ld_table, a.pool.n_heads, cols, (int64_t)a.T * a.group * a.pool.n_heads);
     a.parts = f.parts;
     a.keep = f.keep;
-    const int dim = a.pool.head_dim;
-    if (type == SPMM_CACHE_S8) return dim > 64 ? launch_steps<4, SPMM_CACHE_S8>(a, cols, stream) : launch_steps<2, SPMM_CACHE_S8>(a, cols, stream);
-    return dim > 96 ? launch_steps<4, SPMM_CACHE_BF16>(a, cols, stream)
-         : dim > 64 ? launch_steps<3, SPMM_CACHE_BF16>(a, cols, stream)
-         : dim > 32 ? launch_steps<2, SPMM_CACHE_BF16>(a, cols, stream) : launch_steps<1, SPMM_CACHE_BF16>(a, cols, stream);
+    if (type == SPMM_CACHE_S8) return a.pool.head_dim > 64 ? launch_steps<4, SPMM_CACHE_S8>(a, cols, stream) : launch_steps<2, SPMM_CACHE_S8>(a, cols, stream);
+    return a.pool.head_dim > 64 ? launch_steps<4, SPMM_CACHE_BF16>(a, cols, stream) : launch_steps<2, SPMM_CACHE_BF16>(a, cols, stream);
 }
 
 }  // namespace spmm_cache

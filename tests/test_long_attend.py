@@ -93,6 +93,28 @@ def test_lists_of_all_lengths(page, pages, cache):
     check(p, random_lists(p, pages))
 
 
+@pytest.mark.parametrize("cache", ["bf16", "s8"])
+@pytest.mark.parametrize("q_heads, kv_heads, dim, new", [(4, 4, 64, 300), (8, 4, 128, 260), (20, 5, 80, 210), (40, 4, 32, 130), (12, 12, 16, 90)])
+@pytest.mark.parametrize("causal, window", [(True, 0), (False, 50), (True, 23)])
+def test_many_lists(q_heads, kv_heads, dim, new, causal, window, cache):
+    """More than a thousand: of two sequences, with columns of no sequence before them, and of none at a position."""
+    p = Long([new, 7], [150, 0], q_heads, kv_heads, dim, 16, cache, lead=1, seed=31)
+    p.lens[1] = 4
+    for pages in (1, 6):
+        check(p, random_lists(p, pages, causal, window, seed=pages), causal=causal, window=window)
+    lists = np.random.default_rng(3).integers(-3, p.width + 2, (p.tokens, kv_heads, 9)).astype(np.int32)
+    check(p, lists, out="bf16", causal=causal, window=window, pad=2)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_windows_behind_what_the_table_names(causal):
+    """Positions beyond the row's width, whose windows begin at its end or behind it: nothing is visible."""
+    p = Long([3], [60], 2, 1, 64, 16, seed=32, width=2)
+    lists = np.tile(np.arange(2, dtype=np.int32), (3, 1, 1))
+    for window in (1, 28, 29, 30, 31, 32, 63):
+        check(p, lists, causal=causal, window=window)
+
+
 @pytest.mark.parametrize("news", [[1], [40, 3]])
 @pytest.mark.parametrize("out, scale, zero", [("bf16", 1, 0), ("s8", 0.02, 3), ("u8", 0.02, 128), ("f32", 1, 0)])
 def test_output_types_and_pitches(news, out, scale, zero):
