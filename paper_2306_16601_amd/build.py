@@ -36,9 +36,10 @@ HEADERS = [os.path.join(CSRC, "spmm_internal.h"), os.path.join(CSRC, "spmm_kerne
 
 CACHE_NATIVE = os.path.join(HERE, "_native_cache.so")
 CACHE_NATIVE_SOURCE = os.path.join(CACHE_CSRC, "native_cache.c")
-CACHE_SOURCES = ["cache_api.cpp", "cache_append.hip", "cache_attend.cpp", "cache_attend_few.hip", "cache_attend_many.hip", "cache_attend_selected.hip",
+CACHE_SOURCES = ["cache_api.cpp", "cache_append.hip", "cache_attend.cpp", "cache_attend_few.hip", "cache_attend_lists.hip", "cache_attend_many.hip", "cache_attend_selected.hip",
                  "cache_bounds.hip", "cache_evict.hip", "cache_pages.hip", "cache_score.hip", "cache_select.hip", "cache_weigh.hip"]
-CACHE_HEADERS = [os.path.join(CACHE_CSRC, "cache_internal.h"), os.path.join(CACHE_CSRC, "cache_attend.h"), os.path.join(CACHE_CSRC, "cache_choose.h"), os.path.join(ROOT, "include", "spmm_cache.h")]
+CACHE_HEADERS = [os.path.join(CACHE_CSRC, "cache_internal.h"), os.path.join(CACHE_CSRC, "cache_attend.h"), os.path.join(CACHE_CSRC, "cache_choose.h"),
+                 os.path.join(CACHE_CSRC, "cache_selected.h"), os.path.join(ROOT, "include", "spmm_cache.h")]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

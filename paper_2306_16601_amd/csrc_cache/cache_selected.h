@@ -1,0 +1,209 @@
+// What the kernels of attention over lists of pages share: a list's pages in LDS, and the queries of a token's heads as operands.
+#pragma once
+
+#include "cache_attend.h"
+
+#include <cfloat>
+
+namespace spmm_cache {
+
+constexpr int SELECTED_WAVES = 4;
+constexpr int SELECTED_THREADS = 64 * SELECTED_WAVES;
+constexpr int SELECTED_COLS = 16;           // columns of a tile
+constexpr int LISTED = 1024;                // pages of a list, or of a part of one, that a workgroup has in LDS
+
+template <spmm_cache_type_t TYPE>
+constexpr int SELECTED_KEYS = TYPE == SPMM_CACHE_S8 ? 64 : 32;      // of a wave's step
+
+// A wave's operands: DIM / 16 registers of 16 bytes a lane for keys, and for values (which tokens and dims they hold: Loads in cache_attend_few.hip).
+template <int DIM, spmm_cache_type_t TYPE>
+struct Selected {
+    static constexpr bool S8 = TYPE == SPMM_CACHE_S8;
+    static constexpr int N = DIM / 16, BYTES = S8 ? 1 : 2, TILES = S8 ? 4 : 2, KS = N / TILES, STEP = SELECTED_KEYS<TYPE>, CHUNK = STEP / 4, ROWS = TILES * 4,
+                         LANE = 16 / BYTES, QUERIES = KS * (S8 ? 2 : 1);
+};
+
+// Whether lists of an 8-bit cache have a wave each (launch_attend_lists) rather than a workgroup or several.  A wave each against a workgroup each, us, 16 pages
+// of 64 of 15 thousand tokens: 32 heads on 8 of 128 dims 1024 lists 41 / 44, 1280 63 / 53, 2048 64 / 75, 2056 88 / 81, 4096 113 / 139, 8192 212 / 267; 16 heads
+// of 64 dims 800 lists 24 / 24, 2048 31 / 41, 8192 87 / 145.  Waves of 128 dims come in rounds of 1024 lists (one on each SIMD) of 24 us after 16, workgroups take 33 ns a list
+// after 9.  (In bfloat16, where no codes are widened, a wave each gains nothing: 2048 lists 127 / 121, 8192 472 / 466.)
+inline bool single(const spmm_cache_type_t type, const int dim, const int64_t lists, const int64_t pages)
+{
+    const int64_t rounds = (lists + 1023) / 1024;
+    return type == SPMM_CACHE_S8 && lists >= 960 && pages <= LISTED / SELECTED_WAVES && (dim <= 64 || lists > 736 * rounds + 215);
+}
+int launch_attend_lists(const SelectedArgs& a, int64_t lists, void* stream);
+
+#if defined(__HIPCC__)
+
+// What a column sees, none of it where a window begins behind its last token.
+__device__ __forceinline__ Span seen_span(const AttendArgs& a, const int b, const int t)
+{
+    const Span s = span_of(a.batch, b, t, a.pool.page_shift, a.causal, a.window);
+    return s.from <= s.to ? s : Span{0, -1};
+}
+
+// Page `id` of a row: its number in the pool and the position of its first token, -1 where there is no such page; *visible: whether
+// some token of it is.
+__device__ __forceinline__ int2 listed_page(const AttendArgs& a, const int32_t* const table, const int id, const Span span, bool* const visible)
+{
+    const int shift = a.pool.page_shift;
+    *visible = false;
+    if (id < 0 || id >= a.batch.ld_table) return int2{0, -1};
+    const int first = id << shift;
+    *visible = first <= span.to && first + (1 << shift) - 1 >= span.from;
+    return int2{page_in_pool(table[id], a.pool.n_pages), first};
+}
+
+// The operand of a column's queries; returns what scores are multiplied by.
+template <int DIM, spmm_cache_type_t TYPE, int QUERIES>
+__device__ __forceinline__ float load_queries(const AttendArgs& a, const __bf16* const src, const bool there, const int D, const int g, u32x4 (&q)[QUERIES])
+{
+    using L = Selected<DIM, TYPE>;
+    if constexpr (L::S8) {
+        // (brought to [1, 2) by a power of two, as binary16 holds them)
+        float most = 0.0f;
+        u32x4 raw[QUERIES];
+#pragma unroll
+        for (int i = 0; i < QUERIES; ++i) {
+            const int d = 64 * (i / 2) + 16 * g + 8 * (i % 2);
+            raw[i] = there && d < D ? *(const u32x4*)(src + d) : u32x4{0, 0, 0, 0};
+            const bf16x8 v = __builtin_bit_cast(bf16x8, raw[i]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf((float)v[j]));
+        }
+        most = fmaxf(most, __shfl_xor(most, 16));
+        most = fmaxf(most, __shfl_xor(most, 32));
+        float up;
+        const float down = to_unit(most, &up);
+#pragma unroll
+        for (int i = 0; i < QUERIES; ++i) {
+            const bf16x8 v = __builtin_bit_cast(bf16x8, raw[i]);
+            f16x8 w;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = (_Float16)((float)v[j] * down);
+            q[i] = __builtin_bit_cast(u32x4, w);
+        }
+        return fmaxf(a.scale_log2 * up, FLT_TRUE_MIN);      // (never 0, which what is hidden, -inf, must not be multiplied by)
+    } else {
+#pragma unroll
+        for (int i = 0; i < QUERIES; ++i) {
+            const int d = 32 * i + 8 * g;
+            q[i] = there && d < D ? *(const u32x4*)(src + d) : u32x4{0, 0, 0, 0};
+        }
+        return a.scale_log2;
+    }
+}
+
+// A step's scores, of tokens 16 g + 4 t + i (8 bits) or 8 g + 4 t + i (bfloat16) of it.
+template <int DIM, spmm_cache_type_t TYPE, int QUERIES>
+__device__ __forceinline__ void selected_scores(const u32x4 (&k)[DIM / 16], const u32x4 (&q)[QUERIES], f32x4 (&sc)[Selected<DIM, TYPE>::TILES])
+{
+    using L = Selected<DIM, TYPE>;
+#pragma unroll
+    for (int t = 0; t < L::TILES; ++t) {
+        sc[t] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < L::KS; ++i) {
+            const u32x4 r = k[t * L::KS + i];
+            if constexpr (L::S8) {
+                sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen(r[0], r[1]), __builtin_bit_cast(f16x8, q[2 * i]), sc[t], 0, 0, 0);
+                sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen(r[2], r[3]), __builtin_bit_cast(f16x8, q[2 * i + 1]), sc[t], 0, 0, 0);
+            } else {
+                sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, r), __builtin_bit_cast(bf16x8, q[i]), sc[t], 0, 0, 0);
+            }
+        }
+        if constexpr (L::S8) __builtin_amdgcn_sched_barrier(0);     // (or all codes are widened first, and their registers spilled)
+    }
+}
+
+// A step's values times its weights.
+template <int DIM, spmm_cache_type_t TYPE>
+__device__ __forceinline__ void selected_values(const u32x4 (&v)[DIM / 16], const u32x4 (&w)[Selected<DIM, TYPE>::S8 ? 2 : 1], f32x4 (&o)[DIM / 16])
+{
+#pragma unroll
+    for (int d = 0; d < DIM / 16; ++d) {
+        if constexpr (TYPE == SPMM_CACHE_S8) {
+            o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen(v[d][0], v[d][1]), __builtin_bit_cast(f16x8, w[0]), o[d], 0, 0, 0);
+            o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen(v[d][2], v[d][3]), __builtin_bit_cast(f16x8, w[1]), o[d], 0, 0, 0);
+        } else {
+            o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v[d]), __builtin_bit_cast(bf16x8, w[0]), o[d], 0, 0, 0);
+        }
+        if (TYPE == SPMM_CACHE_S8 && d % 2) __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+// Values of tokens that are hidden, from position `first` on, which may hold anything, as 0.
+template <int N>
+__device__ __forceinline__ void hide_values(u32x4 (&v)[N], const int first, const Span span)
+{
+    u32x4 keep;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int i = first + 2 * j;
+        keep[j] = (i >= span.from && i <= span.to ? 0xffffu : 0u) | (i + 1 >= span.from && i + 1 <= span.to ? 0xffff0000u : 0u);
+    }
+#pragma unroll
+    for (int d = 0; d < N; ++d) v[d] &= keep;
+}
+
+// Weights as operands, and their sum (of the rounded ones in bfloat16, which are what values are multiplied by).
+template <spmm_cache_type_t TYPE, int ROWS>
+__device__ __forceinline__ void pack_weights(const float (&y)[ROWS], u32x4 (&w)[TYPE == SPMM_CACHE_S8 ? 2 : 1], float& sum)
+{
+    if constexpr (TYPE == SPMM_CACHE_S8) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            f16x8 f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] = (_Float16)y[8 * e + j];
+            w[e] = __builtin_bit_cast(u32x4, f);
+        }
+    } else {
+        bf16x8 f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = (__bf16)y[j];
+        w[0] = __builtin_bit_cast(u32x4, f);
+        sum = sum_of(f, sum);
+    }
+}
+
+// The power of two that weights are divided by, which follows the largest of the values' scales.
+struct ValueUnit {
+    float up = __builtin_bit_cast(float, 2u << 23), down = __builtin_bit_cast(float, 252u << 23);
+    // returns what results so far are multiplied by; vs: scales of what is visible, 0 of what is not
+    template <int ROWS>
+    __device__ __forceinline__ float follow(const float (&vs)[ROWS])
+    {
+        float most = 0.0f;
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) most = fmaxf(most, fabsf(vs[i]));
+        most = fmaxf(most, __shfl_xor(most, 16));
+        most = fmaxf(most, __shfl_xor(most, 32));
+        if (!(most <= FLT_MAX)) most = FLT_MAX;
+        float new_up;
+        const float new_down = to_unit(most, &new_up);
+        if (!(new_up > up)) return 1.0f;
+        const float less = up * new_down;
+        up = new_up;
+        down = new_down;
+        return less;
+    }
+};
+
+// An infinite scale makes infinities of both signs of a key's codes, whose score is NaN.
+template <int ROWS>
+__device__ __forceinline__ void key_scales(float (&ks)[ROWS])
+{
+    float most = 0.0f;
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) most = fmaxf(most, fabsf(ks[i]));
+    if (__any(most > FLT_MAX)) {
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) ks[i] = fabsf(ks[i]) > FLT_MAX ? __builtin_nanf("") : ks[i];
+    }
+}
+
+#endif
+
+}  // namespace spmm_cache
