@@ -60,29 +60,38 @@ __device__ __forceinline__ Border border_of(const E& each, uint32_t need, Bins<W
 {
     using B = Bins<WAVES>;
     const int tid = threadIdx.x % (64 * WAVES), lane = tid % 64, wave = tid / 64;
-    // the lowest and the highest
+    // The highest, and a value that at least `need` reach: the lowest of the threads' highest ones, where there are no more to choose than
+    // threads and each has a value, and the lowest of all otherwise.
     uint32_t lo = 0xffffffffu, hi = 0;
-    each([&](const uint32_t v) {
-        lo = min(lo, v - 1);        // (of no value it is the highest number)
-        hi = max(hi, v);
-    });
-    for (int i = 1; i < 64; i <<= 1) {
-        lo = min(lo, (uint32_t)__shfl_xor((int)lo, i));
-        hi = max(hi, (uint32_t)__shfl_xor((int)hi, i));
-    }
-    if constexpr (WAVES > 1) {
-        if (lane == 0) {
-            bins.ends[wave][0] = lo;
-            bins.ends[wave][1] = hi;
+    const auto ends = [&] {
+        for (int i = 1; i < 64; i <<= 1) {
+            lo = min(lo, (uint32_t)__shfl_xor((int)lo, i));
+            hi = max(hi, (uint32_t)__shfl_xor((int)hi, i));
         }
-        __syncthreads();
-        for (int w = 0; w < WAVES; ++w) {
-            lo = min(lo, bins.ends[w][0]);
-            hi = max(hi, bins.ends[w][1]);
+        if constexpr (WAVES > 1) {
+            __syncthreads();
+            if (lane == 0) {
+                bins.ends[wave][0] = lo;
+                bins.ends[wave][1] = hi;
+            }
+            __syncthreads();
+            for (int w = 0; w < WAVES; ++w) {
+                lo = min(lo, bins.ends[w][0]);
+                hi = max(hi, bins.ends[w][1]);
+            }
         }
+        lo = of_lane(lo, 0);
+        hi = of_lane(hi, 0);
+    };
+    each([&](const uint32_t v) { hi = max(hi, v); });
+    lo = need <= 64 * WAVES ? hi : 0;
+    ends();
+    if (lo == 0) {
+        lo = 0xffffffffu;
+        each([&](const uint32_t v) { lo = min(lo, v - 1); });       // (of no value it is the highest number)
+        ends();
+        ++lo;
     }
-    lo = of_lane(lo, 0) + 1;
-    hi = of_lane(hi, 0);
 
     while (lo < hi) {
         const int shift = max(32 - B::LOG - __builtin_clz(hi - lo), 0);
