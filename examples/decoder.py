@@ -5,7 +5,10 @@ spmm_cache_attend (u8)  ->  spmm_run (output projection, quantised for the next 
 library's order, rows = features; between steps spmm_cache_fork moves the beams on and spmm_cache_compact tidies the pool.
 Weights are random and pruned in 4x1 blocks; there is no feed-forward part and no vocabulary, a step's input is random codes.
 
-    python examples/decoder.py          runs it and prints the steps' times
+`long_contexts` is another run of it: prompts whose attention is added up (spmm_cache_weigh) and that are cut down to the tokens that were
+attended to most (spmm_cache_evict), then tokens that read lists of a few pages (spmm_cache_bounds, _score, _select, _attend_selected).
+
+    python examples/decoder.py          runs both and prints the steps' times
 """
 from __future__ import annotations
 
@@ -34,7 +37,7 @@ def pruned(rng, rows, cols):
 
 
 class Decoder:
-    def __init__(self, pages: int, cache="bf16", seed: int = 0):
+    def __init__(self, pages: int, cache="bf16", seed: int = 0, long=False):
         rng = np.random.default_rng(seed)
         dev = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()      # noqa: E731
         self.qkv_rows = (HEADS + 2 * KV_HEADS) * DIM
@@ -45,17 +48,20 @@ class Decoder:
         self.to_qkv = sp.make_epilogue(qkv_scale, SCALE, ZERO, out_type="f32")
         self.to_hidden = sp.make_epilogue(out_scale, SCALE, ZERO, out_type="u8", out_scale=SCALE, out_zero_point=ZERO)
         weights = [dev(rng.uniform(0.5, 1.5, DIM).astype(np.float32)) for _ in range(2)]
-        self.how = sp.make_append(HEADS, "f32", 1.0, 0, weights[0], weights[1], 1e-6, sp.make_rope(4096, DIM).cuda(), False)
+        self.how = lambda positions, rope=sp.make_rope(4096, DIM).cuda(): sp.make_append(HEADS, "f32", 1.0, 0, *weights, 1e-6, rope, False, positions)     # noqa: E731
         shape = (LAYERS, pages, KV_HEADS)
         kind = torch.int8 if cache == "s8" else torch.bfloat16
         scales = [torch.empty((*shape, PAGE), device="cuda") if cache == "s8" else None for _ in range(2)]
-        self.cache = sp.make_cache(torch.empty((*shape, PAGE, DIM), dtype=kind, device="cuda"), torch.empty((*shape, DIM, PAGE), dtype=kind, device="cuda"), *scales)
+        more = [torch.empty((*shape, 2, DIM), dtype=torch.bfloat16, device="cuda"), torch.empty((*shape, PAGE), device="cuda")] if long else []
+        self.cache = sp.make_cache(torch.empty((*shape, PAGE, DIM), dtype=kind, device="cuda"), torch.empty((*shape, DIM, PAGE), dtype=kind, device="cuda"), *scales, *more)
         self.work = torch.empty(sp.spmm_cache_work_bytes(self.cache, 256), dtype=torch.uint8, device="cuda")
         self.info = torch.empty(4, dtype=torch.int32, device="cuda")
 
-    def step(self, x, new, table, kv_len):
+    def step(self, x, new, table, kv_len, positions=None, weighed=0, listed=0):
         """x [HIDDEN][T] u8: the new tokens of all sequences, new[b] each, the last ones of kv_len[b] -> the last layer's
-        output in u8, and the attention of the last layer in binary32, [HEADS * DIM][T]."""
+        output in u8, and the attention of the last layer in binary32, [HEADS * DIM][T].
+        positions: where they are rotated to; weighed: the attention of so many of each sequence's last ones is added up; listed: each reads
+        so many pages of its sequence."""
         T, stream = x.shape[1], torch.cuda.current_stream().cuda_stream
         start = torch.tensor(np.concatenate(([0], np.cumsum(new))).astype(np.int32), device="cuda")
         batch = sp.make_batch(start, kv_len, table)
@@ -65,13 +71,32 @@ class Decoder:
         exact = torch.empty((HEADS * DIM, T), device="cuda")
         attend = sp.make_attend(HEADS, max(new), DIM ** -0.5, True, 0, "u8", SCALE, ZERO)
         look = sp.make_attend(HEADS, max(new), DIM ** -0.5, True, 0, "f32")
-        work = torch.empty(sp.spmm_attend_work_bytes(self.cache, len(new), T, attend), dtype=torch.uint8, device="cuda")
+        weigh, select = sp.make_weigh(HEADS, max(weighed, 1), DIM ** -0.5), sp.make_select(HEADS, max(listed, 2))
+        need = [sp.spmm_selected_work_bytes(self.cache, T, attend, listed) if listed else sp.spmm_attend_work_bytes(self.cache, len(new), T, attend)]
+        need += [sp.spmm_weigh_work_bytes(self.cache, batch, T, weigh)] if weighed else []
+        work = torch.empty(max(need), dtype=torch.uint8, device="cuda")
+        scores = torch.empty((T, KV_HEADS, table.shape[1]), device="cuda")
+        lists = torch.empty((T, KV_HEADS, max(listed, 1)), dtype=torch.int32, device="cuda")
+        how = self.how(positions)
+
+        def read(i, as_, out):
+            if listed:
+                sp.spmm_cache_attend_selected(self.cache, i, batch, q, T, as_, lists, listed, out, T, work, stream)
+            else:
+                sp.spmm_cache_attend(self.cache, i, batch, q, T, as_, out, T, work, stream)
+
         for i in range(LAYERS):
             sp.spmm_run(self.qkv[i], x, T, T, self.to_qkv, qkv, T, stream)
-            sp.spmm_cache_append(self.cache, i, batch, qkv, T, T, self.how, q, stream)
-            sp.spmm_cache_attend(self.cache, i, batch, q, T, attend, mid, T, work, stream)
+            sp.spmm_cache_append(self.cache, i, batch, qkv, T, T, how, q, stream)
+            if weighed:
+                sp.spmm_cache_weigh(self.cache, i, batch, q, T, weigh, work, stream)
+            if listed:
+                sp.spmm_cache_bounds(self.cache, i, batch, T, stream)
+                sp.spmm_cache_score(self.cache, i, batch, q, T, select, scores, scores.shape[2], stream)
+                sp.spmm_cache_select(self.cache, batch, scores, T, scores.shape[2], select, lists, stream)
+            read(i, attend, mid)
             if i == LAYERS - 1:
-                sp.spmm_cache_attend(self.cache, i, batch, q, T, look, exact, T, work, stream)
+                read(i, look, exact)
             x = torch.empty((HIDDEN, T), dtype=torch.uint8, device="cuda")
             sp.spmm_run(self.out[i], mid, T, T, self.to_hidden, x, T, stream)
         return x, exact
@@ -85,6 +110,17 @@ class Decoder:
 
     def compact(self, table):
         sp.spmm_cache_compact(self.cache, table, table, self.info, self.work, torch.cuda.current_stream().cuda_stream)
+
+    def cut(self, table, kv_len, room):
+        """All rows cut down to `room` tokens, in their pages, and the bounds of what stays: the new lengths."""
+        n, stream = table.shape[0], torch.cuda.current_stream().cuda_stream
+        kept, len_out = torch.empty((LAYERS, n, KV_HEADS, room), dtype=torch.int32, device="cuda"), torch.empty(n, dtype=torch.int32, device="cuda")
+        keep = torch.full((n,), room, dtype=torch.int32, device="cuda")
+        sp.spmm_cache_evict(self.cache, table, kv_len, keep, sp.make_evict(4, 16, room), table, len_out, kept, stream)
+        start = torch.cat((torch.zeros(1, dtype=torch.int32, device="cuda"), len_out.cumsum(0, dtype=torch.int32)))
+        for i in range(LAYERS):
+            sp.spmm_cache_bounds(self.cache, i, sp.make_batch(start, len_out, table), n * room, stream)
+        return len_out
 
     def close(self):
         for h in self.qkv + self.out:
@@ -134,5 +170,32 @@ def main(prompts=(70, 33), beams=4, steps=6, cache="bf16", tell=print):
     return codes, last.cpu(), used
 
 
+def long_contexts(prompts=(200, 90), steps=6, room=96, listed=2, cache="bf16", tell=print):
+    """Prompts at once, cut down to `room` tokens each, then tokens that read `listed` pages; returns the sequences' codes, what the last step
+    attended to, and the tokens that the cache holds."""
+    rng = np.random.default_rng(2)
+    model = Decoder(pages=64, cache=cache, long=True)
+    n, width = len(prompts), 8
+    ints = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")      # noqa: E731
+    codes = [rng.integers(0, 256, (HIDDEN, p)).astype(np.uint8) for p in prompts]
+    table, _ = model.fork(torch.full((n, width), -1, dtype=torch.int32, device="cuda"), ints([0] * n), [-1] * n, [0] * n, list(prompts))
+    model.step(columns(codes), list(prompts), table, ints(list(prompts)), weighed=32)
+    held, at = model.cut(table, ints(list(prompts)), room).cpu().tolist(), list(prompts)
+    tell("%s tokens of %s stay" % (held, at))
+    for step in range(steps):
+        table, _ = model.fork(table, ints(held), list(range(n)), held, [k + 1 for k in held])      # (and what is free of the pages that were cut)
+        held = [k + 1 for k in held]
+        token = rng.integers(0, 256, (HIDDEN, n)).astype(np.uint8)
+        codes = [np.concatenate((c, token[:, j:j + 1]), axis=1) for j, c in enumerate(codes)]
+        began = time.perf_counter()
+        _, last = model.step(torch.from_numpy(token).cuda(), [1] * n, table, ints(held), ints(at), listed=listed)
+        torch.cuda.synchronize()
+        at = [a + 1 for a in at]
+        tell("token %d, %d pages each: %.2f ms, %d pages in use" % (step, listed, 1e3 * (time.perf_counter() - began), model.info.cpu().tolist()[2]))
+    model.close()
+    return codes, last.cpu(), held
+
+
 if __name__ == "__main__":
     main()
+    long_contexts()
