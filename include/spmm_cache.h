@@ -174,13 +174,16 @@ spmm_status_t spmm_cache_work_bytes(const spmm_cache_t *cache, int64_t n_rows, i
  * A step of new tokens   spmm_cache_append -> spmm_cache_bounds -> spmm_cache_score -> spmm_cache_select ->
  * spmm_cache_attend_selected   reads the pages of a list for each new token and key/value head instead of all of them.
  * spmm_cache_weigh adds up what attention each token gets, and spmm_cache_evict keeps the tokens that got most of it.
+ * Limits (else SPMM_E_UNSUPPORTED): 65535 sequences or rows in spmm_cache_bounds, _weigh and _evict, T * n_heads <= 2^22 and lists of up to 2^20
+ * pages in spmm_cache_score, _select and _attend_selected (2^40 numbers of lists in all), lds <= 2^30, n_layers * n_heads <= 2^20 in spmm_cache_evict.
  * "Visible" is what it is in spmm_cache_attend (kv_len, causal, window), token by token; columns at a negative position see nothing. */
 
 /* Bounds of the pages that the batch's new tokens lie in (of layer `layer`): of each head and dim the largest and the
  * smallest of the keys' values (code * scale in S8 caches, in binary32, rounded to bfloat16) of all tokens of the page below kv_len;
  * where one of them is not finite, both are NaN.  The call follows spmm_cache_append of the same batch.  A batch that says that all
  * tokens of its sequences are new (q_start[b + 1] - q_start[b] = kv_len[b]) has all of their pages' bounds made again, as after an
- * eviction.  T: columns of the batch; a number that is too small or too large costs time and nothing else. */
+ * eviction.  (Pages that fork copies and cuts keep the bounds of all their tokens, which hold for those that are left, until new ones come to them.)
+ * T: columns of the batch; a number that is too small or too large costs time and nothing else. */
 spmm_status_t spmm_cache_bounds(const spmm_cache_t *cache, int32_t layer, const spmm_batch_t *batch, int64_t T, void *hip_stream);
 
 /* Which pages a new token reads. */
@@ -237,8 +240,8 @@ spmm_status_t spmm_weigh_work_bytes(const spmm_cache_t *cache, const spmm_batch_
  *               softmax over the visible tokens of scale * (q_t . k)   at j  (0 where j is not visible).
  * So weights need no initialisation.  Sequences without a new token are left as they were.  Scores, statistics and sums are binary32, and nothing
  * is rounded to less (codes of S8 caches are exact in the products, and scales are on the scores).  A score of NaN or +inf makes its column's weights NaN,
- * and so do scores of -inf alone.  The order of the sums does not change from call to call.  A page that two rows name gets the weights of one of them
- * (of a call with both; which one is not said).  q: as for spmm_cache_attend.  work: spmm_weigh_work_bytes bytes, as for attend. */
+ * and so do scores of -inf alone.  The order of the sums does not change from call to call.  The weights of a page that two rows with new tokens
+ * both name are not defined after a call with both of them.  q: as for spmm_cache_attend.  work: spmm_weigh_work_bytes bytes, as for attend. */
 spmm_status_t spmm_cache_weigh(const spmm_cache_t *cache, int32_t layer, const spmm_batch_t *batch, const void *q, int64_t T,
                                const spmm_weigh_t *how, void *work, void *hip_stream);
 

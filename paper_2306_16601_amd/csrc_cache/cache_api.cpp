@@ -127,6 +127,15 @@ spmm_status_t check_lists(const spmm_cache_t* c, int64_t T, int64_t pages)
     return pages > MOST_PAGES || T * c->n_heads > MOST_LISTS || T * c->n_heads > MOST_LISTED / pages ? SPMM_E_UNSUPPORTED : SPMM_OK;
 }
 
+spmm_status_t check_selected(const spmm_cache_t* c, int64_t T, const spmm_attend_t* how, int64_t pages, int64_t* bytes)
+{
+    if (const spmm_status_t s = check_lists(c, T, pages)) return s;
+    const int64_t n = selected_work_bytes(c->type, c->page_tokens, T, c->n_heads, how->q_heads / c->n_heads, c->head_dim, pages);
+    if (n < 0) return SPMM_E_UNSUPPORTED;
+    *bytes = n;
+    return SPMM_OK;
+}
+
 spmm_status_t check_attend(const spmm_cache_t* c, int64_t T, const spmm_attend_t* how)
 {
     if (!how || how->max_new < 1) return SPMM_E_ARG;
@@ -405,9 +414,7 @@ spmm_status_t spmm_selected_work_bytes(const spmm_cache_t* cache, int64_t T, con
     if (const spmm_status_t s = check_cache(cache)) return s;
     if (!bytes || pages < 1) return SPMM_E_ARG;
     if (const spmm_status_t s = check_attend(cache, T, how)) return s;
-    if (const spmm_status_t s = check_lists(cache, T, pages)) return s;
-    *bytes = selected_work_bytes(cache->type, cache->page_tokens, T, cache->n_heads, how->q_heads / cache->n_heads, cache->head_dim, pages);
-    return SPMM_OK;
+    return check_selected(cache, T, how, pages, bytes);
 }
 
 spmm_status_t spmm_cache_attend_selected(const spmm_cache_t* cache, int32_t layer, const spmm_batch_t* batch, const void* q, int64_t T,
@@ -421,7 +428,8 @@ spmm_status_t spmm_cache_attend_selected(const spmm_cache_t* cache, int32_t laye
         return SPMM_E_ARG;
     if (const spmm_status_t s = check_attend(cache, T, how)) return s;
     if (const spmm_status_t s = check_how(how, out, ldo)) return s;
-    if (const spmm_status_t s = check_lists(cache, T, pages)) return s;
+    int64_t bytes;
+    if (const spmm_status_t s = check_selected(cache, T, how, pages, &bytes)) return s;
     SelectedArgs a = {};
     a.attend = attend_of(cache, layer, batch, q, T, how, out, ldo, work);
     a.lists = lists;

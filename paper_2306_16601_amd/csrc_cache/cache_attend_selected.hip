@@ -248,6 +248,7 @@ static int parts_of(const spmm_cache_type_t type, const int dim, const int page_
 int64_t selected_work_bytes(const spmm_cache_type_t type, const int page_tokens, const int64_t T, const int n_heads, const int group, const int dim, const int64_t pages)
 {
     const int64_t lists = T * n_heads * ((group + COLS - 1) / COLS), parts = parts_of(type, dim, page_tokens, lists, pages);
+    if (lists * parts >= (int64_t)1 << 24) return -1;       // (a grid has less than 2^32 threads)
     return parts == 1 ? 16 : 4 * lists * parts * part_floats(dim > 64 ? 128 : 64);
 }
 

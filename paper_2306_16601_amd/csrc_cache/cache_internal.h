@@ -135,6 +135,7 @@ int launch_copy(const CopyArgs& a, void* stream);
 int launch_bounds(const BoundsArgs& a, spmm_cache_type_t type, int64_t T, void* stream);
 int launch_score(const ScoreArgs& a, void* stream);
 int launch_select(const SelectArgs& a, void* stream);
+// -1: more parts of lists than a grid holds
 int64_t selected_work_bytes(spmm_cache_type_t type, int page_tokens, int64_t T, int n_heads, int group, int dim, int64_t pages);
 int launch_attend_selected(const SelectedArgs& a, spmm_cache_type_t type, void* stream);
 int64_t weigh_work_bytes(int page_tokens, int64_t n_seqs, int64_t ld_table, int n_heads, int64_t cols, int64_t columns);

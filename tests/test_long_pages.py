@@ -66,6 +66,12 @@ def test_bounds_of_sequences_that_are_not_there():
     bounds(p)
 
 
+def test_bounds_of_any_number_of_columns():
+    """The number of columns only says how many workgroups are wanted: of 64 heads more than a grid holds."""
+    for T in (1, 40, 1 << 20, 1 << 40):
+        bounds(Long([30, 0, 5], [50, 9, 14], 64, 64, 16, 16, seed=62), T)
+
+
 def score(p, causal=True, window=0, pad=0):
     cache, batch = p.on_device()
     T, H, lds = max(1, p.tokens), p.k.shape[2], p.width + pad

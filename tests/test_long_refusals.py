@@ -100,6 +100,10 @@ def test_attend_operands():
     assert f(CACHE, 0, ATTEND, 5, n) == f(CACHE, 9, None, 5, n) == f(CACHE, 9, ATTEND, 0, n) == f(CACHE, 9, ATTEND, 5, None) == ARG
     assert f(CACHE, 9, ATTEND, 1 << 21, n) == UNSUPPORTED
     assert f(CACHE, 9, ATTEND, 5, n) == sp.SPMM_OK and n.value > 0
+    # lists in more parts than a grid has workgroups: 2^24, and 512 columns of 4 heads have 8 tiles each, in 1024 parts
+    wide = changed(ATTEND, q_heads=512)
+    assert f(CACHE, 1 << 18, wide, 1 << 20, n) == selected(T=1 << 18, ldo=1 << 18, how=wide, pages=1 << 20) == UNSUPPORTED
+    assert f(CACHE, 512, wide, 1 << 20, n) == UNSUPPORTED and f(CACHE, 511, wide, 1 << 20, n) == sp.SPMM_OK
 
 
 @pytest.mark.parametrize("want, change", [
