@@ -29,7 +29,7 @@ __global__ __launch_bounds__(THREADS) void cache_bounds(const BoundsArgs a)
 {
     constexpr bool S8 = TYPE == SPMM_CACHE_S8;
     constexpr int N = S8 ? 16 : 8;      // dims of a lane
-    const int b = blockIdx.y, lane = threadIdx.x % 64, shift = a.pool.page_shift, H = a.pool.n_heads, D = a.pool.head_dim;
+    const int b = blockIdx.x, lane = threadIdx.x % 64, shift = a.pool.page_shift, H = a.pool.n_heads, D = a.pool.head_dim;
     const int len = tokens_of(a.batch, b, shift);
     const int64_t new_tokens = (int64_t)a.batch.q_start[b + 1] - a.batch.q_start[b], past = (int64_t)a.batch.kv_len[b] - new_tokens;
     if (new_tokens <= 0 || past >= len) return;
@@ -37,7 +37,7 @@ __global__ __launch_bounds__(THREADS) void cache_bounds(const BoundsArgs a)
     const int wide = D / N, deep = 64 / wide, c = lane % wide, r = lane / wide;
     const int64_t all = (int64_t)pages * H;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    for (int64_t w = (int64_t)blockIdx.x * WAVES + wave; w < all; w += (int64_t)gridDim.x * WAVES) {
+    for (int64_t w = (int64_t)blockIdx.y * WAVES + wave; w < all; w += (int64_t)gridDim.y * WAVES) {
         const int i = first + (int)(w / H), h = (int)(w % H);
         const int page = a.batch.table[b * a.batch.ld_table + i];
         if ((uint32_t)page >= (uint32_t)a.pool.n_pages) continue;
@@ -152,7 +152,9 @@ int launch_bounds(const BoundsArgs& a, const spmm_cache_type_t type, const int64
     const int64_t n = a.batch.n_seqs, most = ((T >> a.pool.page_shift) + 2) * a.pool.n_heads, all = ((T >> a.pool.page_shift) + 2 * n) * a.pool.n_heads;
     const int64_t share = all / n > 2048 / n * WAVES ? all / n : 2048 / n * WAVES, heads = most < share ? most : share;
     const int64_t groups = (heads + WAVES - 1) / WAVES;
-    const dim3 grid((unsigned)(groups < 1 << 20 ? groups : 1 << 20), (unsigned)n);
+    // (sequences side by side: the device deals workgroups to its XCDs in turn, and the first ones of each sequence are those with work; 64
+    // prompts of 100 tokens 4.7 us, 16.4 the other way round.  1024 to 4096 workgroups at least make no difference of 0.7 us.)
+    const dim3 grid((unsigned)n, (unsigned)(groups < 65535 ? groups : 65535));
     return type == SPMM_CACHE_S8 ? launch(cache_bounds<SPMM_CACHE_S8>, grid, dim3(THREADS), a, stream) : launch(cache_bounds<SPMM_CACHE_BF16>, grid, dim3(THREADS), a, stream);
 }
 

@@ -8,6 +8,10 @@
 // cache_weigh_add a wave has keys in its registers, the columns go by, and each key's shares are summed up, first in a lane, then over the lanes of
 // its row.  Every weight is one thread's, so that there are no atomics, and sums have one order.  Products are exact: queries are bfloat16, and so are
 // codes of 8 bits once they are widened (integers up to 256 have 8 bits).
+//
+// 64 sequences of up to 8192 tokens, 32 heads on 8 of 128 dims, a new token each: 143 us for the statistics (4.2 TB/s of keys) and 16 for the
+// kept scores' shares; 32 tokens of 2 prompts of 16 thousand (256 columns): 22.7 + 4.2 + 28.5, where the keys are read twice (14 us each time at the
+// rate of a copy), and latencies, not the instructions, are what is left.
 #include "cache_attend.h"
 
 namespace spmm_cache {
@@ -16,10 +20,10 @@ constexpr int WAVES = 4;
 constexpr int THREADS = 64 * WAVES;
 constexpr int COLS = 16;            // columns of a tile
 constexpr int MANY = 4;             // tiles of columns of a workgroup of cache_weigh_stats, where there are many
-constexpr int NEAR = 2, FAR = 4;    // tiles of 16 keys of a wave's step, in cache_weigh_stats and cache_weigh_add
+constexpr int NEAR = 2;             // tiles of 16 keys of a wave's step in cache_weigh_stats
 constexpr int STEP = 16 * NEAR * WAVES;
 constexpr int LISTED = 128;         // columns that are in LDS at a time
-constexpr double KEPT = 1 << 30;    // most bytes of scores that are kept
+constexpr double KEPT = 1 << 30;    // most bytes of scores that are kept: a limit of scratch, beyond which a call of few columns takes the other way too
 
 // A sequence's columns that count, and its tokens.
 struct Counted {
@@ -336,10 +340,12 @@ struct Columns {
     int64_t id[LISTED];
 };
 
-template <int KS, spmm_cache_type_t TYPE, bool EXACT>
+// FAR: tiles of 16 keys of a wave's step
+template <int KS, spmm_cache_type_t TYPE, bool EXACT, int FAR>
 __global__ __launch_bounds__(THREADS, 2) void cache_weigh_add(const WeighArgs a)
 {
     constexpr int KEYS = 16 * FAR;      // of a wave's step
+    constexpr int TILES = FAR == 1 ? 4 : 1, TILED = TILES * COLS;      // tiles of columns that are multiplied together
     __shared__ Columns<KS> columns;
     const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64), col = lane % 16, g = lane / 16;
     const int H = a.pool.n_heads, G = a.group, h = blockIdx.y, b = blockIdx.z, shift = a.pool.page_shift, inside = (1 << shift) - 1;
@@ -358,7 +364,7 @@ __global__ __launch_bounds__(THREADS, 2) void cache_weigh_add(const WeighArgs a)
         __builtin_amdgcn_sched_barrier(0);
         float sum[4 * FAR] = {};
         for (int c0 = 0; c0 < cols; c0 += LISTED) {
-            const int n = min(cols - c0, LISTED), rounded = (n + COLS - 1) / COLS * COLS;
+            const int n = min(cols - c0, LISTED), rounded = (n + TILED - 1) / TILED * TILED;
             if (cols > LISTED || block == (int)blockIdx.x * KEYS * WAVES) {
                 // (columns that fill the last tile up are the last one, with no share)
                 __syncthreads();        // (the last ones have been read)
@@ -377,34 +383,41 @@ __global__ __launch_bounds__(THREADS, 2) void cache_weigh_add(const WeighArgs a)
                 __syncthreads();
             }
             if (c0 == 0) k.ready();
-            for (int i = 0; i < rounded; i += COLS) {
+            for (int i = 0; i < rounded; i += TILED) {
                 // what the first and the last column see (no column sees less far than one before it)
                 const int first_from = uniform(columns.joined[i].span.from), first_to = uniform(columns.joined[i].span.to);
-                const int last_from = uniform(columns.joined[i + COLS - 1].span.from), last_to = uniform(columns.joined[i + COLS - 1].span.to);
-                if (k0 > last_to || k0 + KEYS <= first_from) continue;      // (no column of the tile sees any of the keys)
-                bf16x8 q[1][KS];
+                const int last_from = uniform(columns.joined[i + TILED - 1].span.from), last_to = uniform(columns.joined[i + TILED - 1].span.to);
+                if (k0 > last_to || k0 + KEYS <= first_from) continue;      // (no column of the tiles sees any of the keys)
+                bf16x8 q[TILES][KS];
 #pragma unroll
-                for (int x = 0; x < KS; ++x) q[0][x] = *(const bf16x8*)&columns.q[i + col][dim_of<TYPE>(x, g)];
-                const float most = columns.joined[i + col].most, inv = columns.joined[i + col].inv;
-                f32x4 sc[1][FAR];
+                for (int c = 0; c < TILES; ++c)
+#pragma unroll
+                    for (int x = 0; x < KS; ++x) q[c][x] = *(const bf16x8*)&columns.q[i + c * COLS + col][dim_of<TYPE>(x, g)];
+                f32x4 sc[TILES][FAR];
                 scores_of(k, q, sc);
-                if (k0 >= last_from && k0 + KEYS - 1 <= first_to) {
+                const bool whole = k0 >= last_from && k0 + KEYS - 1 <= first_to;
 #pragma unroll
-                    for (int t = 0; t < FAR; ++t)
+                for (int c = 0; c < TILES; ++c) {
+                    const Joined& column = columns.joined[i + c * COLS + col];
+                    const float most = column.most, inv = column.inv;
+                    if (whole) {
 #pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            sum[4 * t + j] = __fmaf_rn(__builtin_amdgcn_exp2f(__fmaf_rn(sc[0][t][j], a.scale_log2, -most)), inv, sum[4 * t + j]);
-                } else {
-                    const Span span = columns.joined[i + col].span;
+                        for (int t = 0; t < FAR; ++t)
 #pragma unroll
-                    for (int t = 0; t < FAR; ++t)
+                            for (int j = 0; j < 4; ++j)
+                                sum[4 * t + j] = __fmaf_rn(__builtin_amdgcn_exp2f(__fmaf_rn(sc[c][t][j], a.scale_log2, -most)), inv, sum[4 * t + j]);
+                    } else {
+                        const Span span = column.span;
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const int key = k0 + 16 * t + 4 * g + j;
-                            const bool sees = key >= span.from && key <= span.to;
-                            const float p = __builtin_amdgcn_exp2f(__fmaf_rn(sc[0][t][j], a.scale_log2, -most));
-                            sum[4 * t + j] = __fmaf_rn(sees ? p : 0.0f, sees ? inv : 0.0f, sum[4 * t + j]);
-                        }
+                        for (int t = 0; t < FAR; ++t)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const int key = k0 + 16 * t + 4 * g + j;
+                                const bool sees = key >= span.from && key <= span.to;
+                                const float p = __builtin_amdgcn_exp2f(__fmaf_rn(sc[c][t][j], a.scale_log2, -most));
+                                sum[4 * t + j] = __fmaf_rn(sees ? p : 0.0f, sees ? inv : 0.0f, sum[4 * t + j]);
+                            }
+                    }
                 }
             }
         }
@@ -442,10 +455,13 @@ struct WeighShape {
 static WeighShape shape_of(const int page_tokens, const int64_t n_seqs, const int64_t ld_table, const int n_heads, const int64_t cols, const int64_t columns)
 {
     const int64_t keys = ld_table * page_tokens, most = (keys + STEP - 1) / STEP, blocks = cols <= COLS ? 1 : (cols + MANY * COLS - 1) / (MANY * COLS);
-    const int64_t want = (cols <= COLS ? 2048 : 512) / (n_seqs * n_heads * blocks);
+    // Workgroups in all.  Few columns: 64 sequences of up to 8192 tokens of all lengths 143 us with 2048, 164 with 1024; 4 tokens of one of 60 thousand 43
+    // and 39 (more parts, more to join).  Many: 128 columns a head of 2 times 16 thousand 28 us (with the join) with 256, 30 with 512, 37 with 1024, 54 with 2048.
+    const int64_t want = (cols <= COLS ? 2048 : 256) / (n_seqs * n_heads * blocks);
     WeighShape f;
     f.parts = (int)(want < 1 ? 1 : want < most ? want : most);
     const double kept = 4.0 * n_seqs * n_heads * cols * kept_keys(keys);
+    // (with kept scores against without, us: 64 single tokens of 8 thousand each 252 / 414, one 12 / 33, 4 of 60 thousand 43 / 87)
     f.keep = cols <= COLS && kept <= KEPT;
     f.bytes = (columns * f.parts + 1) / 2 * 16 + (f.keep ? (int64_t)kept : (int64_t)sizeof(Joined) * columns);
     return f;
@@ -468,11 +484,15 @@ static int launch_exact(const WeighArgs& a, const int64_t cols, void* stream)
     if (a.keep) return launch(cache_weigh_kept, blocks_of(4 * THREADS), threads, a, stream);
     const int64_t columns = (int64_t)a.T * a.group * a.pool.n_heads;
     if (const int rc = launch(cache_weigh_join, dim3((unsigned)((columns + THREADS - 1) / THREADS)), threads, a, stream)) return rc;
-    // (a workgroup takes several blocks of keys with the columns it has put together, where there are more blocks than it takes to fill the device)
-    dim3 all = blocks_of(16 * FAR * WAVES);
-    const int64_t enough = (512 + (int64_t)all.y * all.z - 1) / ((int64_t)all.y * all.z);
+    // A workgroup takes several blocks of keys with the columns it has put together, where there are more blocks than it takes to fill the device (128
+    // columns a head of 2 times 16 thousand keys: 28 us with 512 workgroups, 34 with 256, 37 with 2048); where there are fewer it takes blocks of 64 keys, and
+    // multiplies four tiles of columns together (1024 tokens on 2048 keys 138 us against 228, 32 on 4000 8.7 against 13; from 288 blocks on the larger
+    // ones are ahead, 26 against 29).
+    dim3 all = blocks_of(16 * 4 * WAVES);
+    const int64_t others = (int64_t)all.y * all.z, enough = (512 + others - 1) / others;
+    if (all.x * others < 256) return launch(cache_weigh_add<KS, TYPE, EXACT, 1>, blocks_of(16 * WAVES), threads, a, stream);
     if (all.x > enough) all.x = (unsigned)enough;
-    return launch(cache_weigh_add<KS, TYPE, EXACT>, all, threads, a, stream);
+    return launch(cache_weigh_add<KS, TYPE, EXACT, 4>, all, threads, a, stream);
 }
 
 template <int KS, spmm_cache_type_t TYPE>
