@@ -248,6 +248,16 @@ def test_weights_of_long_ones(news, pasts):
     check_weights(Long(news, pasts, 2, 1, 128, 128, "s8", seed=24), max_new=20)
 
 
+@pytest.mark.parametrize("cache", ["bf16", "s8"])
+@pytest.mark.parametrize("q_heads, kv_heads, dim", [(32, 8, 64), (32, 8, 128), (32, 8, 80), (160, 8, 16)])
+@pytest.mark.parametrize("causal, window", [(True, 0), (False, 0), (True, 300)])
+def test_weights_of_many_keys_and_columns(q_heads, kv_heads, dim, causal, window, cache):
+    """Enough blocks of keys for the larger ones, and several of them for a workgroup."""
+    check_weights(Long([5, 0, 6, 5, 5, 40, 5, 5], [900, 17, 1100, 3, 640, 1023, 511, 70], q_heads, kv_heads, dim, 64, cache, seed=31), causal=causal, window=window)
+    if dim == 64:
+        check_weights(Long([6] * 8, [250 * i + 1700 for i in range(8)], q_heads, kv_heads, dim, 64, cache, seed=32), causal=causal, window=window)
+
+
 @pytest.mark.parametrize("decay", [0.0, 0.25, 1.0])
 def test_what_stays_of_earlier_weights(decay):
     p = Long([2, 0, 5], [100, 30, 0], 4, 2, 64, 16, seed=25)

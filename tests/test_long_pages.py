@@ -97,10 +97,15 @@ def test_scores(q_heads, kv_heads, dim, causal, window):
     score(Long([3, 0, 70, 17, 1], [0, 5, 31, 130, 64], q_heads, kv_heads, dim, 32, layers=2, layer=1, lead=2, seed=7), causal, window, pad=3)
 
 
-@pytest.mark.parametrize("q_heads, kv_heads, dim", HEADS)
+@pytest.mark.parametrize("q_heads, kv_heads, dim", HEADS + [(4, 2, 64), (6, 3, 128)])
 @pytest.mark.parametrize("causal, window", [(True, 0), (False, 0), (True, 200)])
 def test_scores_of_many_columns(q_heads, kv_heads, dim, causal, window):
     score(Long([300, 20, 0, 130], [700, 0, 5, 64], q_heads, kv_heads, dim, 16, lead=3, seed=61), causal, window, pad=2)
+
+
+def test_scores_of_two_heads_each():
+    score(Long([1] * 6, [0, 1, 31, 32, 200, 1000], 4, 2, 64, 16, seed=63))
+    score(Long([3, 0, 9, 7, 1], [0, 5, 31, 130, 64], 6, 3, 112, 32, seed=64))
 
 
 def test_scores_of_many_pages_and_columns():
