@@ -197,7 +197,7 @@ typedef struct {
 } spmm_select_t;
 
 /* scores[t][h][i] (device, binary32 [T][n_heads][lds], lds >= ld_table, 4-byte aligned): of every column t, key/value head h and
- * page i of its sequence's row with a visible token, an upper bound of the products q . k of the page's keys:
+ * page i of its sequence's row with a visible token, an upper bound (in S8 caches but for the bounds' rounding) of the products q . k of the page's keys:
  *   max over the query heads of h of   sum_d q_d > 0 ? q_d hi_d : q_d lo_d,
  * binary32 sums of products of the bounds hi, lo; NaN where a bound is.  Pages without a visible token, up to ld_table: -inf.  Columns of no
  * sequence are left as they were.  q: as for spmm_cache_attend.  (pages, first and last are not read, but checked.) */

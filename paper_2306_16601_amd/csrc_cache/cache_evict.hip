@@ -7,8 +7,10 @@
 // lane.  Values, whose tokens are contiguous, are gathered one by one, tokens side by side in a wave, so that it finds them in a few lines
 // of memory: nearly all lines of the values are read wherever one token in sixteen stays.
 //
-// 8 rows of up to 12 thousand tokens in 8 bits, 8 layers of 8 heads of 128 dims, to 2048 each: 33 us to choose, 235 to move (0.94 GB with the lines that are
-// read whole, 4.0 TB/s); 4 rows of 1000, 12 layers of 12 heads of 64 dims, to 250: 8.8 and 26.4.
+// 8 rows of up to 12 thousand tokens in 8 bits, 8 layers of 8 heads of 128 dims, to 2048 each: 33 us to choose, 235 to move (405 MB read and 288
+// written by the counters, 2.9 TB/s: the vector unit is busy a quarter of the time, and
+// loads, byte picks and barriers wait for each other); 4 rows of 1000, 12 layers of 12 heads of 64 dims in
+// bfloat16, to 250: 8.8 and 26.4 (130 MB with the lines that are read whole, 4.9 TB/s).
 #include "cache_choose.h"
 
 #include <type_traits>

@@ -107,12 +107,14 @@ class Long(Problem):
 
     def selected_wanted(self, lists, scale, causal=True, window=0):
         out = np.full((self.q_heads, self.dim, max(1, self.tokens)), np.nan)
-        mag = out.copy()
+        mag, rows = out.copy(), {}
         for t, b, at in self.columns():
             lo, hi = self.span(b, at, causal, window)
             for h in range(self.q_heads):
                 kv = h // self.group
-                k, v = self.keys(b, kv), self.values(b, kv)
+                if (b, kv) not in rows:
+                    rows[b, kv] = self.keys(b, kv), self.values(b, kv)
+                k, v = rows[b, kv]
                 j = np.concatenate([np.arange(i * self.page, (i + 1) * self.page) for i in lists[t, kv] if 0 <= i < self.width] or [np.zeros(0, int)]).astype(int)
                 j = j[(j >= lo) & (j <= hi)]
                 if not len(j):
