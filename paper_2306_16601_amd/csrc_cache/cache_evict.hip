@@ -7,10 +7,9 @@
 // lane.  Values, whose tokens are contiguous, are gathered one by one, tokens side by side in a wave, so that it finds them in a few lines
 // of memory: nearly all lines of the values are read wherever one token in sixteen stays.
 //
-// 8 rows of up to 12 thousand tokens in 8 bits, 8 layers of 8 heads of 128 dims, to 2048 each: 33 us to choose, 235 to move (405 MB read and 288
-// written by the counters, 2.9 TB/s: the vector unit is busy a quarter of the time, and
-// loads, byte picks and barriers wait for each other); 4 rows of 1000, 12 layers of 12 heads of 64 dims in
-// bfloat16, to 250: 8.8 and 26.4 (130 MB with the lines that are read whole, 4.9 TB/s).
+// 8 rows of up to 12 thousand tokens in 8 bits, 8 layers of 8 heads of 128 dims, to 2048 each: 33 us to choose, 226 to move (405 MB read and 288
+// written by the counters, 3.1 TB/s; without the picks it takes as long, with more workgroups on a CU too: it is the memory's answer to runs of 64 bytes to 1 KB); 4 rows of 1000, 12 layers of 12 heads of 64 dims in
+// bfloat16, to 250: 8.5 and 25.4 (130 MB with the lines that are read whole, 5 TB/s).
 #include "cache_choose.h"
 
 #include <type_traits>
@@ -95,8 +94,9 @@ struct Moved {
 __device__ __forceinline__ Moved moved(const EvictArgs& a, const int slices)
 {
     Moved m;
-    const int lh = blockIdx.x / slices, H = a.pool.n_heads;
-    m.slice = blockIdx.x % slices;
+    // (a head's slices one after the other on one XCD, which workgroups are dealt to in turn: 8 rows in 8 bits 226 us against 235 with slices side by side)
+    const int heads = gridDim.x / slices, lh = blockIdx.x % heads, H = a.pool.n_heads;
+    m.slice = blockIdx.x / heads;
     m.h = lh % H;
     m.layer = lh / H;
     m.b = blockIdx.y;
