@@ -1,11 +1,12 @@
-// Attention over lists of pages of an 8-bit cache where there are enough of them for a wave each: chunks of prompts, whose tokens have lists of their own.
+// Attention over lists of pages of an 8-bit cache where there are enough of them for a wave each, or for four: chunks of prompts, whose tokens have lists
+// of their own.
 //
 // What the waves read is in the L2 then, and the vector unit bounds them: widening codes, and the softmax, which would be computed for 16 columns
 // of the matrix instruction whether they are there or not.  So the columns that a token's heads leave free take other keys: with G heads (padded to
 // a power of two) 16 / G steps of keys, streams, are multiplied one after the other, each column picks its own stream's scores, and one softmax serves all of
 // them.  Streams have maxima and sums of their own, and values are multiplied stream by stream, by weights that are 0 in the other
 // streams' columns (a value that is not finite reaches them as NaN, but they are the same heads, which see it too).  At the end
-// the streams of a head are joined by shuffles.  Keys and values of the next step are on their way while a wave works on this one's; the workgroups are
+// the streams of a head are joined by shuffles, and the waves of a list in LDS.  Keys and values of the next step are on their way while a wave works on this one's; the workgroups are
 // dealt out so that lists of the same head run on the same XCD, whose cache they share.
 #include "cache_selected.h"
 
@@ -14,28 +15,28 @@ namespace spmm_cache {
 constexpr int WAVES = SELECTED_WAVES, THREADS = SELECTED_THREADS, COLS = SELECTED_COLS;
 constexpr int XCDS = 8;
 
-// STREAMS: an even number of them, else one
-template <int DIM, bool EXACT, bool STREAMS>
+// STREAMS: an even number of them, else one; SHARE: waves of a list, 1 or all of a workgroup
+template <int DIM, bool EXACT, bool STREAMS, int SHARE>
 __global__ __launch_bounds__(THREADS, 2) void cache_attend_lists(const SelectedArgs args, const int log_group)
 {
     constexpr spmm_cache_type_t TYPE = SPMM_CACHE_S8;
     using L = Selected<DIM, TYPE>;
     constexpr int N = L::N, KS = L::KS, STEP = L::STEP, CHUNK = L::CHUNK, ROWS = L::ROWS, LANE = L::LANE;
-    __shared__ int2 all_listed[WAVES][LISTED / WAVES];
+    __shared__ int2 all_listed[WAVES / SHARE][LISTED / WAVES * SHARE];
 
     const AttendArgs& a = args.attend;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 16, g = lane / 16;
     const int D = EXACT ? DIM : a.pool.head_dim, G = a.group, H = a.pool.n_heads, shift = a.pool.page_shift, inside = (1 << shift) - 1;
     const int tiles = (G + COLS - 1) / COLS;
     // lists head by head; the device deals workgroups to the XCDs in turn
-    const int each = gridDim.x / XCDS, list = (int)(blockIdx.x % XCDS * each + blockIdx.x / XCDS) * WAVES + wave;
+    const int each = gridDim.x / XCDS, list = (int)(blockIdx.x % XCDS * each + blockIdx.x / XCDS) * (WAVES / SHARE) + wave / SHARE;
     if (list >= a.T * H * tiles) return;
     const int t = list % a.T, h = list / a.T % H, tile = list / a.T / H;
     const int b = sequence_of(a.batch, t);
     if (b < 0) return;
     const Span span = seen_span(a, b, t);
 
-    int2* const listed = all_listed[wave];
+    int2* const listed = all_listed[wave / SHARE];      // (waves that share a list all write the same)
     const int32_t* const ids = args.lists + ((int64_t)t * H + h) * args.pages;
     const int32_t* const table = a.batch.table + b * a.batch.ld_table;
     int end = 0;
@@ -62,7 +63,7 @@ __global__ __launch_bounds__(THREADS, 2) void cache_attend_lists(const SelectedA
 
     const int k_end = end << shift, last = max(end - 1, 0), steps = (k_end + STEP - 1) / STEP;
     // steps of keys that share a softmax (behind the last one there are steps of nothing)
-    const int width = STREAMS ? min(COLS >> log_group, (steps + 1) & ~1) : 1;
+    const int width = STREAMS ? min(COLS >> log_group, ((steps + SHARE - 1) / SHARE + 1) & ~1) : 1;
     const int chunk_k = CHUNK * (col >> 2), chunk_v = CHUNK * g;
     const char* const k_base = (const char*)a.pool.k + (col & 3) * D + LANE * g;
     const char* const v_base = (const char*)a.pool.v + ((int64_t)col << shift);
@@ -89,8 +90,9 @@ __global__ __launch_bounds__(THREADS, 2) void cache_attend_lists(const SelectedA
     };
 
     u32x4 even[N], odd[N];
-    if (steps) load(0, false, even);
-    for (int base = 0; base < steps; base += width) {
+    const int begin = SHARE > 1 ? wave * width : 0;
+    if (begin < steps) load(begin, false, even);
+    for (int base = begin; base < steps; base += SHARE * width) {
         // the lane's own tokens of these steps
         int page, off;
         int first = first_of(base + stream, &page, &off);
@@ -156,7 +158,7 @@ __global__ __launch_bounds__(THREADS, 2) void cache_attend_lists(const SelectedA
             for (int e = 0; e < 2; ++e) mine[e] = !STREAMS || stream == x ? w[e] : u32x4{0, 0, 0, 0};
             selected_values<DIM, TYPE>(v, mine, o);
         };
-        const int after = base + width < steps ? base + width : 0;      // (behind the last one something that is there, and not used)
+        const int after = base + SHARE * width < steps ? base + SHARE * width : 0;      // (behind the last one something that is there, and not used)
         if constexpr (STREAMS) {
 #pragma unroll 1
             for (int x = 0; x < width; x += 2) {
@@ -197,34 +199,69 @@ __global__ __launch_bounds__(THREADS, 2) void cache_attend_lists(const SelectedA
     const float share = __builtin_amdgcn_exp2f(m - (top == NONE ? 0.0f : top));
     l *= share;
     for (int i = 1 << log_group; i < COLS; i <<= 1) l += __shfl_xor(l, i);
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l, mine = share * values.up, nothing = of_nothing(0, end - 1);
+    const float nothing = of_nothing(0, end - 1), mine = share * values.up;
+    if constexpr (SHARE == 1) {
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
-    for (int d = 0; d < N; ++d)
+        for (int d = 0; d < N; ++d)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            float y = o[d][e] * mine;
-            for (int i = 1 << log_group; i < COLS; i <<= 1) y += __shfl_xor(y, i);
-            const int row = 16 * d + 4 * g + e;
-            if (there && stream == 0 && row < D) store_out(a, (((int64_t)h * G + column) * D + row) * a.ldo + t, l == 0.0f ? nothing : y * inv);
+            for (int e = 0; e < 4; ++e) {
+                float y = o[d][e] * mine;
+                for (int i = 1 << log_group; i < COLS; i <<= 1) y += __shfl_xor(y, i);
+                const int row = 16 * d + 4 * g + e;
+                if (there && stream == 0 && row < D) store_out(a, (((int64_t)h * G + column) * D + row) * a.ldo + t, l == 0.0f ? nothing : y * inv);
+            }
+    } else {
+        // then the waves
+        __shared__ float part[WAVES][N * 4][64], stat[WAVES][2][COLS];
+        if (g == 0) {
+            stat[wave][0][col] = top;
+            stat[wave][1][col] = l;
         }
+        __syncthreads();
+        float most = NONE, all = 0.0f;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) most = fmaxf(most, stat[i][0][col]);
+        const float ms = most == NONE ? 0.0f : most;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) all += stat[i][1][col] * __builtin_amdgcn_exp2f(stat[i][0][col] - ms);
+        const float scaled = mine * __builtin_amdgcn_exp2f(top - ms);
+#pragma unroll
+        for (int d = 0; d < N; ++d)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) part[wave][d * 4 + e][lane] = o[d][e] * scaled;
+        __syncthreads();
+        const float inv = all == 0.0f ? 0.0f : 1.0f / all;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const int i = wave + WAVES * j, row = 16 * (i / 4) + 4 * g + i % 4;
+            float y = 0.0f;
+#pragma unroll
+            for (int x = 0; x < WAVES; ++x) y += part[x][i][lane];
+            for (int k = 1 << log_group; k < COLS; k <<= 1) y += __shfl_xor(y, k);
+            if (there && stream == 0 && row < D) store_out(a, (((int64_t)h * G + column) * D + row) * a.ldo + t, all == 0.0f ? nothing : y * inv);
+        }
+    }
 }
 
-template <int DIM>
+template <int DIM, int SHARE>
 static int launch_dim(const SelectedArgs& a, const int64_t lists, void* stream)
 {
     int log_group = 0;
     while (1 << log_group < a.attend.group && 1 << log_group < COLS) ++log_group;
-    const int64_t groups = (lists + WAVES - 1) / WAVES;
+    const int64_t groups = (lists + WAVES / SHARE - 1) / (WAVES / SHARE);
     void* args[] = {const_cast<SelectedArgs*>(&a), &log_group};
     const bool streams = 2 << log_group <= COLS;
-    const void* const kernel = a.attend.pool.head_dim == DIM ? streams ? (const void*)cache_attend_lists<DIM, true, true> : (const void*)cache_attend_lists<DIM, true, false>
-                                                             : streams ? (const void*)cache_attend_lists<DIM, false, true> : (const void*)cache_attend_lists<DIM, false, false>;
+    const void* const kernel = a.attend.pool.head_dim == DIM
+                                   ? streams ? (const void*)cache_attend_lists<DIM, true, true, SHARE> : (const void*)cache_attend_lists<DIM, true, false, SHARE>
+                                   : streams ? (const void*)cache_attend_lists<DIM, false, true, SHARE> : (const void*)cache_attend_lists<DIM, false, false, SHARE>;
     return (int)hipLaunchKernel(kernel, dim3((unsigned)((groups + XCDS - 1) / XCDS * XCDS)), dim3(THREADS), args, 0, (hipStream_t)stream);
 }
 
-int launch_attend_lists(const SelectedArgs& a, const int64_t lists, void* stream)
+int launch_attend_lists(const SelectedArgs& a, const int64_t lists, const bool shared, void* stream)
 {
-    return a.attend.pool.head_dim > 64 ? launch_dim<128>(a, lists, stream) : launch_dim<64>(a, lists, stream);
+    if (shared) return a.attend.pool.head_dim > 64 ? launch_dim<128, WAVES>(a, lists, stream) : launch_dim<64, WAVES>(a, lists, stream);
+    return a.attend.pool.head_dim > 64 ? launch_dim<128, 1>(a, lists, stream) : launch_dim<64, 1>(a, lists, stream);
 }
 
 }  // namespace spmm_cache

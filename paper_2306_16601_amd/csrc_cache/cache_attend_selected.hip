@@ -238,7 +238,7 @@ __global__ __launch_bounds__(THREADS) void cache_join_selected(const SelectedArg
 // Workgroups that share a list: as many as fill the device, but none without a unit of keys.
 static int parts_of(const spmm_cache_type_t type, const int dim, const int page_tokens, const int64_t lists, const int64_t pages)
 {
-    if (single(type, dim, lists, pages)) return 1;
+    if (waves_of(type, dim, lists, pages)) return 1;
     const int unit = WAVES * (type == SPMM_CACHE_S8 ? SELECTED_KEYS<SPMM_CACHE_S8> : SELECTED_KEYS<SPMM_CACHE_BF16>);
     const int64_t units = (pages * page_tokens + unit - 1) / unit, want = CUS * PER_CU / lists, least = (pages + LISTED - 1) / LISTED;
     const int64_t most = units < pages ? units : pages, n = want < 1 ? 1 : want < most ? want : most;
@@ -266,7 +266,7 @@ int launch_attend_selected(const SelectedArgs& args, const spmm_cache_type_t typ
     SelectedArgs a = args;
     const int64_t lists = (int64_t)a.attend.T * a.attend.pool.n_heads * ((a.attend.group + COLS - 1) / COLS);
     const int dim = a.attend.pool.head_dim;
-    if (single(type, dim, lists, a.pages)) return launch_attend_lists(a, lists, stream);
+    if (const int waves = waves_of(type, dim, lists, a.pages)) return launch_attend_lists(a, lists, waves > 1, stream);
     a.parts = parts_of(type, dim, 1 << a.attend.pool.page_shift, lists, a.pages);
     if (dim > 64)
         return type == SPMM_CACHE_S8 ? launch_dim<128, SPMM_CACHE_S8>(a, lists, stream) : launch_dim<128, SPMM_CACHE_BF16>(a, lists, stream);

@@ -23,16 +23,20 @@ struct Selected {
                          LANE = 16 / BYTES, QUERIES = KS * (S8 ? 2 : 1);
 };
 
-// Whether lists of an 8-bit cache have a wave each (launch_attend_lists) rather than a workgroup or several.  A wave each against a workgroup each, us, 16 pages
-// of 64 of 15 thousand tokens: 32 heads on 8 of 128 dims 1024 lists 41 / 44, 1280 63 / 53, 2048 64 / 75, 2056 88 / 81, 4096 113 / 139, 8192 212 / 267; 16 heads
-// of 64 dims 800 lists 24 / 24, 2048 31 / 41, 8192 87 / 145.  Waves of 128 dims come in rounds of 1024 lists (one on each SIMD) of 24 us after 16, workgroups take 33 ns a list
-// after 9.  (In bfloat16, where no codes are widened, a wave each gains nothing: 2048 lists 127 / 121, 8192 472 / 466.)
-inline bool single(const spmm_cache_type_t type, const int dim, const int64_t lists, const int64_t pages)
+// Waves that a list of an 8-bit cache has in launch_attend_lists, 1 or 4, or 0: it goes to the workgroups of cache_attend_selected.  One wave / four / those, us,
+// 16 pages of 64 of 15 thousand tokens: 32 heads on 8 of 128 dims 128 lists 37 / 14 / 17, 256 37 / 15 / 20, 768 39 / 33 / 35, 1024 40 / 41 / 43, 1280 62 / 49 / 53,
+// 2048 66 / 73 / 79, 2056 90 / 81 / 84, 4096 121 / 136 / 149, 8192 232 / 263 / 291; 64 pages 128 lists 110 / 33 / 29, 256 111 / 34 / 43, 2056 294 / 227 / 260; 16 heads of 64
+// dims 256 lists 21 / 10 / 14, 1024 23 / 23 / 25, 2048 31 / 38 / 44; 32 heads on 2, which leave no columns free, 256 lists 67 / 24 / 30, 4096 272 / 291 / 279.  Waves of 128 dims
+// come in rounds of 1024 lists (one on each SIMD) of 24 us after 16, workgroups take 32 ns a list after 9.  (In bfloat16, where no codes are
+// widened, a wave each gains nothing: 2048 lists 127 / - / 121, 8192 472 / - / 466.)
+inline int waves_of(const spmm_cache_type_t type, const int dim, const int64_t lists, const int64_t pages)
 {
     const int64_t rounds = (lists + 1023) / 1024;
-    return type == SPMM_CACHE_S8 && lists >= 960 && pages <= LISTED / SELECTED_WAVES && (dim <= 64 || lists > 736 * rounds + 215);
+    if (type != SPMM_CACHE_S8) return 0;
+    if (lists >= 960 && pages <= LISTED / SELECTED_WAVES && (dim <= 64 || lists > 736 * rounds + 215)) return 1;
+    return lists >= 256 && pages <= LISTED ? SELECTED_WAVES : 0;
 }
-int launch_attend_lists(const SelectedArgs& a, int64_t lists, void* stream);
+int launch_attend_lists(const SelectedArgs& a, int64_t lists, bool shared, void* stream);
 
 #if defined(__HIPCC__)
 

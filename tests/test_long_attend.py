@@ -106,6 +106,23 @@ def test_many_lists(q_heads, kv_heads, dim, new, causal, window, cache):
     check(p, lists, out="bf16", causal=causal, window=window, pad=2)
 
 
+@pytest.mark.parametrize("cache", ["bf16", "s8"])
+@pytest.mark.parametrize("q_heads, kv_heads, dim, new", [(4, 4, 64, 70), (8, 4, 128, 65), (20, 5, 80, 60), (40, 2, 96, 45), (12, 12, 16, 22), (16, 2, 48, 140), (32, 2, 128, 130)])
+@pytest.mark.parametrize("page, pages", [(16, 40), (64, 9), (32, 1)])
+def test_lists_of_a_workgroup_each(q_heads, kv_heads, dim, new, page, pages, cache):
+    """A few hundred lists, shorter and longer than the steps of a workgroup's waves."""
+    for causal, window in ((True, 0), (False, 50)):
+        p = Long([new, 3], [600, 20], q_heads, kv_heads, dim, page, cache, seed=66)
+        lists = random_lists(p, pages, causal, window, seed=67)
+        lists[1], lists[2, 0, 1:] = -1, -1
+        check(p, lists, causal=causal, window=window)
+
+
+def test_lists_of_many_pages():
+    p = Long([130], [3000], 2, 2, 32, 16, "s8", seed=68)
+    check(p, random_lists(p, 1000, seed=69))
+
+
 @pytest.mark.parametrize("causal", [True, False])
 def test_windows_behind_what_the_table_names(causal):
     """Positions beyond the row's width, whose windows begin at its end or behind it: nothing is visible."""
