@@ -45,7 +45,7 @@ __global__ __launch_bounds__(64 * W, (REGS > 16 ? 4 : 8)) void cache_evict_choos
     __shared__ Bins<W> bins;
     __shared__ int totals[(REGS ? REGS : 1) * W][2];
     const int H = a.pool.n_heads, h = blockIdx.x % H, layer = blockIdx.x / H, b = blockIdx.y;
-    const int shift = a.pool.page_shift, inside = (1 << shift) - 1, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int shift = a.pool.page_shift, inside = (1 << shift) - 1;
     const Stay s = stay_of(a, b);
     int32_t* const kept = a.kept + (((int64_t)layer * a.n_rows + b) * H + h) * a.most;
     if (blockIdx.x == 0 && threadIdx.x == 0) a.kv_len_out[b] = s.n;
@@ -66,12 +66,12 @@ __global__ __launch_bounds__(64 * W, (REGS > 16 ? 4 : 8)) void cache_evict_choos
         return;
     }
     if constexpr (REGS > 0) {
+        // (behind the last token its weight is loaded again: loads that may be left out come one after the other)
         uint32_t v[REGS];
 #pragma unroll
-        for (int k = 0; k < REGS; ++k) {
-            const int i = (k * W + wave) * 64 + lane;
-            v[k] = i < n ? rank(i) : 0;
-        }
+        for (int k = 0; k < REGS; ++k) v[k] = rank(min(k * 64 * W + (int)threadIdx.x, n - 1));
+#pragma unroll
+        for (int k = 0; k < REGS; ++k) v[k] = k * 64 * W + (int)threadIdx.x < n ? v[k] : 0;
         choose<W>(v, need, bins, totals, put);
     } else {
         choose_long<W>(n, need, bins, totals, rank, put);

@@ -50,6 +50,17 @@ __device__ __forceinline__ void ends_of(const SelectArgs& a, const Row& r, const
     for (int i = at; i < a.last; i += step) r.list[a.pages - a.last + i] = r.first + r.pages - a.last + i;
 }
 
+// Ranks of a row's scores, those of a thread.  (Behind the last score it is loaded again: loads that may be left out come one after the other.)
+template <int WAVES, int REGS>
+__device__ __forceinline__ void ranks_of(const Row& r, const int thread, uint32_t (&v)[REGS])
+{
+    float x[REGS];
+#pragma unroll
+    for (int k = 0; k < REGS; ++k) x[k] = r.scores[r.from + min(k * 64 * WAVES + thread, r.n - 1)];
+#pragma unroll
+    for (int k = 0; k < REGS; ++k) v[k] = k * 64 * WAVES + thread < r.n ? rank_of(x[k]) : 0;
+}
+
 template <int REGS>
 __global__ __launch_bounds__(64 * SMALL_WAVES) void cache_select(const SelectArgs a)
 {
@@ -60,11 +71,7 @@ __global__ __launch_bounds__(64 * SMALL_WAVES) void cache_select(const SelectArg
     ends_of(a, r, lane, 64);
     if (r.need == 0) return;
     uint32_t v[REGS];
-#pragma unroll
-    for (int k = 0; k < REGS; ++k) {
-        const int j = k * 64 + lane;
-        v[k] = j < r.n ? rank_of(r.scores[r.from + j]) : 0;
-    }
+    ranks_of<1>(r, lane, v);
     choose<1>(v, r.need, bins[threadIdx.x / 64], (int (*)[2])nullptr, [&](const int j, const int place) { r.list[r.head + place] = r.from + j; });
 }
 
@@ -73,7 +80,6 @@ __global__ __launch_bounds__(64 * WAVES) void cache_select_long(const SelectArgs
 {
     __shared__ Bins<WAVES> bins;
     __shared__ int totals[(REGS ? REGS : 1) * WAVES][2];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     for (int i = blockIdx.x; i < a.T * a.n_heads; i += gridDim.x) {
         Row r;
         if (!row_of(a, i, &r) || all_of(a, r, threadIdx.x, 64 * WAVES)) continue;
@@ -83,11 +89,7 @@ __global__ __launch_bounds__(64 * WAVES) void cache_select_long(const SelectArgs
         __syncthreads();        // (the last row's counts have been read)
         if constexpr (REGS > 0) {
             uint32_t v[REGS];
-#pragma unroll
-            for (int k = 0; k < REGS; ++k) {
-                const int j = (k * WAVES + wave) * 64 + lane;
-                v[k] = j < r.n ? rank_of(r.scores[r.from + j]) : 0;
-            }
+            ranks_of<WAVES>(r, threadIdx.x, v);
             choose<WAVES>(v, r.need, bins, totals, put);
         } else {
             choose_long<WAVES>(r.n, r.need, bins, totals, [&](const int j) { return rank_of(r.scores[r.from + j]); }, put);
