@@ -214,16 +214,35 @@ __global__ __launch_bounds__(THREADS) void cache_join_selected(const SelectedArg
     if (sequence_of(a.batch, t) < 0) return;
     const float* const parts = a.work + (int64_t)blockIdx.x * args.parts * part_floats(DIM);
     float top = NONE, all = 0.0f, seen = 0.0f;
-    for (int p = 0; p < args.parts; ++p) top = fmaxf(top, parts[p * part_floats(DIM) + col]);
+    constexpr int AHEAD = 4;        // parts that are loaded together (behind the last one it again, and nothing of it counts)
+    for (int p0 = 0; p0 < args.parts; p0 += 4 * AHEAD) {
+        float x[4 * AHEAD];
+#pragma unroll
+        for (int k = 0; k < 4 * AHEAD; ++k) x[k] = parts[min(p0 + k, args.parts - 1) * part_floats(DIM) + col];
+#pragma unroll
+        for (int k = 0; k < 4 * AHEAD; ++k) top = fmaxf(top, x[k]);
+    }
     const float ms = top == NONE ? 0.0f : top;
     float y[SLICE] = {};
-    for (int p = 0; p < args.parts; ++p) {
-        const float* const in = parts + p * part_floats(DIM);
-        const float share = __builtin_amdgcn_exp2f(in[col] - ms);
-        all += in[COLS + col] * share;
-        seen += in[2 * COLS + col];
+    for (int p0 = 0; p0 < args.parts; p0 += AHEAD) {
+        float x[AHEAD][3 + SLICE];
 #pragma unroll
-        for (int i = 0; i < SLICE; ++i) y[i] += in[3 * COLS + (wave * SLICE + i) * 64 + lane] * share;
+        for (int k = 0; k < AHEAD; ++k) {
+            const float* const in = parts + min(p0 + k, args.parts - 1) * part_floats(DIM);
+#pragma unroll
+            for (int i = 0; i < 3; ++i) x[k][i] = in[i * COLS + col];
+#pragma unroll
+            for (int i = 0; i < SLICE; ++i) x[k][3 + i] = in[3 * COLS + (wave * SLICE + i) * 64 + lane];
+        }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            if (p0 + k >= args.parts) break;
+            const float share = __builtin_amdgcn_exp2f(x[k][0] - ms);
+            all += x[k][1] * share;
+            seen += x[k][2];
+#pragma unroll
+            for (int i = 0; i < SLICE; ++i) y[i] += x[k][3 + i] * share;
+        }
     }
     const int column = tile * COLS + col;
     if (column >= G) return;

@@ -18,6 +18,7 @@ namespace spmm_cache {
 
 constexpr int MOVE_THREADS = 256;
 constexpr int PIECE = 1024;         // tokens that are moved with one list of places
+constexpr int EACH = PIECE / MOVE_THREADS;      // of these of a thread
 constexpr int KEYS_AHEAD = 8;       // steps whose loads are under way together
 constexpr int VALUE_DIMS = 16;      // of a workgroup
 template <int BYTES>
@@ -129,10 +130,12 @@ __device__ __forceinline__ void move_keys(const EvictArgs& a, const Moved& m, co
     for (int i0 = 0; i0 < m.stay.n; i0 += PIECE) {
         const int n = min(m.stay.n - i0, PIECE);
         __syncthreads();        // (the last piece has been read)
-        for (int i = tid; i < n; i += MOVE_THREADS) {
-            from[i] = max(slot_of(a, m.table, m.h, m.kept[i0 + i]), (int64_t)0);
-            if (i % 16 == 0) to[i / 16] = slot_of(a, m.table_to, m.h, i0 + i);
-        }
+        int at[EACH];
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) at[k] = m.kept[i0 + min(k * MOVE_THREADS + tid, n - 1)];
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) from[k * MOVE_THREADS + tid] = max(slot_of(a, m.table, m.h, at[k]), (int64_t)0);
+        if (tid * 16 < n) to[tid] = slot_of(a, m.table_to, m.h, i0 + tid * 16);
         __syncthreads();
         if (m.slice < slices) {
             const int per = row / 16 / slices, c = tid % per, rows = MOVE_THREADS / per, r = tid / per;
@@ -192,13 +195,15 @@ __device__ __forceinline__ void move_values(const EvictArgs& a, const Moved& m, 
     for (int i0 = 0; i0 < m.stay.n; i0 += PIECE) {
         const int n = min(m.stay.n - i0, PIECE);
         __syncthreads();        // (the last piece has been read)
-        for (int i = tid; i < n; i += MOVE_THREADS) {
-            ids[i] = m.kept[i0 + i];
-            if (i % 16 == 0) {
-                // (of the slice's first dim: pages hold a head's dims one after the other)
-                const int64_t slot = slot_of(a, m.table_to, m.h, i0 + i);
-                to[i / 16] = slot < 0 ? -1 : (slot >> shift << shift) * D + ((int64_t)d0 << shift) + (slot & inside);
-            }
+        int at[EACH];
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) at[k] = m.kept[i0 + min(k * MOVE_THREADS + tid, n - 1)];
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) ids[k * MOVE_THREADS + tid] = at[k];
+        if (tid * 16 < n) {
+            // (of the slice's first dim: pages hold a head's dims one after the other)
+            const int64_t slot = slot_of(a, m.table_to, m.h, i0 + tid * 16);
+            to[tid] = slot < 0 ? -1 : (slot >> shift << shift) * D + ((int64_t)d0 << shift) + (slot & inside);
         }
         __syncthreads();
         u32x4 v[LOADS];

@@ -79,6 +79,21 @@ __device__ __forceinline__ int64_t column_of(const WeighArgs& a, const Counted& 
     return ((int64_t)(s.first + c / a.group) * a.pool.n_heads + h) * a.group + c % a.group;
 }
 
+// Parts from, from + step, .. of a column's statistics, put together in their order; AHEAD of them are loaded together (behind the last one nothing).
+__device__ __forceinline__ void join_parts(const WeighArgs& a, const int64_t column, const int from, const int step, float& top, float& sum)
+{
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    constexpr int AHEAD = 8;
+    for (int p0 = from; p0 < a.parts; p0 += AHEAD * step) {
+        f32x2 x[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) x[k] = *(const f32x2*)stat_of(a, column, min(p0 + k * step, a.parts - 1));
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+            if (p0 + k * step < a.parts) join(top, sum, x[k][0], x[k][1]);
+    }
+}
+
 // Operands of 32 dims of a product: queries' and keys'.  bfloat16: step s holds dims 32 s + 8 g ..; 8 bits: dims 64 (s / 2) + 16 g + 8 (s % 2) ..
 template <spmm_cache_type_t TYPE>
 __device__ __forceinline__ int dim_of(const int s, const int g)
@@ -285,7 +300,7 @@ __global__ __launch_bounds__(THREADS) void cache_weigh_kept(const WeighArgs a)
     float top = NONE, sum = 0.0f;
     if (c < cols) {
         const int64_t column = column_of(a, s, h, c);
-        for (int p = p0; p < a.parts; p += EACH) join(top, sum, stat_of(a, column, p)[0], stat_of(a, column, p)[1]);
+        join_parts(a, column, p0, EACH, top, sum);
         if (p0 == 0) spans[c] = span_of(a, b, s.first + c / a.group);
     }
     tops[p0][c] = top;
@@ -302,14 +317,22 @@ __global__ __launch_bounds__(THREADS) void cache_weigh_kept(const WeighArgs a)
     if ((uint32_t)page >= (uint32_t)a.pool.n_pages) return;
     float* const out = a.pool.weight + (((int64_t)page * a.pool.n_heads + h) << shift) + (key & inside);
     f32x4 w = *(const f32x4*)out, add = {0, 0, 0, 0};
-    for (int i = 0; i < cols; ++i) {
-        const f32x4 x = *(const f32x4*)(kept_of(a, b, h, i) + key);
-        const Span span = spans[i];
-        const float m = most[i], f = inv[i];
+    constexpr int AHEAD = 4;        // columns whose scores are loaded together
+    for (int i0 = 0; i0 < cols; i0 += AHEAD) {
+        f32x4 x[AHEAD];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float p = __builtin_amdgcn_exp2f(__fmaf_rn(x[j], a.scale_log2, -m)) * f;
-            add[j] += key + j >= span.from && key + j <= span.to ? p : 0.0f;
+        for (int k = 0; k < AHEAD; ++k) x[k] = *(const f32x4*)(kept_of(a, b, h, min(i0 + k, cols - 1)) + key);
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const int i = i0 + k;
+            if (i >= cols) break;
+            const Span span = spans[i];
+            const float m = most[i], f = inv[i];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float p = __builtin_amdgcn_exp2f(__fmaf_rn(x[k][j], a.scale_log2, -m)) * f;
+                add[j] += key + j >= span.from && key + j <= span.to ? p : 0.0f;
+            }
         }
     }
 #pragma unroll
@@ -324,10 +347,7 @@ __global__ __launch_bounds__(THREADS) void cache_weigh_join(const WeighArgs a)
     const int t = (int)(column / (a.group * a.pool.n_heads)), b = sequence_of(a.batch, t);
     if (b < 0) return;
     float top = NONE, sum = 0.0f;
-    for (int p = 0; p < a.parts; ++p) {
-        const float* const in = stat_of(a, column, p);
-        join(top, sum, in[0], in[1]);
-    }
+    join_parts(a, column, 0, 1, top, sum);
     *joined_of(a, column) = Joined{top, 1.0f / sum, span_of(a, b, t)};
 }
 
