@@ -32,7 +32,7 @@ __global__ __launch_bounds__(THREADS, 2) void cache_attend_lists(const SelectedA
     const int each = gridDim.x / XCDS, list = (int)(blockIdx.x % XCDS * each + blockIdx.x / XCDS) * (WAVES / SHARE) + wave / SHARE;
     if (list >= a.T * H * tiles) return;
     const int t = list % a.T, h = list / a.T % H, tile = list / a.T / H;
-    const int b = sequence_of(a.batch, t);
+    const int b = sequence_near(a.batch, t);
     if (b < 0) return;
     const Span span = seen_span(a, b, t);
 

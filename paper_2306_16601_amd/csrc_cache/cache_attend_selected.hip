@@ -32,7 +32,7 @@ __global__ __launch_bounds__(THREADS, PER_CU) void cache_attend_selected(const S
     const int tiles = (G + COLS - 1) / COLS;
     const int list = blockIdx.x / (uint32_t)(tiles * args.parts), rest = blockIdx.x % (uint32_t)(tiles * args.parts);
     const int tile = rest / args.parts, p = rest % args.parts, t = list / H, h = list % H;
-    const int b = sequence_of(a.batch, t);
+    const int b = sequence_near(a.batch, t);
     if (b < 0) return;
     const Span span = seen_span(a, b, t);
 
@@ -211,7 +211,7 @@ __global__ __launch_bounds__(THREADS) void cache_join_selected(const SelectedArg
     const int H = a.pool.n_heads, G = a.group, D = a.pool.head_dim, tiles = (G + COLS - 1) / COLS;
     const int64_t list = blockIdx.x / (uint32_t)tiles;
     const int tile = blockIdx.x % (uint32_t)tiles, t = (int)(list / H), h = (int)(list % H);
-    if (sequence_of(a.batch, t) < 0) return;
+    if (sequence_near(a.batch, t) < 0) return;
     const float* const parts = a.work + (int64_t)blockIdx.x * args.parts * part_floats(DIM);
     float top = NONE, all = 0.0f, seen = 0.0f;
     constexpr int AHEAD = 4;        // parts that are loaded together (behind the last one it again, and nothing of it counts)

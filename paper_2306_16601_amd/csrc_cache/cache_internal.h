@@ -175,6 +175,13 @@ __device__ __forceinline__ int sequence_of(const Batch& s, const int t)
     return lo < s.n_seqs && t >= s.q_start[lo] ? lo : -1;
 }
 
+// The same, which looks first where t is if every sequence has one new token.
+__device__ __forceinline__ int sequence_near(const Batch& s, const int t)
+{
+    const int b = t < s.n_seqs ? t : s.n_seqs - 1;
+    return s.q_start[b] <= t && t < s.q_start[b + 1] ? b : sequence_of(s, t);
+}
+
 // Tokens of a sequence that its table can name (a table's row names less than 2^30: cache_api.cpp).
 __host__ __device__ __forceinline__ int tokens_of(const Batch& s, const int b, const int page_shift)
 {

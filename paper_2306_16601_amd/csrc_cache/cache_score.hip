@@ -118,7 +118,7 @@ __global__ __launch_bounds__(THREADS, 3) void cache_score(const ScoreArgs a, con
     const int t0 = (int)(blockIdx.x / H) * f.tokens, t1 = min(t0 + f.tokens, a.T);
     const int p0 = (int)(blockIdx.y * WAVES + wave) * f.steps * PAGES, p1 = min(p0 + f.steps * PAGES, width);
     for (int t = t0; t < t1;) {
-        const int b = sequence_of(a.batch, t);
+        const int b = sequence_near(a.batch, t);
         if (b < 0) {
             ++t;
             continue;
@@ -172,7 +172,7 @@ __global__ __launch_bounds__(THREADS, 2) void cache_score_many(const ScoreArgs a
     const int t0 = (int)(blockIdx.x / H) * f.tokens * WAVES, t1 = min(t0 + f.tokens * WAVES, a.T);
     const int p0 = (int)blockIdx.y * f.steps * PAGES, p1 = min(p0 + f.steps * PAGES, width);
     for (int t = t0; t < t1;) {
-        const int b = sequence_of(a.batch, t);
+        const int b = sequence_near(a.batch, t);
         if (b < 0) {
             ++t;
             continue;

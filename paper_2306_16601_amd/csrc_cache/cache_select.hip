@@ -21,7 +21,7 @@ struct Row {
 // false: a column of no sequence
 __device__ __forceinline__ bool row_of(const SelectArgs& a, const int i, Row* const r)      // (there are at most 2^22)
 {
-    const int t = i / a.n_heads, b = sequence_of(a.batch, t);
+    const int t = i / a.n_heads, b = sequence_near(a.batch, t);
     if (b < 0) return false;
     const Span s = span_of(a.batch, b, t, a.page_shift, a.causal, a.window);
     r->first = s.from <= s.to ? s.from >> a.page_shift : 0;

@@ -344,7 +344,7 @@ __global__ __launch_bounds__(THREADS) void cache_weigh_join(const WeighArgs a)
 {
     const int64_t column = (int64_t)blockIdx.x * THREADS + threadIdx.x;
     if (column >= (int64_t)a.T * a.group * a.pool.n_heads) return;
-    const int t = (int)(column / (a.group * a.pool.n_heads)), b = sequence_of(a.batch, t);
+    const int t = (int)(column / (a.group * a.pool.n_heads)), b = sequence_near(a.batch, t);
     if (b < 0) return;
     float top = NONE, sum = 0.0f;
     join_parts(a, column, 0, 1, top, sum);
