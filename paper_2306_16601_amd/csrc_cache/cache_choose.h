@@ -5,7 +5,7 @@
 // other: a row of a thousand scores takes one pass of bins, and seldom another.  Counts do not depend on the order of additions, and
 // nothing is moved, so a row stays in the registers that it was loaded to.  What is chosen keeps its order by counting too: ranks
 // are sums over the lanes before.  (A border that is halved until its count is right takes 10 to 22 passes over the row, 42 us for 16000
-// rows of 970 scores; with bins it is 32, and 26 since only those values are counted that can be chosen: where no more are chosen than the row has threads,
+// rows of 970 scores; with bins it is 32, and 26 (21 with the row loaded at once) since only those values are counted that can be chosen: where no more are chosen than the row has threads,
 // the lowest of the threads' highest values is a bound.)
 #pragma once
 

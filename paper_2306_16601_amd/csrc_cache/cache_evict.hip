@@ -7,9 +7,9 @@
 // lane.  Values, whose tokens are contiguous, are gathered one by one, tokens side by side in a wave, so that it finds them in a few lines
 // of memory: nearly all lines of the values are read wherever one token in sixteen stays.
 //
-// 8 rows of up to 12 thousand tokens in 8 bits, 8 layers of 8 heads of 128 dims, to 2048 each: 33 us to choose, 226 to move (405 MB read and 288
-// written by the counters, 3.1 TB/s; without the picks it takes as long, with more workgroups on a CU too: it is the memory's answer to runs of 64 bytes to 1 KB); 4 rows of 1000, 12 layers of 12 heads of 64 dims in
-// bfloat16, to 250: 8.5 and 25.4 (130 MB with the lines that are read whole, 5 TB/s).
+// 8 rows of up to 12 thousand tokens in 8 bits, 8 layers of 8 heads of 128 dims, to 2048 each: 27 us to choose, 223 to move (386 MB read and 291
+// written by the counters, 3 TB/s; without the picks it takes as long, with more workgroups on a CU too: it is the memory's answer to runs of 64 bytes to 1 KB); 4 rows of 1000, 12 layers of 12 heads of 64 dims in
+// bfloat16, to 250: 7.1 and 26 (130 MB with the lines that are read whole, 5 TB/s).
 #include "cache_choose.h"
 
 #include <type_traits>
@@ -292,11 +292,12 @@ int launch_evict(const EvictArgs& a, const spmm_cache_type_t type, void* stream)
     const int64_t most = a.ld_table << a.pool.page_shift, heads = (int64_t)a.n_layers * a.pool.n_heads;
     const dim3 rows((unsigned)heads, (unsigned)a.n_rows);
     int rc;
-    // As few waves and registers as hold a row, us, 4 (32) rows of 4 layers of 8 heads: 1000 tokens with 4 registers of 4 waves 7.2 (10.8), with 16 of
-    // them 9.3 (13.1); 4000 with 16 registers of 4 waves 18.1 (27.7), of 16 waves 13.5 (34.2); 16000 with 16 registers of 16 waves 30.9, with weights
-    // read again at each pass 58.9; 32000 49 and 150.
+    // As few waves and registers as hold a row, us, 4 (32) rows of 4 layers of 8 heads: 1000 tokens with 4 registers of 4 waves 5.9 (8.4), with 16 of
+    // them 7.8 (11.9); 4000 with 16 registers of 4 waves 10.1 (17), of 16 waves 12.6 (32); 8000 with 32 registers of 4 waves 18.8 (26.6), with 16 of 16 16.2 (43); 16000 with
+    // 16 registers of 16 waves 19.8, with weights read again at each pass 58; 32000 26.7 and 146.
     if (most <= 64 * 4 * 4) rc = launch(cache_evict_choose<4, 4>, rows, dim3(64 * 4), a, stream);
     else if (most <= 64 * 4 * 16) rc = launch(cache_evict_choose<4, 16>, rows, dim3(64 * 4), a, stream);
+    else if (most <= 64 * 4 * 32) rc = launch(cache_evict_choose<4, 32>, rows, dim3(64 * 4), a, stream);
     else if (most <= 64 * 16 * 16) rc = launch(cache_evict_choose<16, 16>, rows, dim3(64 * 16), a, stream);
     else if (most <= 64 * 16 * 32) rc = launch(cache_evict_choose<16, 32>, rows, dim3(64 * 16), a, stream);
     else rc = launch(cache_evict_choose<16, 0>, rows, dim3(64 * 16), a, stream);

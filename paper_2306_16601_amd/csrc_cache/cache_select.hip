@@ -1,8 +1,8 @@
 // Which pages a new token reads: the first, the last, and those of the highest scores, in ascending order (cache_choose.h).
 //
 // A wave has a row of up to 1024 pages in its registers; longer ones take a workgroup, and those of more than 32 thousand pages are read
-// again at each pass.  Reading the scores once would take 13 us for 16000 rows of 970 of them; it takes 25.7:
-// 580 vector instructions a row are 15 us of it, and wait for LDS.
+// again at each pass.  Reading the scores once would take 13 us for 16000 rows of 970 of them; it takes 19.7:
+// 600 vector instructions a row are 15 us of it.
 #include "cache_choose.h"
 
 namespace spmm_cache {
@@ -102,13 +102,16 @@ int launch_select(const SelectArgs& a, void* stream)
     const int64_t rows = (int64_t)a.T * a.n_heads, most = a.batch.ld_table;
     const unsigned grid = (unsigned)(rows < 1 << 20 ? rows : 1 << 20);
     const dim3 small((unsigned)((rows + SMALL_WAVES - 1) / SMALL_WAVES)), threads(64 * SMALL_WAVES);
-    // 64 / 4096 rows, us: 1000 pages by a wave 8.1 / 11.9, by four 8.6 / 33.5; 4000 pages by four 10.1 / 52, by sixteen 14.4 / 212; 30000 pages by sixteen with
-    // the row in registers 18 / -, without 49 / -, and 8000 15 / 233 and 18 / 280.
+    // As few waves as hold a row, 64 / 4096 rows, us: 1000 pages by a wave 6.5 / 9.2, by four 8.2 / 33; 4000 pages by four 8.9 / 36, by sixteen 15 / 215; 8000 by four
+    // with 32 registers 11.6 / 66, by sixteen 15.2 / 219; 16000 by sixteen with 16 registers 11.3 / 163, with 32 15.5 / 221; 30000 with the row in registers 15.8,
+    // without 47.
     if (most <= 128) return launch(cache_select<2>, small, threads, a, stream);
     if (most <= 256) return launch(cache_select<4>, small, threads, a, stream);
     if (most <= 512) return launch(cache_select<8>, small, threads, a, stream);
     if (most <= 1024) return launch(cache_select<16>, small, threads, a, stream);
     if (most <= 4096) return launch(cache_select_long<4, 16>, dim3(grid), dim3(256), a, stream);
+    if (most <= 8192) return launch(cache_select_long<4, 32>, dim3(grid), dim3(256), a, stream);
+    if (most <= 16384) return launch(cache_select_long<16, 16>, dim3(grid), dim3(1024), a, stream);
     if (most <= 32768) return launch(cache_select_long<16, 32>, dim3(grid), dim3(1024), a, stream);
     return launch(cache_select_long<16, 0>, dim3(grid), dim3(1024), a, stream);
 }

@@ -159,13 +159,13 @@ def test_select(pages, first, last, causal, window):
     select(small([100, 0, 900], [20, 0, 33], lead=3), pages, first, last, causal, window)
 
 
-@pytest.mark.parametrize("pages_held", [129, 257, 513, 1025, 4097, 9000, 32769, 40000])
+@pytest.mark.parametrize("pages_held", [129, 257, 513, 1025, 4097, 9000, 20000, 32769, 40000])
 def test_select_from_long_rows(pages_held):
     select(small([16 * pages_held - 1, 16 * (pages_held // 2)]), 50, 1, 2)
     select(small([16 * pages_held - 1, 5]), pages_held - 7, 1, 2)
 
 
-@pytest.mark.parametrize("pages_held", [100, 700, 3000, 40000])
+@pytest.mark.parametrize("pages_held", [100, 700, 3000, 6000, 10000, 20000, 40000])
 def test_equal_scores_take_the_lower_page(pages_held):
     p = small([16 * pages_held])
     select(p, 33, 1, 1, change=lambda s: s.copy_((s * 2).round()))
