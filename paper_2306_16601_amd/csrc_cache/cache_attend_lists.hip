@@ -65,7 +65,8 @@ __global__ __launch_bounds__(THREADS, 2) void cache_attend_lists(const SelectedA
     // steps of keys that share a softmax (behind the last one there are steps of nothing)
     const int width = STREAMS ? min(COLS >> log_group, ((steps + SHARE - 1) / SHARE + 1) & ~1) : 1;
     const int chunk_k = CHUNK * (col >> 2), chunk_v = CHUNK * g;
-    const char* const k_base = (const char*)a.pool.k + (col & 3) * D + LANE * g;
+    // (lanes whose dims are not there load the first ones of the token: what lies 16 g bytes behind them may be behind the last token of the pool)
+    const char* const k_base = (const char*)a.pool.k + (col & 3) * D + (EXACT || LANE * g < D ? LANE * g : 0);
     const char* const v_base = (const char*)a.pool.v + ((int64_t)col << shift);
     // a step's keys, or its values: the same loads, other addresses and strides
     const auto load = [&](const int step, const bool are_values, u32x4 (&r)[N]) {

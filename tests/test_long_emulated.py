@@ -1,0 +1,38 @@
+"""Kernels for long contexts on the CPU (tests/emu): every operand ends, and a page table begins, at memory that must not be touched, and results are compared with
+their definitions."""
+import json
+import os
+import subprocess
+import sys
+
+import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+sys.path.insert(0, os.path.join(HERE, "emu"))
+import build_long_emu  # noqa: E402
+
+pytestmark = pytest.mark.skipif(not build_long_emu.available(), reason="no host clang++ for the emulation build")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def emulated():
+    return build_long_emu.build()
+
+
+def run(call, news, pasts, q_heads, kv_heads, dim, page, cache, problem=(), **how):
+    case = {"call": call, "problem": dict(news=news, pasts=pasts, q_heads=q_heads, kv_heads=kv_heads, dim=dim, page=page, cache=cache, **dict(problem)), **how}
+    r = subprocess.run([sys.executable, os.path.join(HERE, "emu", "run_long.py"), json.dumps(case)], capture_output=True, text=True, timeout=600)
+    assert r.returncode == 0, "emulated run failed (rc %d):\n%s" % (r.returncode, r.stderr[-3000:])
+    said = json.loads(r.stdout.strip().splitlines()[-1])
+    assert said["bad"] == 0, said
+
+
+# weights in bfloat16 and binary16: what test_long_attend.py holds
+TOL = 2.0 ** -8 + 1e-4
+
+
+@pytest.mark.parametrize("new, pages", [(70, 6), (250, 2)])
+@pytest.mark.parametrize("dim", [16, 32, 48, 64, 80, 112])
+def test_lists_of_8_bit_caches_read_no_key_behind_the_last(dim, new, pages):
+    """Lists that have four waves each, and one: some of them name the pool's last page."""
+    run("selected", [new, 1], [13, 30], 4, 4, dim, 16, "s8", problem=dict(spare=0, seed=1), pages=pages, tol=TOL)
