@@ -372,7 +372,7 @@ __global__ __launch_bounds__(THREADS, 2) void cache_weigh_add(const WeighArgs a)
     const int D = EXACT ? 32 * KS : a.pool.head_dim;
     const Counted s = counted(a, b);
     const int cols = s.tokens * G;
-    if (cols <= 0) return;
+    if (cols <= 0 || s.len == 0) return;        // (keys are loaded ahead: of a row without tokens there would be none, nor a page)
     const int32_t* const table = a.batch.table + b * a.batch.ld_table;
     const int stride = gridDim.x * KEYS * WAVES;
     Keys<KS, TYPE, EXACT, FAR> k, next;

@@ -36,3 +36,10 @@ TOL = 2.0 ** -8 + 1e-4
 def test_lists_of_8_bit_caches_read_no_key_behind_the_last(dim, new, pages):
     """Lists that have four waves each, and one: some of them name the pool's last page."""
     run("selected", [new, 1], [13, 30], 4, 4, dim, 16, "s8", problem=dict(spare=0, seed=1), pages=pages, tol=TOL)
+
+
+@pytest.mark.parametrize("cache", ["bf16", "s8"])
+@pytest.mark.parametrize("lens", [[0, 9], [-4, 9]])
+def test_weights_of_a_first_row_without_tokens(lens, cache):
+    """New columns, but no token (padding): nothing in front of the page table is read.  (Rows of 1024 numbers: the table begins at a protected page.)"""
+    run("weigh", [20, 5], [10, 4], 2, 1, 64, 16, cache, problem=dict(width=1024, seed=2), lens=lens, tol=3e-4)
