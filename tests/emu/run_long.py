@@ -1,6 +1,6 @@
 """Runs one call for long contexts through the host emulation and compares it with its definition (tests/long_reference.py).  Called as a subprocess: an access
 outside the operands ends it with a segmentation fault, a barrier that not all waves reach with the emulator's deadlock report.
-usage: run_long.py JSON     {"call": "selected" | "weigh", "problem": arguments of Long, and what the call takes}"""
+usage: run_long.py JSON     {"call": "selected" | "weigh" | "bounds" | "score" | "evict", "problem": arguments of Long, and what the call takes}"""
 import ctypes
 import json
 import os
@@ -15,7 +15,7 @@ sys.path[:0] = [ROOT, os.path.dirname(HERE), HERE]
 import build_long_emu  # noqa: E402
 import torch  # noqa: E402
 
-from long_reference import POISON, Long  # noqa: E402
+from long_reference import POISON, Long, kept_of  # noqa: E402
 from paper_2306_16601_amd import cache_binding as cb  # noqa: E402
 
 lib = ctypes.CDLL(build_long_emu.LIB)
@@ -92,6 +92,67 @@ def weigh(p, tol, max_new=None, causal=True, window=0, decay=0.5):
     return compared(p.d["weight"].back(), want, tol * added + 2.0 ** -22 * np.abs(want))
 
 
+def bounds(p, T=None):
+    cache, batch = described(p)
+    want = p.bounds_wanted()
+    call("spmm_cache_bounds", cache, i32(p.layer), batch, i64(T or max(1, p.tokens)), None)
+    got = torch.from_numpy(p.d["bounds"].back()).view(torch.bfloat16).double()
+    return compared(got.numpy(), want.numpy(), 0.0 if p.kind == "bf16" else np.abs(want.numpy()) * (2.0 ** -8 + 2.0 ** -22))
+
+
+def score(p, causal=True, window=0, pad=0, pages=5, first=1, last=1):
+    """And select, of what it gives."""
+    cache, batch = described(p)
+    T, heads, lds = max(1, p.tokens), p.k.shape[2], p.table.shape[1] + pad
+    how = cb.spmm_select_t(p.q_heads, pages, first, last, causal, window)
+    out, lists = Device(np.full((T, heads, lds), POISON, np.float32)), Device(np.full((T, heads, pages), POISON, np.int32))
+    call("spmm_cache_score", cache, i32(p.layer), batch, p.d["q"], i64(T), how, out, i64(lds), None)
+    call("spmm_cache_select", cache, batch, out, i64(T), i64(lds), how, lists, None)
+    got = out.back()
+    want, mag, mine = p.scores_wanted(causal, window)
+    full, tol = np.full(got.shape, float(POISON)), np.zeros(got.shape)
+    full[mine, :, :lds - pad], tol[:, :, :lds - pad] = want[mine], mag * 2.0 ** -23 * (2 * p.dim + 2)
+    said = compared(got, full, tol)
+    wrong = int((lists.back() != p.lists_wanted(got, pages, first, last, causal, window)).sum())
+    return said | {"bad": said["bad"] + wrong, "lists": wrong}
+
+
+def evict(p, keep, first, recent, most, inplace):
+    """To the same pages, or to new ones (behind the old ones in the pool)."""
+    if not inplace:
+        tail = lambda x: None if x is None else torch.cat((x, x.flip(1)), 1)        # noqa: E731
+        p.k, p.v, p.k_scale, p.v_scale, p.weight, p.bounds = (tail(getattr(p, n)) for n in ("k", "v", "k_scale", "v_scale", "weight", "bounds"))
+    to = p.table.copy() if inplace else np.where(p.table >= 0, 2 * p.pages - 1 - p.table, -1).astype(np.int32)
+    p.pages = p.k.shape[1]
+    cache, batch = described(p)
+    rows, heads = len(p.news), p.k.shape[2]
+    kept, lens = Device(np.full((p.layers, rows, heads, most), POISON, np.int32)), Device(np.full(rows, POISON, np.int32))
+    call("spmm_cache_evict", cache, p.d["table"], i64(p.table.shape[1]), p.d["lens"], i64(rows), Device(np.full(rows, keep, np.int32)), cb.spmm_evict_t(first, recent, most), Device(to), lens,
+         kept, None)
+    bad, kept = 0, kept.back()
+    want = {n: getattr(p, n).clone() for n in ("k", "v", "weight") + (("k_scale", "v_scale") if p.kind == "s8" else ())}
+    for b in range(rows):
+        n = min(keep, p.held(b), most)
+        bad += int(lens.back()[b] != n)
+        for i in range(p.layers):
+            for h in range(heads):
+                j = np.arange(p.held(b))
+                ids = kept_of(p.weight[i, p.table[b, j // p.page], h, j % p.page].numpy(), n, first, recent)
+                bad += int((kept[i, b, h] != ids + [-1] * (most - n)).sum())
+                src, dst = np.asarray(ids, int), np.arange(n)
+                for name, x in want.items():
+                    old = getattr(p, name)
+                    if name == "v":
+                        x[i, to[b, dst // p.page], h, :, dst % p.page] = old[i, p.table[b, src // p.page], h, :, src % p.page]
+                    else:
+                        x[i, to[b, dst // p.page], h, dst % p.page] = old[i, p.table[b, src // p.page], h, src % p.page]
+    for name, x in want.items():
+        got = p.d[name].back()
+        same = got.view(np.uint8).reshape(-1) == Device(x).back().view(np.uint8).reshape(-1)
+        bad += int((~same).sum())
+    return {"bad": bad}
+
+
 def compared(got, want, tol):
     got = got.astype(np.float64)
     with np.errstate(invalid="ignore"):
@@ -105,7 +166,7 @@ def main():
     for name in ("lens", "table"):
         if name in case:
             setattr(p, name, np.asarray(case.pop(name), np.int32) if name == "table" else case.pop(name))
-    print(json.dumps({"selected": selected, "weigh": weigh}[case.pop("call")](p, **case)))
+    print(json.dumps({"selected": selected, "weigh": weigh, "bounds": bounds, "score": score, "evict": evict}[case.pop("call")](p, **case)))
 
 
 if __name__ == "__main__":

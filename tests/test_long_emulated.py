@@ -43,3 +43,18 @@ def test_lists_of_8_bit_caches_read_no_key_behind_the_last(dim, new, pages):
 def test_weights_of_a_first_row_without_tokens(lens, cache):
     """New columns, but no token (padding): nothing in front of the page table is read.  (Rows of 1024 numbers: the table begins at a protected page.)"""
     run("weigh", [20, 5], [10, 4], 2, 1, 64, 16, cache, problem=dict(width=1024, seed=2), lens=lens, tol=3e-4)
+
+
+@pytest.mark.parametrize("cache", ["bf16", "s8"])
+@pytest.mark.parametrize("q_heads, kv_heads, dim, page", [(4, 4, 16, 16), (5, 1, 48, 64), (6, 2, 80, 256), (40, 2, 128, 16)])
+def test_no_call_leaves_its_operands(q_heads, kv_heads, dim, page, cache):
+    """Pools without a spare page, tables and lists without a spare number."""
+    shape = (q_heads, kv_heads, dim, page, cache, dict(spare=0, seed=3))
+    run("bounds", [1, 0, 5, 3 * page + 1], [0, 9, page - 2, page], *shape)
+    run("score", [1, 3, 1], [40, 3 * page, 5 * page + 3], *shape, pages=3)
+    run("score", [70, 3], [40, 3 * page], *shape, window=50, pad=3, pages=3)
+    run("selected", [1, 5], [600, page], *shape, pages=4, tol=TOL)
+    run("weigh", [1, 2], [600, page], *shape, tol=3e-4)
+    run("weigh", [33, 2], [300, page], *shape, tol=3e-4, window=40)
+    for inplace in (True, False):
+        run("evict", [1, 1, 1], [300, page, 2 * page + 3], *shape, keep=120, first=3, recent=20, most=130, inplace=inplace)
