@@ -216,8 +216,10 @@ spmm_status_t spmm_selected_work_bytes(const spmm_cache_t *cache, int64_t T, con
 
 /* spmm_cache_attend over the pages of lists [T][n_heads][pages] (device, int32): column t's softmax for the query heads of h is over the visible
  * tokens of the pages lists[t][h] of its row.  Numbers below 0 or not below ld_table name no page; pages may come in any order, and one that is
- * named twice counts twice.  All columns of a sequence are computed (how->max_new is not read, but checked).  Results, rounding, out, ldo
- * and work as for spmm_cache_attend, with S8 caches as for few columns there. */
+ * named twice counts twice.  All columns of a sequence are computed (how->max_new is not read, but checked).  Results, out, ldo and work as for
+ * spmm_cache_attend, but weights are not rounded to 16 bits: BF16 caches: values are multiplied by three bfloat16 numbers, whose sum is the weight.  S8
+ * caches: codes are multiplied by two binary16 numbers, whose sum is 22 bits of a weight times its value's scale; queries to binary16, over a power of two.  What is below
+ * 2^-24 of the largest query, or of the largest scale it is multiplied beside, is lost.  The sum of weights is that of the unrounded ones. */
 spmm_status_t spmm_cache_attend_selected(const spmm_cache_t *cache, int32_t layer, const spmm_batch_t *batch, const void *q, int64_t T,
                                          const spmm_attend_t *how, const int32_t *lists, int64_t pages, void *out, int64_t ldo, void *work,
                                          void *hip_stream);

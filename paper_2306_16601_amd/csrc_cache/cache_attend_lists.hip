@@ -105,7 +105,7 @@ __global__ __launch_bounds__(THREADS, 2) void cache_attend_lists(const SelectedA
         for (int i = 0; i < ROWS; i += 4) *(f32x4*)(ks + i) = *(const f32x4*)(a.pool.k_scale + slot + i);
 #pragma unroll
         for (int i = 0; i < ROWS; ++i) y[i] = 0.0f;
-        u32x4 w[2];
+        u32x4 w[L::WEIGHTS];
 
         const auto softmax = [&]() {
 #pragma unroll
@@ -135,7 +135,7 @@ __global__ __launch_bounds__(THREADS, 2) void cache_attend_lists(const SelectedA
                 sum += y[i];
                 y[i] *= vs[i] * values.down;
             }
-            pack_weights<TYPE>(y, w, sum);
+            pack_terms<_Float16, L::TERMS, L::HALVES>(y, values.infinite, w);
             l = l * fade + sum;
             if (__any(less != 1.0f)) {
 #pragma unroll
@@ -154,9 +154,9 @@ __global__ __launch_bounds__(THREADS, 2) void cache_attend_lists(const SelectedA
             for (int i = 0; i < ROWS; ++i) y[i] = !STREAMS || stream == x ? sc[i / 4][i % 4] : y[i];
         };
         const auto products = [&](const int x, u32x4 (&v)[N]) {
-            u32x4 mine[2];
+            u32x4 mine[L::WEIGHTS];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) mine[e] = !STREAMS || stream == x ? w[e] : u32x4{0, 0, 0, 0};
+            for (int e = 0; e < L::WEIGHTS; ++e) mine[e] = !STREAMS || stream == x ? w[e] : u32x4{0, 0, 0, 0};
             selected_values<DIM, TYPE>(v, mine, o);
         };
         const int after = base + SHARE * width < steps ? base + SHARE * width : 0;      // (behind the last one something that is there, and not used)

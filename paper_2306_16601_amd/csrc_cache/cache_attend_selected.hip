@@ -1,7 +1,7 @@
 // Attention over the pages of a list for each new token and key/value head: bound by reading those pages.
 //
 // Columns are the query heads of one token that share a key/value head, up to 16 of them, and as in attention over all pages
-// (cache_attend.h) scores are computed transposed and weights go from registers to registers.  A workgroup has a list, or a part of
+// (cache_attend.h) scores are computed transposed and weights go from registers to registers, as sums of terms that hold all of them (pack_terms).  A workgroup has a list, or a part of
 // one: it first writes where the listed pages are, and what positions they hold, to LDS; its four waves then take the keys of the
 // list in turn, next step's keys on their way while a wave works on this one's.  All columns see the same keys, so that what is hidden is
 // hidden from all: its scores are -inf and its values 0.  Parts of a list are joined by cache_join_selected, in their order.
@@ -144,13 +144,12 @@ __global__ __launch_bounds__(THREADS, PER_CU) void cache_attend_selected(const S
 #pragma unroll
         for (int i = 0; i < ROWS; ++i) {
             y[i] = __builtin_amdgcn_exp2f(__fmaf_rn(y[i], unit, -ms));
-            if constexpr (S8) {
-                sum += y[i];
-                y[i] *= vs[i] * values.down;
-            }
+            sum += y[i];
+            if constexpr (S8) y[i] *= vs[i] * values.down;
         }
-        u32x4 w[S8 ? 2 : 1];
-        pack_weights<TYPE>(y, w, sum);
+        u32x4 w[L::WEIGHTS];
+        if constexpr (S8) pack_terms<_Float16, L::TERMS, L::HALVES>(y, values.infinite, w);
+        else pack_terms<__bf16, L::TERMS, L::HALVES>(y, false, w);
         l = l * fade + sum;
         if (__any(fade != 1.0f)) {
 #pragma unroll

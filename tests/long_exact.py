@@ -1,0 +1,43 @@
+"""How far attention over lists of pages may be from its definition where nothing is rounded to less than binary32 (test infrastructure).
+
+With n visible tokens, D dims, A the largest sum of |q k| scale over the dims of a key, and unit roundings of 2^-24 (additions inside the matrix instruction are counted as 2^-23,
+whichever way it rounds):
+  scores      D additions of exact products: D 2^-23 A; queries beside 8-bit codes lose 2^-25 of the largest one: 2^-25 max |q| sum |k| scale; scale, the key's
+              scale, the largest score and the exponent are rounded once each, to 2^-24 of at most 2 A log2(e) < 3 A: less than 2^-20 A together
+  weights     twice that (their own error, and that of their sum), the exponential 2^-22; of 8-bit caches, in two terms of binary16, 2^-23 of themselves and
+              2^-24 of the largest scale that they are multiplied beside: of the largest weight, which is part of the sum
+  sums        3 n additions for products of three terms, n for the sum of the weights, 32 to join lanes, waves and parts: (4 n + 32) 2^-23
+All but the losses beside the largest query and scale are relative to sum p |v|."""
+import numpy as np
+
+
+def limits(p, lists, scale, causal=True, window=0):
+    """(result, how far off it may be), [q_heads * dim, tokens]; NaN in columns of no sequence."""
+    out = np.full((p.q_heads, p.dim, max(1, p.tokens)), np.nan)
+    tol, rows = out.copy(), {}
+    for t, b, at in p.columns():
+        lo, hi = p.span(b, at, causal, window)
+        for h in range(p.q_heads):
+            kv = h // p.group
+            if (b, kv) not in rows:
+                j = np.arange(p.held(b))
+                scales = None if p.v_scale is None else p.v_scale.double().numpy()[p.layer, p.table[b, j // p.page], kv, j % p.page]
+                rows[b, kv] = p.keys(b, kv), p.values(b, kv), scales
+            k, v, scales = rows[b, kv]
+            j = np.concatenate([np.arange(i * p.page, (i + 1) * p.page) for i in lists[t, kv] if 0 <= i < p.width] or [np.zeros(0, int)]).astype(int)
+            j = j[(j >= lo) & (j <= hi)]
+            if not len(j):
+                out[h, :, t] = tol[h, :, t] = 0
+                continue
+            q = p.q[t, h].double().numpy()
+            s = k[j] @ q * scale
+            y = np.exp(s - s.max())
+            w, n = y / y.sum(), len(j)
+            off = (p.dim * 2.0 ** -23 + 2.0 ** -20) * (np.abs(k[j]) @ np.abs(q)).max() * scale
+            lost = 0.0
+            if scales is not None:
+                off += 2.0 ** -25 * np.abs(q).max() * np.abs(k[j]).sum(1).max() * scale
+                lost = 2.0 ** -24 * scales[j].max() * (np.abs(v[j]) / scales[j, None]).sum(0) / y.sum()
+            out[h, :, t] = w @ v[j]
+            tol[h, :, t] = (w @ np.abs(v[j])) * (2 * off + 2.0 ** -22 + 2.0 ** -23 + (4 * n + 32) * 2.0 ** -23) + lost
+    return out.reshape(-1, max(1, p.tokens)), tol.reshape(-1, max(1, p.tokens))

@@ -58,3 +58,14 @@ def test_no_call_leaves_its_operands(q_heads, kv_heads, dim, page, cache):
     run("weigh", [33, 2], [300, page], *shape, tol=3e-4, window=40)
     for inplace in (True, False):
         run("evict", [1, 1, 1], [300, page, 2 * page + 3], *shape, keep=120, first=3, recent=20, most=130, inplace=inplace)
+
+
+# (columns, heads of queries and of keys, dims): lists with several workgroups each, with four waves each, with one
+FORMS = [([1, 3], 4, 2, 64), ([2], 20, 1, 80), ([70], 4, 4, 16), ([140], 32, 2, 128), ([250], 4, 4, 48), ([250], 16, 4, 96)]
+
+
+@pytest.mark.parametrize("cache", ["bf16", "s8"])
+@pytest.mark.parametrize("news, q_heads, kv_heads, dim", FORMS)
+def test_weights_of_values_are_not_rounded(news, q_heads, kv_heads, dim, cache):
+    """Small scores of a few tokens, whose weights are all alike: a rounding of them to 16 bits is many times what binary32 is off by."""
+    run("selected", news, [20] * len(news), q_heads, kv_heads, dim, 16, cache, problem=dict(seed=4), pages=2, scale=0.01)
