@@ -40,8 +40,10 @@ def for_the_host(s: str) -> str:
 def build(force: bool = False) -> str:
     if not force and up_to_date():
         return LIB
-    src, obj = os.path.join(OUT, "src"), os.path.join(OUT, "obj")
-    shutil.rmtree(OUT, ignore_errors=True)
+    # (a folder of this process: several may build at once)
+    mine = os.path.join(OUT, str(os.getpid()))
+    src, obj = os.path.join(mine, "src"), os.path.join(mine, "obj")
+    shutil.rmtree(mine, ignore_errors=True)
     os.makedirs(src)
     os.makedirs(obj)
     for f in SOURCES + [f for f in os.listdir(CSRC) if f.endswith(".h")]:
@@ -59,8 +61,9 @@ def build(force: bool = False) -> str:
     objs = [os.path.join(obj, os.path.basename(f) + ".o") for f in files]
     with ThreadPoolExecutor(max(1, min(8, os.cpu_count() or 1))) as pool:
         list(pool.map(lambda fo: run([CXX, *flags, "-c", fo[0], "-o", fo[1]]), zip(files, objs)))
-    run([CXX, "-shared", "-fPIC", *objs, "-lpthread", "-o", LIB])
-    shutil.rmtree(obj, ignore_errors=True)
+    run([CXX, "-shared", "-fPIC", *objs, "-lpthread", "-o", os.path.join(mine, "lib.so")])
+    os.replace(os.path.join(mine, "lib.so"), LIB)
+    shutil.rmtree(mine, ignore_errors=True)
     return LIB
 
 

@@ -15,7 +15,7 @@ sys.path[:0] = [ROOT, os.path.dirname(HERE), HERE]
 import build_long_emu  # noqa: E402
 import torch  # noqa: E402
 
-from long_exact import limits  # noqa: E402
+from long_exact import compare, limits, plant  # noqa: E402
 from long_reference import POISON, Long, kept_of  # noqa: E402
 from paper_2306_16601_amd import cache_binding as cb  # noqa: E402
 
@@ -69,8 +69,10 @@ def random_lists(p, pages, causal, window, seed):
     return lists
 
 
-def selected(p, pages, tol=None, causal=True, window=0, scale=None, seed=0):
+def selected(p, pages, tol=None, causal=True, window=0, scale=None, seed=0, odd=None):
     """tol: of the sum of magnitudes; without one nothing is rounded to less than binary32."""
+    if odd:
+        plant(p, odd)
     cache, batch = described(p)
     T, scale = max(1, p.tokens), scale or p.dim ** -0.5
     lists = random_lists(p, pages, causal, window, seed)
@@ -79,6 +81,9 @@ def selected(p, pages, tol=None, causal=True, window=0, scale=None, seed=0):
     call("spmm_selected_work_bytes", cache, i64(T), how, i64(pages), ctypes.byref(n))
     out = Device(np.full((p.q_heads * p.dim, T), POISON, np.float32))
     call("spmm_cache_attend_selected", cache, i32(p.layer), batch, p.d["q"], i64(T), how, Device(lists), i64(pages), out, i64(T), Device(np.full(n.value, 255, np.uint8)), None)
+    if odd:
+        bad, *where = compare(out.back().astype(np.float64), p, lists, scale, causal, window)
+        return {"bad": bad, "where": where}
     ref, mag = p.selected_wanted(lists, scale, causal=causal, window=window) if tol else limits(p, lists, scale, causal, window)
     return compared(out.back(), np.where(np.isnan(mag), POISON, ref), np.where(np.isnan(mag), 0, mag) * (tol or 1))
 

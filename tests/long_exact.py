@@ -41,3 +41,34 @@ def limits(p, lists, scale, causal=True, window=0):
             out[h, :, t] = w @ v[j]
             tol[h, :, t] = (w @ np.abs(v[j])) * (2 * off + 2.0 ** -22 + 2.0 ** -23 + (4 * n + 32) * 2.0 ** -23) + lost
     return out.reshape(-1, max(1, p.tokens)), tol.reshape(-1, max(1, p.tokens))
+
+
+def plant(p, what):
+    """Puts into an 8-bit cache of one sequence: a scale that is not finite at the first token, and at the one in the middle of the new ones, which half of them see ("k nan",
+    "k inf", "v nan", "v inf"), or value scales that differ by many powers of two from page to page ("spread", "wide")."""
+    r = np.random.default_rng(9)
+    if what in ("spread", "wide"):
+        for i in range(p.width):
+            if 0 <= p.table[0, i] < p.pages:
+                p.v_scale[:, p.table[0, i]] *= 2.0 ** int(r.integers(-24, 25) if what == "spread" else r.choice((-120, 0, 100)))
+        return
+    part, value = what.split()
+    scale = p.k_scale if part == "k" else p.v_scale
+    for j in (0, p.lens[0] - p.news[0] + p.news[0] // 2):
+        scale[p.layer, p.table[0, j // p.page], :, j % p.page] = float(value)
+
+
+def compare(got, p, lists, scale, causal=True, window=0):
+    """(number of results that are wrong, where): what is not finite in the definition has to be so, and nothing else."""
+    with np.errstate(all="ignore"):
+        ref, tol = limits(p, lists, scale, causal, window)
+        mine = np.zeros(got.shape, bool)
+        mine[:, [t for t, _, _ in p.columns()]] = True
+        fine = np.isfinite(ref)
+        bad = mine & ~np.where(fine, np.abs(got - ref) <= tol, ~np.isfinite(got))
+    return int(bad.sum()), np.argwhere(bad)[:3].tolist(), got[bad][:3].tolist(), ref[bad][:3].tolist(), tol[bad][:3].tolist()
+
+
+ODD = ["k nan", "k inf", "v nan", "v inf", "spread", "wide"]
+# heads of queries and keys, dims, new tokens: lists with four waves each, and with one; 16, 4, 2 streams and one of the columns that heads leave free
+MANY = [(4, 4, 64, 70), (4, 1, 128, 270), (10, 2, 48, 140), (16, 1, 96, 260), (6, 6, 64, 180), (16, 4, 64, 250), (32, 4, 32, 250), (64, 4, 128, 250)]

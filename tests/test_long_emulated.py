@@ -10,6 +10,7 @@ import pytest
 HERE = os.path.dirname(os.path.abspath(__file__))
 sys.path.insert(0, os.path.join(HERE, "emu"))
 import build_long_emu  # noqa: E402
+from long_exact import MANY, ODD  # noqa: E402
 
 pytestmark = pytest.mark.skipif(not build_long_emu.available(), reason="no host clang++ for the emulation build")
 
@@ -69,3 +70,9 @@ FORMS = [([1, 3], 4, 2, 64), ([2], 20, 1, 80), ([70], 4, 4, 16), ([140], 32, 2, 
 def test_weights_of_values_are_not_rounded(news, q_heads, kv_heads, dim, cache):
     """Small scores of a few tokens, whose weights are all alike: a rounding of them to 16 bits is many times what binary32 is off by."""
     run("selected", news, [20] * len(news), q_heads, kv_heads, dim, 16, cache, problem=dict(seed=4), pages=2, scale=0.01)
+
+
+@pytest.mark.parametrize("odd", ODD)
+@pytest.mark.parametrize("q_heads, kv_heads, dim, new", MANY[:6:2])
+def test_odd_scales_in_lists_of_8_bit_caches(q_heads, kv_heads, dim, new, odd):
+    run("selected", [new], [60], q_heads, kv_heads, dim, 16, "s8", problem=dict(seed=6), pages=4, scale=0.02, odd=odd)

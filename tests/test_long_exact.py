@@ -2,7 +2,7 @@
 import numpy as np
 import pytest
 
-from long_exact import limits
+from long_exact import MANY, ODD, compare, limits, plant
 from long_reference import POISON, Long
 from test_long_attend import attend, random_lists
 from test_long_emulated import FORMS
@@ -36,3 +36,16 @@ def test_longer_lists_and_larger_scores(news, past, page, pages, causal, window,
     lists = random_lists(p, pages, causal, window)
     for scale in (0.02, 0.125):
         held(p, lists, scale, causal, window)
+
+
+@gpu
+@pytest.mark.parametrize("odd", ODD)
+@pytest.mark.parametrize("q_heads, kv_heads, dim, new", MANY)
+@pytest.mark.parametrize("causal, window, pages", [(True, 0, 4), (True, 33, 9), (False, 0, 20)])
+def test_odd_scales_in_lists_of_8_bit_caches(q_heads, kv_heads, dim, new, causal, window, pages, odd):
+    """Lists that have a wave or four each, in which columns share a softmax over streams of keys."""
+    p = Long([new], [60], q_heads, kv_heads, dim, 16, "s8", seed=6)
+    plant(p, odd)
+    lists = random_lists(p, pages, causal, window)
+    bad = compare(attend(p, lists, scale=0.02, causal=causal, window=window).double().numpy(), p, lists, 0.02, causal, window)
+    assert bad[0] == 0, bad
