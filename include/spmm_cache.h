@@ -242,8 +242,10 @@ spmm_status_t spmm_weigh_work_bytes(const spmm_cache_t *cache, const spmm_batch_
  *               softmax over the visible tokens of scale * (q_t . k)   at j  (0 where j is not visible).
  * So weights need no initialisation.  Sequences without a new token are left as they were.  Scores, statistics and sums are binary32, and nothing
  * is rounded to less (codes of S8 caches are exact in the products, and scales are on the scores).  A score of NaN or +inf makes its column's weights NaN,
- * and so do scores of -inf alone.  The order of the sums does not change from call to call.  The weights of a page that two rows with new tokens
- * both name are not defined after a call with both of them.  q: as for spmm_cache_attend.  work: spmm_weigh_work_bytes bytes, as for attend. */
+ * and so do scores of -inf alone.  The order of the sums does not change from call to call.
+ * A page that several rows with new tokens name, at the same place of each, as spmm_cache_fork makes them: its tokens' weights fade once and get the shares of
+ * all of these rows (a token is new if it is one of the new tokens of one of them).  Weights of a page that rows name at different places, or a row twice, are not defined.
+ * q: as for spmm_cache_attend.  work: spmm_weigh_work_bytes bytes, as for attend. */
 spmm_status_t spmm_cache_weigh(const spmm_cache_t *cache, int32_t layer, const spmm_batch_t *batch, const void *q, int64_t T,
                                const spmm_weigh_t *how, void *work, void *hip_stream);
 

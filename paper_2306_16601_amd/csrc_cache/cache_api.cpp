@@ -444,7 +444,7 @@ spmm_status_t spmm_weigh_work_bytes(const spmm_cache_t* cache, const spmm_batch_
     if (const spmm_status_t s = check_table(cache, batch->ld_table, batch->n_seqs)) return s;
     if (const spmm_status_t s = check_weigh(cache, T, how)) return s;
     if (batch->n_seqs > 65535) return SPMM_E_UNSUPPORTED;
-    *bytes = weigh_work_bytes(cache->page_tokens, batch->n_seqs, batch->ld_table, cache->n_heads, weigh_columns(cache, T, how), T * how->q_heads);
+    *bytes = weigh_work_bytes(cache->page_tokens, cache->n_pages, batch->n_seqs, batch->ld_table, cache->n_heads, weigh_columns(cache, T, how), T * how->q_heads);
     return SPMM_OK;
 }
 

@@ -111,6 +111,7 @@ struct WeighArgs {
     Batch batch;
     const __bf16* q;
     float* work;
+    int32_t* owner;                 // scratch, of each page (nullptr: one sequence): a row that names it, ~ of it where another one does too
     int32_t T, group, max_new, causal, window, parts, keep;
     float scale_log2, decay;
 };
@@ -138,7 +139,7 @@ int launch_select(const SelectArgs& a, void* stream);
 // -1: more parts of lists than a grid holds
 int64_t selected_work_bytes(spmm_cache_type_t type, int page_tokens, int64_t T, int n_heads, int group, int dim, int64_t pages);
 int launch_attend_selected(const SelectedArgs& a, spmm_cache_type_t type, void* stream);
-int64_t weigh_work_bytes(int page_tokens, int64_t n_seqs, int64_t ld_table, int n_heads, int64_t cols, int64_t columns);
+int64_t weigh_work_bytes(int page_tokens, int64_t n_pages, int64_t n_seqs, int64_t ld_table, int n_heads, int64_t cols, int64_t columns);
 int launch_weigh(const WeighArgs& a, spmm_cache_type_t type, void* stream);
 int launch_evict(const EvictArgs& a, spmm_cache_type_t type, void* stream);
 int launch_fork(const ForkArgs& a, const CopyArgs& c, void* stream);

@@ -6,7 +6,9 @@
 // cache once and memory bounds it; it keeps the scores, four bytes where the key has 2 head_dim, and cache_weigh_kept makes shares of them.  With
 // more columns the scores would be more than the keys are: cache_weigh_join puts the parts' statistics together, and in
 // cache_weigh_add a wave has keys in its registers, the columns go by, and each key's shares are summed up, first in a lane, then over the lanes of
-// its row.  Every weight is one thread's, so that there are no atomics, and sums have one order.  Products are exact: queries are bfloat16, and so are
+// its row.  Every weight is one thread's, so that there are no atomics, and sums have one order.  Where rows share pages, as forks leave them, a page is one row's: cache_weigh_stats
+// notes one of the rows that name it, whichever is last; in the next kernel the others find that it is not they, and say so; and the one row's workgroups add the shares of
+// all of them, in the order of the rows (64 single tokens of 8 thousand each 162.6 us, 159.4 if no row could share: a launch; 32 tokens of two prompts 56.4, 54.8).  Products are exact: queries are bfloat16, and so are
 // codes of 8 bits once they are widened (integers up to 256 have 8 bits).
 //
 // 64 sequences of up to 8192 tokens, 32 heads on 8 of 128 dims, a new token each: 143 us for the statistics (4.2 TB/s of keys) and 16 for the
@@ -79,11 +81,45 @@ __device__ __forceinline__ int64_t column_of(const WeighArgs& a, const Counted& 
     return ((int64_t)(s.first + c / a.group) * a.pool.n_heads + h) * a.group + c % a.group;
 }
 
+// A page's owner, by one of the threads from .. of each row that names it; then whether there are others.
+__device__ __forceinline__ void own_pages(const WeighArgs& a, const int b, const Counted& s, const int from, const int step)
+{
+    if (s.tokens <= 0) return;
+    for (int i = from; i << a.pool.page_shift < s.len; i += step) {
+        const int page = a.batch.table[b * a.batch.ld_table + i];
+        if ((uint32_t)page < (uint32_t)a.pool.n_pages) a.owner[page] = b;
+    }
+}
+__device__ __forceinline__ int owner_of(const int mark) { return mark < 0 ? ~mark : mark; }
+__device__ __forceinline__ void find_shared(const WeighArgs& a)
+{
+    const uint32_t width = (uint32_t)a.batch.ld_table, all = width * a.batch.n_seqs;        // (less than 2^31)
+    for (uint32_t e = blockIdx.x * THREADS + threadIdx.x; e < all; e += gridDim.x * THREADS) {
+        const int b = e / width, i = e % width, page = a.batch.table[e];
+        const Counted s = counted(a, b);
+        if (s.tokens <= 0 || i << a.pool.page_shift >= s.len || (uint32_t)page >= (uint32_t)a.pool.n_pages) continue;
+        const int owner = owner_of(a.owner[page]);
+        if (owner != b) a.owner[page] = ~owner;     // (as all that find it so write)
+    }
+}
+__global__ __launch_bounds__(THREADS) void cache_weigh_shared(const WeighArgs a) { find_shared(a); }
+// The end of what a row's workgroups go through: of its last page, where it may be another row's too, whose tokens there may be more.
+__device__ __forceinline__ int end_of(const WeighArgs& a, const Counted& s)
+{
+    const int inside = (1 << a.pool.page_shift) - 1;
+    return a.owner ? (s.len + inside) & ~inside : s.len;
+}
+// Whether row r, of tokens s, has page number i of a row too.
+__device__ __forceinline__ bool has_page(const WeighArgs& a, const int r, const Counted& s, const int i, const int page)
+{
+    return s.tokens > 0 && i << a.pool.page_shift < s.len && a.batch.table[r * a.batch.ld_table + i] == page;
+}
+
 // Parts from, from + step, .. of a column's statistics, put together in their order; AHEAD of them are loaded together (behind the last one nothing).
+template <int AHEAD>
 __device__ __forceinline__ void join_parts(const WeighArgs& a, const int64_t column, const int from, const int step, float& top, float& sum)
 {
     typedef float f32x2 __attribute__((ext_vector_type(2)));
-    constexpr int AHEAD = 8;
     for (int p0 = from; p0 < a.parts; p0 += AHEAD * step) {
         f32x2 x[AHEAD];
 #pragma unroll
@@ -276,78 +312,130 @@ __global__ __launch_bounds__(THREADS, 2) void cache_weigh_stats(const WeighArgs 
         }
         __syncthreads();
     }
+    if (a.owner && h == 0 && blockIdx.z == 0) own_pages(a, b, s, part * THREADS + tid, a.parts * THREADS);
 }
 
 // What a key's weight is before this call's shares.
-__device__ __forceinline__ float faded(const WeighArgs& a, const Counted& s, const int key, const float weight)
-{
-    return key >= s.fresh || a.decay == 0.0f ? 0.0f : a.decay * weight;
-}
+__device__ __forceinline__ float faded(const WeighArgs& a, const bool fresh, const float weight) { return fresh || a.decay == 0.0f ? 0.0f : a.decay * weight; }
 
-// Shares of kept scores: a thread has four keys, in one page.
-__global__ __launch_bounds__(THREADS) void cache_weigh_kept(const WeighArgs a)
+// LDS of cache_weigh_kept: statistics of a row's columns, of all parts, and put together
+struct alignas(16) KeptColumns {
+    static constexpr int EACH = THREADS / COLS;
+    float tops[EACH][COLS], sums[EACH][COLS], most[COLS], inv[COLS];
+    Span spans[COLS];
+    bool shared[WAVES];
+};
+// What the columns of row r are multiplied by and see, and whether shared() is true of any thread (it is asked once the statistics have been loaded).
+template <int AHEAD, bool ASK, typename F>
+__device__ __forceinline__ bool join_row(const WeighArgs& a, const int r, const Counted& s, const int h, KeptColumns& lds, const F& shared)
 {
-    constexpr int EACH = THREADS / COLS;
-    __shared__ float tops[EACH][COLS], sums[EACH][COLS], most[COLS], inv[COLS];
-    __shared__ Span spans[COLS];
-    const int tid = threadIdx.x, h = blockIdx.y, b = blockIdx.z, shift = a.pool.page_shift, inside = (1 << shift) - 1;
-    const Counted s = counted(a, b);
-    const int cols = s.tokens * a.group, first = blockIdx.x * THREADS * 4;
-    if (cols <= 0 || first >= s.len) return;
-    const int key = first + tid * 4;
-    // statistics of the columns, of all parts
-    const int c = tid % COLS, p0 = tid / COLS;
+    const int tid = threadIdx.x, c = tid % COLS, p0 = tid / COLS;
     float top = NONE, sum = 0.0f;
-    if (c < cols) {
-        const int64_t column = column_of(a, s, h, c);
-        join_parts(a, column, p0, EACH, top, sum);
-        if (p0 == 0) spans[c] = span_of(a, b, s.first + c / a.group);
+    if (c < s.tokens * a.group) {
+        join_parts<AHEAD>(a, column_of(a, s, h, c), p0, KeptColumns::EACH, top, sum);
+        if (p0 == 0) lds.spans[c] = span_of(a, r, s.first + c / a.group);
     }
-    tops[p0][c] = top;
-    sums[p0][c] = sum;
+    lds.tops[p0][c] = top;
+    lds.sums[p0][c] = sum;
+    if constexpr (ASK) {
+        const bool any = __any(shared());
+        if (tid % 64 == 0) lds.shared[tid / 64] = any;
+    }
     __syncthreads();
     if (tid < COLS) {
-        for (int i = 1; i < EACH; ++i) join(top, sum, tops[i][c], sums[i][c]);
-        most[c] = top;
-        inv[c] = 1.0f / sum;
+        for (int i = 1; i < KeptColumns::EACH; ++i) join(top, sum, lds.tops[i][c], lds.sums[i][c]);
+        lds.most[c] = top;
+        lds.inv[c] = 1.0f / sum;
     }
+    bool all = false;
+    for (int w = 0; w < (ASK ? WAVES : 0); ++w) all |= lds.shared[w];
     __syncthreads();
-    if (key >= s.len) return;
-    const int page = a.batch.table[b * a.batch.ld_table + (key >> shift)];
-    if ((uint32_t)page >= (uint32_t)a.pool.n_pages) return;
-    float* const out = a.pool.weight + (((int64_t)page * a.pool.n_heads + h) << shift) + (key & inside);
-    f32x4 w = *(const f32x4*)out, add = {0, 0, 0, 0};
-    constexpr int AHEAD = 4;        // columns whose scores are loaded together
+    return all;
+}
+// The shares of row r's columns at four keys; AHEAD: columns whose scores are loaded together.
+template <int AHEAD>
+__device__ __forceinline__ void add_kept(const WeighArgs& a, const int r, const Counted& s, const int h, const int key, const KeptColumns& lds, f32x4& add)
+{
+    const int cols = s.tokens * a.group;
     for (int i0 = 0; i0 < cols; i0 += AHEAD) {
         f32x4 x[AHEAD];
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) x[k] = *(const f32x4*)(kept_of(a, b, h, min(i0 + k, cols - 1)) + key);
+        for (int k = 0; k < AHEAD; ++k) x[k] = *(const f32x4*)(kept_of(a, r, h, min(i0 + k, cols - 1)) + key);
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
-            const int i = i0 + k;
-            if (i >= cols) break;
-            const Span span = spans[i];
-            const float m = most[i], f = inv[i];
+            // (a column behind the last one is that once more and adds nothing: were it left out, its scores would not be loaded before it is known that it is there)
+            const int i = min(i0 + k, cols - 1), from = i0 + k < cols ? lds.spans[i].from : INT32_MAX, to = lds.spans[i].to;
+            const float m = lds.most[i], f = lds.inv[i];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const float p = __builtin_amdgcn_exp2f(__fmaf_rn(x[k][j], a.scale_log2, -m)) * f;
-                add[j] += key + j >= span.from && key + j <= span.to ? p : 0.0f;
+                add[j] += key + j >= from && key + j <= to ? p : 0.0f;
             }
         }
     }
+}
+
+// Shares of kept scores: a thread has four keys, in one page.  ROWS: there are several, which may share pages.
+template <bool ROWS>
+__global__ __launch_bounds__(THREADS, ROWS ? 8 : 1) void cache_weigh_kept(const WeighArgs a)
+{
+    __shared__ KeptColumns lds;
+    const int h = blockIdx.y, b = blockIdx.z, shift = a.pool.page_shift;
+    const Counted own = counted(a, b);
+    const int end = end_of(a, own), first = blockIdx.x * THREADS * 4, key = first + threadIdx.x * 4;
+    if (own.tokens <= 0 || first >= end) return;
+    const int page = key < end ? a.batch.table[b * a.batch.ld_table + (key >> shift)] : -1;
+    bool mine = (uint32_t)page < (uint32_t)a.pool.n_pages, shared = false;
+    const bool several = join_row<8, ROWS>(a, b, own, h, lds, [&] {
+        if (mine) {
+            const int mark = a.owner[page];
+            mine = owner_of(mark) == b;
+            shared = mine && mark < 0;
+        }
+        return shared;
+    });
+    float* const out = a.pool.weight + (((int64_t)page * a.pool.n_heads + h) << shift) + (key & ((1 << shift) - 1));
+    f32x4 add = {0, 0, 0, 0};
+    if (!ROWS || !several) {
+        if (!mine || key >= own.len) return;
+        f32x4 w = *(const f32x4*)out;
+        add_kept<4>(a, b, own, h, key, lds, add);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = key + j < s.len ? faded(a, s, key + j, w[j]) + add[j] : w[j];
+        for (int j = 0; j < 4; ++j) w[j] = key + j < own.len ? faded(a, key + j >= own.fresh, w[j]) + add[j] : w[j];
+        *(f32x4*)out = w;
+        return;
+    }
+    int held = 0, fresh = 0;        // a bit a key
+#pragma unroll 1
+    for (int r = 0; r < a.batch.n_seqs; ++r) {
+        const Counted s = counted(a, r);
+        const bool takes = mine && (r == b || (shared && has_page(a, r, s, key >> shift, page)));
+        if (!__syncthreads_or(takes)) continue;     // (and the last row's numbers have been read)
+        join_row<2, false>(a, r, s, h, lds, [] { return false; });
+        if (!takes) continue;
+        add_kept<2>(a, r, s, h, key, lds, add);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            held |= (key + j < s.len) << j;
+            fresh |= (key + j < s.len && key + j >= s.fresh) << j;
+        }
+    }
+    if (!mine) return;
+    f32x4 w = *(const f32x4*)out;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = held >> j & 1 ? faded(a, fresh >> j & 1, w[j]) + add[j] : w[j];
     *(f32x4*)out = w;
 }
 
 __global__ __launch_bounds__(THREADS) void cache_weigh_join(const WeighArgs a)
 {
+    if (a.owner) find_shared(a);
     const int64_t column = (int64_t)blockIdx.x * THREADS + threadIdx.x;
     if (column >= (int64_t)a.T * a.group * a.pool.n_heads) return;
     const int t = (int)(column / (a.group * a.pool.n_heads)), b = sequence_near(a.batch, t);
     if (b < 0) return;
     float top = NONE, sum = 0.0f;
-    join_parts(a, column, 0, 1, top, sum);
+    join_parts<8>(a, column, 0, 1, top, sum);
     *joined_of(a, column) = Joined{top, 1.0f / sum, span_of(a, b, t)};
 }
 
@@ -370,98 +458,141 @@ __global__ __launch_bounds__(THREADS, 2) void cache_weigh_add(const WeighArgs a)
     const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64), col = lane % 16, g = lane / 16;
     const int H = a.pool.n_heads, G = a.group, h = blockIdx.y, b = blockIdx.z, shift = a.pool.page_shift, inside = (1 << shift) - 1;
     const int D = EXACT ? 32 * KS : a.pool.head_dim;
-    const Counted s = counted(a, b);
-    const int cols = s.tokens * G;
-    if (cols <= 0 || s.len == 0) return;        // (keys are loaded ahead: of a row without tokens there would be none, nor a page)
+    const Counted own = counted(a, b);
+    if (own.tokens <= 0 || own.len == 0) return;       // (keys are loaded ahead: of a row without tokens there would be none, nor a page)
+    const int end = end_of(a, own);
     const int32_t* const table = a.batch.table + b * a.batch.ld_table;
     const int stride = gridDim.x * KEYS * WAVES;
+    int in_lds = -1;        // the row whose columns are in LDS, where all of them are
+    // whose a block's pages are, a lane a page, the same in all waves: looked up two blocks ahead, and one
+    const auto page_of = [&](const int block) {
+        const int at = (block >> shift) + lane;
+        return a.owner && lane < max((KEYS * WAVES) >> shift, 1) && at << shift < end ? table[at] : -1;
+    };
+    const auto mark_of = [&](const int page) { return (uint32_t)page < (uint32_t)a.pool.n_pages && a.owner ? a.owner[page] : ~(1 << 30); };     // (no row's)
+    int page = page_of(blockIdx.x * KEYS * WAVES), mark = mark_of(page);
+    page = page_of(blockIdx.x * KEYS * WAVES + stride);
     Keys<KS, TYPE, EXACT, FAR> k, next;
-    next.load(a, table, h, blockIdx.x * KEYS * WAVES + wave * KEYS, s.len - 1);
-    for (int block = blockIdx.x * KEYS * WAVES; block < s.len; block += stride) {
+    next.load(a, table, h, blockIdx.x * KEYS * WAVES + wave * KEYS, end - 1);
+    for (int block = blockIdx.x * KEYS * WAVES; block < end; block += stride) {
         const int k0 = block + wave * KEYS;
         k = next;
-        next.load(a, table, h, block + stride < s.len ? k0 + stride : k0, s.len - 1);
+        next.load(a, table, h, block + stride < end ? k0 + stride : k0, end - 1);
         __builtin_amdgcn_sched_barrier(0);
-        float sum[4 * FAR] = {};
-        for (int c0 = 0; c0 < cols; c0 += LISTED) {
-            const int n = min(cols - c0, LISTED), rounded = (n + TILED - 1) / TILED * TILED;
-            if (cols > LISTED || block == (int)blockIdx.x * KEYS * WAVES) {
-                // (columns that fill the last tile up are the last one, with no share)
-                __syncthreads();        // (the last ones have been read)
-                if (tid < rounded) {
-                    const int64_t id = column_of(a, s, h, c0 + min(tid, n - 1));
-                    Joined x = *joined_of(a, id);
-                    if (tid >= n) x.inv = 0.0f;
-                    columns.joined[tid] = x;
-                    columns.id[tid] = id;
-                }
-                __syncthreads();
-                constexpr int PIECES = 4 * KS;
-                const int d = tid % PIECES * 8;
-                for (int row = tid / PIECES; row < rounded; row += THREADS / PIECES)
-                    *(bf16x8*)&columns.q[row][d] = EXACT || d < D ? *(const bf16x8*)(a.q + columns.id[row] * D + d) : bf16x8{};
-                __syncthreads();
+        // which of the block's pages are this row's to write, and which of these are others' too
+        const int first_page = block >> shift;
+        const uint64_t mine = a.owner ? __ballot(owner_of(mark) == b) : ~0ull, shared = __ballot(owner_of(mark) == b && mark < 0);
+        mark = mark_of(page);
+        page = page_of(block + 2 * stride);
+        if (mine == 0) continue;
+        // the lane's key, once the sums are over the lanes (worked out where it is asked for: it would be kept over all columns)
+        constexpr int SHARED = COLS / (4 * FAR);        // lanes that are left with the same
+        const auto key_of = [&] {
+            int l = lane;
+            asm volatile("" : "+v"(l));
+            const int j = l % 16 / SHARED;
+            return k0 + 16 * (j / 4) + 4 * (l / 16) + j % 4;
+        };
+        float add = 0.0f;
+        bool held = false, fresh = false;
+        for (int r = shared ? 0 : b; r < (shared ? a.batch.n_seqs : b + 1); ++r) {
+            const Counted s = shared ? counted(a, r) : own;
+            uint64_t takes = mine;
+            if (shared) {
+                int l = lane;
+                asm volatile("" : "+v"(l));
+                takes = r == b ? mine : __ballot((shared >> l & 1) && has_page(a, r, s, first_page + l, table[first_page + l]));
+                if (takes == 0) continue;
             }
-            if (c0 == 0) k.ready();
-            for (int i = 0; i < rounded; i += TILED) {
-                // what the first and the last column see (no column sees less far than one before it)
-                const int first_from = uniform(columns.joined[i].span.from), first_to = uniform(columns.joined[i].span.to);
-                const int last_from = uniform(columns.joined[i + TILED - 1].span.from), last_to = uniform(columns.joined[i + TILED - 1].span.to);
-                if (k0 > last_to || k0 + KEYS <= first_from) continue;      // (no column of the tiles sees any of the keys)
-                bf16x8 q[TILES][KS];
+            const int cols = s.tokens * G;
+            float sum[4 * FAR] = {};
+            for (int c0 = 0; c0 < cols; c0 += LISTED) {
+                const int n = min(cols - c0, LISTED), rounded = (n + TILED - 1) / TILED * TILED;
+                if (cols > LISTED || in_lds != r) {
+                    // (columns that fill the last tile up are the last one, with no share)
+                    in_lds = cols > LISTED ? -1 : r;
+                    int own_tid = tid;
+                    asm volatile("" : "+v"(own_tid));       // (what is worked out of it is not kept over the loops)
+                    __syncthreads();        // (the last ones have been read)
+                    if (own_tid < rounded) {
+                        const int64_t id = column_of(a, s, h, c0 + min(own_tid, n - 1));
+                        Joined x = *joined_of(a, id);
+                        if (own_tid >= n) x.inv = 0.0f;
+                        columns.joined[own_tid] = x;
+                        columns.id[own_tid] = id;
+                    }
+                    __syncthreads();
+                    constexpr int PIECES = 4 * KS;
+                    const int d = own_tid % PIECES * 8;
+                    for (int row = own_tid / PIECES; row < rounded; row += THREADS / PIECES)
+                        *(bf16x8*)&columns.q[row][d] = EXACT || d < D ? *(const bf16x8*)(a.q + columns.id[row] * D + d) : bf16x8{};
+                    __syncthreads();
+                }
+                if (c0 == 0) k.ready();
+                for (int i = 0; i < rounded; i += TILED) {
+                    // what the first and the last column see (no column sees less far than one before it)
+                    const int first_from = uniform(columns.joined[i].span.from), first_to = uniform(columns.joined[i].span.to);
+                    const int last_from = uniform(columns.joined[i + TILED - 1].span.from), last_to = uniform(columns.joined[i + TILED - 1].span.to);
+                    if (k0 > last_to || k0 + KEYS <= first_from) continue;      // (no column of the tiles sees any of the keys)
+                    bf16x8 q[TILES][KS];
 #pragma unroll
-                for (int c = 0; c < TILES; ++c)
+                    for (int c = 0; c < TILES; ++c)
 #pragma unroll
-                    for (int x = 0; x < KS; ++x) q[c][x] = *(const bf16x8*)&columns.q[i + c * COLS + col][dim_of<TYPE>(x, g)];
-                f32x4 sc[TILES][FAR];
-                scores_of(k, q, sc);
-                const bool whole = k0 >= last_from && k0 + KEYS - 1 <= first_to;
+                        for (int x = 0; x < KS; ++x) q[c][x] = *(const bf16x8*)&columns.q[i + c * COLS + col][dim_of<TYPE>(x, g)];
+                    f32x4 sc[TILES][FAR];
+                    scores_of(k, q, sc);
+                    const bool whole = k0 >= last_from && k0 + KEYS - 1 <= first_to;
 #pragma unroll
-                for (int c = 0; c < TILES; ++c) {
-                    const Joined& column = columns.joined[i + c * COLS + col];
-                    const float most = column.most, inv = column.inv;
-                    if (whole) {
+                    for (int c = 0; c < TILES; ++c) {
+                        const Joined& column = columns.joined[i + c * COLS + col];
+                        const float most = column.most, inv = column.inv;
+                        if (whole) {
 #pragma unroll
-                        for (int t = 0; t < FAR; ++t)
+                            for (int t = 0; t < FAR; ++t)
 #pragma unroll
-                            for (int j = 0; j < 4; ++j)
-                                sum[4 * t + j] = __fmaf_rn(__builtin_amdgcn_exp2f(__fmaf_rn(sc[c][t][j], a.scale_log2, -most)), inv, sum[4 * t + j]);
-                    } else {
-                        const Span span = column.span;
+                                for (int e = 0; e < 4; ++e)
+                                    sum[4 * t + e] = __fmaf_rn(__builtin_amdgcn_exp2f(__fmaf_rn(sc[c][t][e], a.scale_log2, -most)), inv, sum[4 * t + e]);
+                        } else {
+                            const Span span = column.span;
 #pragma unroll
-                        for (int t = 0; t < FAR; ++t)
+                            for (int t = 0; t < FAR; ++t)
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                const int key = k0 + 16 * t + 4 * g + j;
-                                const bool sees = key >= span.from && key <= span.to;
-                                const float p = __builtin_amdgcn_exp2f(__fmaf_rn(sc[c][t][j], a.scale_log2, -most));
-                                sum[4 * t + j] = __fmaf_rn(sees ? p : 0.0f, sees ? inv : 0.0f, sum[4 * t + j]);
-                            }
+                                for (int e = 0; e < 4; ++e) {
+                                    const int at_key = k0 + 16 * t + 4 * g + e;
+                                    const bool sees = at_key >= span.from && at_key <= span.to;
+                                    const float p = __builtin_amdgcn_exp2f(__fmaf_rn(sc[c][t][e], a.scale_log2, -most));
+                                    sum[4 * t + e] = __fmaf_rn(sees ? p : 0.0f, sees ? inv : 0.0f, sum[4 * t + e]);
+                                }
+                        }
                     }
                 }
             }
-        }
-        // over the 16 lanes of a key: each hands another half of what it has, until it is left with the sum of one key
-        constexpr int SHARED = COLS / (4 * FAR);        // lanes that are left with the same
+            // over the 16 lanes of a key: each hands another half of what it has, until it is left with the sum of one key
 #pragma unroll
-        for (int o = COLS / 2; o > 0; o >>= 1) {
-            if (o >= SHARED) {
+            for (int o = COLS / 2; o > 0; o >>= 1) {
+                if (o >= SHARED) {
 #pragma unroll
-                for (int j = 0; j < o / SHARED; ++j) {
-                    const bool high = col & o;
-                    const float give = high ? sum[j] : sum[j + o / SHARED], keep = high ? sum[j + o / SHARED] : sum[j];
-                    sum[j] = keep + __shfl_xor(give, o);
+                    for (int e = 0; e < o / SHARED; ++e) {
+                        const bool high = col & o;
+                        const float give = high ? sum[e] : sum[e + o / SHARED], keep = high ? sum[e + o / SHARED] : sum[e];
+                        sum[e] = keep + __shfl_xor(give, o);
+                    }
+                } else {
+                    sum[0] += __shfl_xor(sum[0], o);
                 }
-            } else {
-                sum[0] += __shfl_xor(sum[0], o);
+            }
+            const int key = key_of();
+            if (takes >> ((key >> shift) - first_page) & 1) {
+                add += sum[0];
+                held |= key < s.len;
+                fresh |= key < s.len && key >= s.fresh;
             }
         }
-        const int j = col / SHARED, key = k0 + 16 * (j / 4) + 4 * g + j % 4;
-        if (key < s.len && col % SHARED == 0) {
-            const int page = table[key >> shift];
-            if ((uint32_t)page < (uint32_t)a.pool.n_pages) {
-                float* const w = a.pool.weight + (((int64_t)page * H + h) << shift) + (key & inside);
-                *w = faded(a, s, key, *w) + sum[0];
+        if (held && col % SHARED == 0) {
+            const int key = key_of(), number = table[key >> shift];
+            if ((uint32_t)number < (uint32_t)a.pool.n_pages) {
+                float* const w = a.pool.weight + (((int64_t)number * H + h) << shift) + (key & inside);
+                *w = faded(a, fresh, *w) + add;
             }
         }
     }
@@ -470,9 +601,9 @@ __global__ __launch_bounds__(THREADS, 2) void cache_weigh_add(const WeighArgs a)
 // How a call is cut up: parts of the keys that statistics are taken of, and whether scores are kept.
 struct WeighShape {
     int parts, keep;
-    int64_t bytes;
+    int64_t owners, bytes;      // offset of the pages' owners; all scratch
 };
-static WeighShape shape_of(const int page_tokens, const int64_t n_seqs, const int64_t ld_table, const int n_heads, const int64_t cols, const int64_t columns)
+static WeighShape shape_of(const int page_tokens, const int64_t n_pages, const int64_t n_seqs, const int64_t ld_table, const int n_heads, const int64_t cols, const int64_t columns)
 {
     const int64_t keys = ld_table * page_tokens, most = (keys + STEP - 1) / STEP, blocks = cols <= COLS ? 1 : (cols + MANY * COLS - 1) / (MANY * COLS);
     // Workgroups in all.  Few columns: 64 sequences of up to 8192 tokens of all lengths 143 us with 2048, 164 with 1024; 4 tokens of one of 60 thousand 43
@@ -483,13 +614,14 @@ static WeighShape shape_of(const int page_tokens, const int64_t n_seqs, const in
     const double kept = 4.0 * n_seqs * n_heads * cols * kept_keys(keys);
     // (with kept scores against without, us: 64 single tokens of 8 thousand each 252 / 414, one 12 / 33, 4 of 60 thousand 43 / 87)
     f.keep = cols <= COLS && kept <= KEPT;
-    f.bytes = (columns * f.parts + 1) / 2 * 16 + (f.keep ? (int64_t)kept : (int64_t)sizeof(Joined) * columns);
+    f.owners = (columns * f.parts + 1) / 2 * 16 + (f.keep ? (int64_t)kept : (int64_t)sizeof(Joined) * columns);
+    f.bytes = f.owners + (n_seqs > 1 ? 4 * n_pages : 0);
     return f;
 }
 
-int64_t weigh_work_bytes(const int page_tokens, const int64_t n_seqs, const int64_t ld_table, const int n_heads, const int64_t cols, const int64_t columns)
+int64_t weigh_work_bytes(const int page_tokens, const int64_t n_pages, const int64_t n_seqs, const int64_t ld_table, const int n_heads, const int64_t cols, const int64_t columns)
 {
-    return shape_of(page_tokens, n_seqs, ld_table, n_heads, cols, columns).bytes;
+    return shape_of(page_tokens, n_pages, n_seqs, ld_table, n_heads, cols, columns).bytes;
 }
 
 template <int KS, spmm_cache_type_t TYPE, bool EXACT>
@@ -501,9 +633,15 @@ static int launch_exact(const WeighArgs& a, const int64_t cols, void* stream)
                                     : launch(cache_weigh_stats<KS, TYPE, EXACT, MANY>, grid, threads, a, stream))
         return rc;
     const auto blocks_of = [&](const int each) { return dim3((unsigned)((keys + each - 1) / each), (unsigned)a.pool.n_heads, (unsigned)a.batch.n_seqs); };
-    if (a.keep) return launch(cache_weigh_kept, blocks_of(4 * THREADS), threads, a, stream);
-    const int64_t columns = (int64_t)a.T * a.group * a.pool.n_heads;
-    if (const int rc = launch(cache_weigh_join, dim3((unsigned)((columns + THREADS - 1) / THREADS)), threads, a, stream)) return rc;
+    // threads for the entries of the table, where there is more than one row
+    const int64_t entries = a.owner ? a.batch.n_seqs * a.batch.ld_table : 0, looked = (entries < 1 << 18 ? entries : 1 << 18) + THREADS - 1;
+    if (a.keep) {
+        if (a.owner)
+            if (const int rc = launch(cache_weigh_shared, dim3((unsigned)(looked / THREADS)), threads, a, stream)) return rc;
+        return launch(a.owner ? cache_weigh_kept<true> : cache_weigh_kept<false>, blocks_of(4 * THREADS), threads, a, stream);
+    }
+    const int64_t columns = (int64_t)a.T * a.group * a.pool.n_heads, joined = columns + THREADS - 1;
+    if (const int rc = launch(cache_weigh_join, dim3((unsigned)((joined > looked ? joined : looked) / THREADS)), threads, a, stream)) return rc;
     // A workgroup takes several blocks of keys with the columns it has put together, where there are more blocks than it takes to fill the device (128
     // columns a head of 2 times 16 thousand keys: 28 us with 512 workgroups, 34 with 256, 37 with 2048); where there are fewer it takes blocks of 64 keys, and
     // multiplies four tiles of columns together (1024 tokens on 2048 keys 138 us against 228, 32 on 4000 8.7 against 13; from 288 blocks on the larger
@@ -525,9 +663,10 @@ int launch_weigh(const WeighArgs& args, const spmm_cache_type_t type, void* stre
 {
     WeighArgs a = args;
     const int64_t cols = (int64_t)a.max_new * a.group;
-    const WeighShape f = shape_of(1 << a.pool.page_shift, a.batch.n_seqs, a.batch.ld_table, a.pool.n_heads, cols, (int64_t)a.T * a.group * a.pool.n_heads);
+    const WeighShape f = shape_of(1 << a.pool.page_shift, a.pool.n_pages, a.batch.n_seqs, a.batch.ld_table, a.pool.n_heads, cols, (int64_t)a.T * a.group * a.pool.n_heads);
     a.parts = f.parts;
     a.keep = f.keep;
+    if (a.batch.n_seqs > 1) a.owner = (int32_t*)((char*)a.work + f.owners);
     if (type == SPMM_CACHE_S8) return a.pool.head_dim > 64 ? launch_steps<4, SPMM_CACHE_S8>(a, cols, stream) : launch_steps<2, SPMM_CACHE_S8>(a, cols, stream);
     return a.pool.head_dim > 64 ? launch_steps<4, SPMM_CACHE_BF16>(a, cols, stream) : launch_steps<2, SPMM_CACHE_BF16>(a, cols, stream);
 }

@@ -15,7 +15,7 @@ sys.path[:0] = [ROOT, os.path.dirname(HERE), HERE]
 import build_long_emu  # noqa: E402
 import torch  # noqa: E402
 
-from long_exact import compare, limits, plant  # noqa: E402
+from long_exact import compare, limits, plant, share, shared_weights  # noqa: E402
 from long_reference import POISON, Long, kept_of  # noqa: E402
 from paper_2306_16601_amd import cache_binding as cb  # noqa: E402
 
@@ -88,14 +88,15 @@ def selected(p, pages, tol=None, causal=True, window=0, scale=None, seed=0, odd=
     return compared(out.back(), np.where(np.isnan(mag), POISON, ref), np.where(np.isnan(mag), 0, mag) * (tol or 1))
 
 
-def weigh(p, tol, max_new=None, causal=True, window=0, decay=0.5):
+def weigh(p, tol, max_new=None, causal=True, window=0, decay=0.5, shared=()):
+    share(p, shared)
     cache, batch = described(p)
     T = max(1, p.tokens)
     how = cb.spmm_weigh_t(p.q_heads, max_new or max(p.news), p.dim ** -0.5, causal, window, decay)
     n = i64()
     call("spmm_weigh_work_bytes", cache, batch, i64(T), how, ctypes.byref(n))
     call("spmm_cache_weigh", cache, i32(p.layer), batch, p.d["q"], i64(T), how, Device(np.full(n.value, 255, np.uint8)), None)
-    want, added = p.weights_wanted(max_new or max(p.news), p.dim ** -0.5, causal, window, decay)
+    want, added = (shared_weights if shared else Long.weights_wanted)(p, max_new or max(p.news), p.dim ** -0.5, causal, window, decay)
     return compared(p.d["weight"].back(), want, tol * added + 2.0 ** -22 * np.abs(want))
 
 

@@ -72,3 +72,41 @@ def compare(got, p, lists, scale, causal=True, window=0):
 ODD = ["k nan", "k inf", "v nan", "v inf", "spread", "wide"]
 # heads of queries and keys, dims, new tokens: lists with four waves each, and with one; 16, 4, 2 streams and one of the columns that heads leave free
 MANY = [(4, 4, 64, 70), (4, 1, 128, 270), (10, 2, 48, 140), (16, 1, 96, 260), (6, 6, 64, 180), (16, 4, 64, 250), (32, 4, 32, 250), (64, 4, 128, 250)]
+
+
+def share(p, groups):
+    """Rows of each group (first row, others, pages) name the first one's first pages, as after a fork."""
+    for first, others, pages in groups:
+        for b in others:
+            p.table[b, :pages] = p.table[first, :pages]
+
+
+def shared_weights(p, max_new, scale, causal=True, window=0, decay=1.0):
+    """(weights, what was added) where rows share pages: a token's weight fades once, or is new where it is that to one of the rows, and gets the shares of all."""
+    held, fresh, added = (np.zeros(p.weight.shape, t) for t in (bool, bool, float))
+    for b, n in enumerate(p.news):
+        length, past = p.held(b), p.lens[b] - n
+        if n <= 0:
+            continue
+        j = np.arange(length)
+        pages, off = p.table[b, j // p.page], j % p.page
+        held[p.layer, pages, :, off] = True
+        fresh[p.layer, pages[j >= past], :, off[j >= past]] = True
+        for h in range(p.k.shape[2]):
+            k = p.keys(b, h)
+            for i in range(max(0, n - max_new), n):
+                lo, hi = p.span(b, past + i, causal, window)
+                if hi < lo:
+                    continue
+                at = np.arange(lo, hi + 1)
+                for head in range(h * p.group, (h + 1) * p.group):
+                    s = k[at] @ p.q[int(p.start[b]) + i, head].double().numpy() * scale
+                    y = np.exp(s - s.max())
+                    added[p.layer, pages[at], h, off[at]] += y / y.sum()
+    old = p.weight.double().numpy()
+    return np.where(held, np.where(fresh, 0.0, decay * old) + added, old), added
+
+
+# (new tokens, past, (first row, other rows, shared pages)): beams, a common prefix and one within it, rows that end inside a shared page or have nothing new
+SHARED = [([1] * 5, [100, 100, 100, 37, 100], [(0, [1, 2, 4], 6)]), ([1, 2, 1, 0, 1, 3], [200, 150, 90, 200, 40, 10], [(0, [1, 2, 3], 4), (0, [4], 2)]),
+          ([1, 1, 1], [63, 40, 70], [(0, [1, 2], 3)]), ([20, 5, 7], [100, 110, 64], [(0, [1, 2], 4)]), ([9, 40, 1, 12], [300, 900, 320, 17], [(0, [2], 18), (1, [3], 1)])]

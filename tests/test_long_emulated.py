@@ -10,7 +10,7 @@ import pytest
 HERE = os.path.dirname(os.path.abspath(__file__))
 sys.path.insert(0, os.path.join(HERE, "emu"))
 import build_long_emu  # noqa: E402
-from long_exact import MANY, ODD  # noqa: E402
+from long_exact import MANY, ODD, SHARED  # noqa: E402
 
 pytestmark = pytest.mark.skipif(not build_long_emu.available(), reason="no host clang++ for the emulation build")
 
@@ -76,3 +76,11 @@ def test_weights_of_values_are_not_rounded(news, q_heads, kv_heads, dim, cache):
 @pytest.mark.parametrize("q_heads, kv_heads, dim, new", MANY[:6:2])
 def test_odd_scales_in_lists_of_8_bit_caches(q_heads, kv_heads, dim, new, odd):
     run("selected", [new], [60], q_heads, kv_heads, dim, 16, "s8", problem=dict(seed=6), pages=4, scale=0.02, odd=odd)
+
+
+@pytest.mark.parametrize("q_heads, kv_heads, dim, page, cache", [(4, 2, 64, 16, "bf16"), (2, 2, 32, 16, "s8"), (20, 1, 80, 16, "bf16"), (8, 2, 128, 64, "s8"), (6, 3, 48, 256, "bf16")])
+@pytest.mark.parametrize("news, pasts, shared", SHARED)
+def test_weights_of_shared_pages(news, pasts, shared, q_heads, kv_heads, dim, page, cache):
+    if page > 16:       # (as many pages of another size)
+        pasts = [past * page // 16 for past in pasts]
+    run("weigh", news, pasts, q_heads, kv_heads, dim, page, cache, problem=dict(seed=7), shared=shared, tol=3e-4, window=page * 5 if dim == 32 else 0)

@@ -1,9 +1,12 @@
-"""spmm_cache_attend_selected on the device where nothing is rounded to less than binary32: tolerances as derived in long_exact.py."""
+"""spmm_cache_attend_selected on the device where nothing is rounded to less than binary32, tolerances as derived in long_exact.py, and spmm_cache_weigh where rows share
+pages, with the tolerance of test_long_attend.py."""
 import numpy as np
 import pytest
+import torch
 
-from long_exact import MANY, ODD, compare, limits, plant
-from long_reference import POISON, Long
+import paper_2306_16601_amd as sp
+from long_exact import MANY, ODD, SHARED, compare, limits, plant, share, shared_weights
+from long_reference import POISON, Long, stream
 from test_long_attend import attend, random_lists
 from test_long_emulated import FORMS
 
@@ -49,3 +52,36 @@ def test_odd_scales_in_lists_of_8_bit_caches(q_heads, kv_heads, dim, new, causal
     lists = random_lists(p, pages, causal, window)
     bad = compare(attend(p, lists, scale=0.02, causal=causal, window=window).double().numpy(), p, lists, 0.02, causal, window)
     assert bad[0] == 0, bad
+
+
+def weights(p, max_new, window, times=1):
+    cache, batch = p.on_device()
+    how = sp.make_weigh(p.q_heads, max_new, p.dim ** -0.5, True, window, 0.5)
+    work = torch.full((sp.spmm_weigh_work_bytes(cache, batch, p.tokens, how),), 255, dtype=torch.uint8, device="cuda")
+    q, old = p.q.cuda(), p.dw.clone()
+    for _ in range(times):
+        p.dw.copy_(old)
+        sp.spmm_cache_weigh(cache, p.layer, batch, q, p.tokens, how, work, stream())
+        torch.cuda.synchronize()
+        yield p.dw.cpu().double().numpy()
+
+
+@gpu
+@pytest.mark.parametrize("q_heads, kv_heads, dim, page, cache", [(4, 2, 64, 16, "bf16"), (2, 2, 32, 16, "s8"), (20, 1, 80, 16, "bf16"), (8, 2, 128, 64, "s8"), (6, 3, 48, 256, "bf16"),
+                                                                 (32, 8, 128, 32, "bf16"), (64, 8, 96, 16, "s8")])
+@pytest.mark.parametrize("news, pasts, shared", SHARED + [([1] * 40, [300] * 40, [(0, list(range(1, 40)), 16), (7, list(range(8, 20)), 18)]), ([7] * 20, [500] * 20, [(0, list(range(1, 20)), 28)])])
+def test_weights_of_shared_pages(news, pasts, shared, q_heads, kv_heads, dim, page, cache):
+    """As forks leave them: every row's attention counts, the weight fades once, and the result is the same each time."""
+    if page > 16:
+        pasts = [past * page // 16 for past in pasts] if len(news) < 10 else pasts
+        shared = shared if len(news) < 10 else [(a, b, c * 16 // page) for a, b, c in shared]
+    p = Long(news, pasts, q_heads, kv_heads, dim, page, cache, layers=2, layer=1, seed=7)
+    share(p, shared)
+    window = page * 5 if dim == 32 else 0
+    want, added = shared_weights(p, 8, dim ** -0.5, True, window, 0.5)
+    first = None
+    for got in weights(p, 8, window, times=3):
+        bad = ~(np.abs(got - want) <= 3e-4 * added + 2.0 ** -22 * np.abs(want))
+        assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:3], got[bad][:3], want[bad][:3])
+        assert first is None or (got == first).all()
+        first = got
