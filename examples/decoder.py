@@ -71,7 +71,7 @@ class Decoder:
         exact = torch.empty((HEADS * DIM, T), device="cuda")
         attend = sp.make_attend(HEADS, max(new), DIM ** -0.5, True, 0, "u8", SCALE, ZERO)
         look = sp.make_attend(HEADS, max(new), DIM ** -0.5, True, 0, "f32")
-        weigh, select = sp.make_weigh(HEADS, max(weighed, 1), DIM ** -0.5), sp.make_select(HEADS, max(listed, 2))
+        weigh, select = sp.make_weigh(HEADS, max(weighed, 1), DIM ** -0.5), sp.make_select(HEADS, max(listed, 1), int(listed > 1), 1)
         need = [sp.spmm_selected_work_bytes(self.cache, T, attend, listed) if listed else sp.spmm_attend_work_bytes(self.cache, len(new), T, attend)]
         need += [sp.spmm_weigh_work_bytes(self.cache, batch, T, weigh)] if weighed else []
         work = torch.empty(max(need), dtype=torch.uint8, device="cuda")
