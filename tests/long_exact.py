@@ -81,17 +81,19 @@ def share(p, groups):
             p.table[b, :pages] = p.table[first, :pages]
 
 
-def shared_weights(p, max_new, scale, causal=True, window=0, decay=1.0):
-    """(weights, what was added) where rows share pages: a token's weight fades once, or is new where it is that to one of the rows, and gets the shares of all."""
+def shared_weights(p, max_new, scale, causal=True, window=0, decay=1.0, off=None):
+    """(weights, what was added) where rows share pages: a token's weight fades once, or is new where it is that to one of the rows, and gets the shares of all.
+    off: an array that how far each may be off is added to (the errors of scores, powers and sums as above; products are exact in both types of cache)."""
     held, fresh, added = (np.zeros(p.weight.shape, t) for t in (bool, bool, float))
+    columns = np.zeros(p.weight.shape)
     for b, n in enumerate(p.news):
         length, past = p.held(b), p.lens[b] - n
         if n <= 0:
             continue
         j = np.arange(length)
-        pages, off = p.table[b, j // p.page], j % p.page
-        held[p.layer, pages, :, off] = True
-        fresh[p.layer, pages[j >= past], :, off[j >= past]] = True
+        pages, slots = p.table[b, j // p.page], j % p.page
+        held[p.layer, pages, :, slots] = True
+        fresh[p.layer, pages[j >= past], :, slots[j >= past]] = True
         for h in range(p.k.shape[2]):
             k = p.keys(b, h)
             for i in range(max(0, n - max_new), n):
@@ -102,7 +104,13 @@ def shared_weights(p, max_new, scale, causal=True, window=0, decay=1.0):
                 for head in range(h * p.group, (h + 1) * p.group):
                     s = k[at] @ p.q[int(p.start[b]) + i, head].double().numpy() * scale
                     y = np.exp(s - s.max())
-                    added[p.layer, pages[at], h, off[at]] += y / y.sum()
+                    added[p.layer, pages[at], h, slots[at]] += y / y.sum()
+                    columns[p.layer, pages[at], h, slots[at]] += 1
+                    if off is not None:
+                        worst = (np.abs(k[at]) @ np.abs(p.q[int(p.start[b]) + i, head].double().numpy())).max() * scale
+                        off[p.layer, pages[at], h, slots[at]] += y / y.sum() * (2 * (p.dim * 2.0 ** -23 + 2.0 ** -20) * worst + 2.0 ** -22 + (len(at) + 32) * 2.0 ** -23)
+    if off is not None:
+        off += (columns + 32) * 2.0 ** -23 * added + 2.0 ** -22 * p.weight.double().numpy() * held
     old = p.weight.double().numpy()
     return np.where(held, np.where(fresh, 0.0, decay * old) + added, old), added
 

@@ -54,9 +54,9 @@ def test_odd_scales_in_lists_of_8_bit_caches(q_heads, kv_heads, dim, new, causal
     assert bad[0] == 0, bad
 
 
-def weights(p, max_new, window, times=1):
+def weights(p, max_new, window, times=1, scale=None):
     cache, batch = p.on_device()
-    how = sp.make_weigh(p.q_heads, max_new, p.dim ** -0.5, True, window, 0.5)
+    how = sp.make_weigh(p.q_heads, max_new, scale or p.dim ** -0.5, True, window, 0.5)
     work = torch.full((sp.spmm_weigh_work_bytes(cache, batch, p.tokens, how),), 255, dtype=torch.uint8, device="cuda")
     q, old = p.q.cuda(), p.dw.clone()
     for _ in range(times):
@@ -85,3 +85,17 @@ def test_weights_of_shared_pages(news, pasts, shared, q_heads, kv_heads, dim, pa
         assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:3], got[bad][:3], want[bad][:3])
         assert first is None or (got == first).all()
         first = got
+
+
+@gpu
+@pytest.mark.parametrize("cache", ["bf16", "s8"])
+@pytest.mark.parametrize("news, pasts, q_heads, kv_heads, dim, page, window", [
+    ([1, 1, 3], [300, 40, 700], 4, 2, 64, 16, 0), ([1], [3000], 8, 1, 128, 64, 0), ([30, 7], [50, 600], 6, 2, 80, 16, 0), ([100], [900], 32, 4, 128, 32, 250), ([5] * 9, [1500] * 9, 16, 8, 32, 64, 0)])
+def test_weights_are_off_by_what_binary32_is(news, pasts, q_heads, kv_heads, dim, page, window, cache):
+    p = Long(news, pasts, q_heads, kv_heads, dim, page, cache, seed=8)
+    for scale in (0.01, 0.1):
+        tol = np.zeros(p.weight.shape)
+        want, _ = shared_weights(p, 40, scale, True, window, 0.5, tol)
+        got, = weights(p, 40, window, scale=scale)
+        bad = ~(np.abs(got - want) <= tol)
+        assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:3], got[bad][:3], want[bad][:3], tol[bad][:3])
