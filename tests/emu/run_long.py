@@ -1,6 +1,6 @@
-"""Runs one call for long contexts through the host emulation and compares it with its definition (tests/long_reference.py).  Called as a subprocess: an access
+"""Runs calls for long contexts through the host emulation and compares them with their definitions (tests/long_reference.py).  Called as a subprocess, which prints a line for each: an access
 outside the operands ends it with a segmentation fault, a barrier that not all waves reach with the emulator's deadlock report.
-usage: run_long.py JSON     {"call": "selected" | "weigh" | "bounds" | "score" | "evict", "problem": arguments of Long, and what the call takes}"""
+usage: run_long.py JSON ...     {"call": "selected" | "weigh" | "bounds" | "score" | "evict", "problem": arguments of Long, and what the call takes}"""
 import ctypes
 import json
 import os
@@ -169,12 +169,13 @@ def compared(got, want, tol):
 
 
 def main():
-    case = json.loads(sys.argv[1])
-    p = Long(**case.pop("problem"))
-    for name in ("lens", "table"):
-        if name in case:
-            setattr(p, name, np.asarray(case.pop(name), np.int32) if name == "table" else case.pop(name))
-    print(json.dumps({"selected": selected, "weigh": weigh, "bounds": bounds, "score": score, "evict": evict}[case.pop("call")](p, **case)))
+    for text in sys.argv[1:]:
+        case = json.loads(text)
+        p = Long(**case.pop("problem"))
+        for name in ("lens", "table"):
+            if name in case:
+                setattr(p, name, np.asarray(case.pop(name), np.int32) if name == "table" else case.pop(name))
+        print(json.dumps({"selected": selected, "weigh": weigh, "bounds": bounds, "score": score, "evict": evict}[case.pop("call")](p, **case)), flush=True)
 
 
 if __name__ == "__main__":

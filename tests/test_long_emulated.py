@@ -20,12 +20,20 @@ def emulated():
     return build_long_emu.build()
 
 
-def run(call, news, pasts, q_heads, kv_heads, dim, page, cache, problem=(), **how):
-    case = {"call": call, "problem": dict(news=news, pasts=pasts, q_heads=q_heads, kv_heads=kv_heads, dim=dim, page=page, cache=cache, **dict(problem)), **how}
-    r = subprocess.run([sys.executable, os.path.join(HERE, "emu", "run_long.py"), json.dumps(case)], capture_output=True, text=True, timeout=600)
-    assert r.returncode == 0, "emulated run failed (rc %d):\n%s" % (r.returncode, r.stderr[-3000:])
-    said = json.loads(r.stdout.strip().splitlines()[-1])
-    assert said["bad"] == 0, said
+def case(call, news, pasts, q_heads, kv_heads, dim, page, cache, problem=(), **how):
+    return {"call": call, "problem": dict(news=news, pasts=pasts, q_heads=q_heads, kv_heads=kv_heads, dim=dim, page=page, cache=cache, **dict(problem)), **how}
+
+
+def run_all(cases):
+    r = subprocess.run([sys.executable, os.path.join(HERE, "emu", "run_long.py"), *map(json.dumps, cases)], capture_output=True, text=True, timeout=900)
+    said = [json.loads(line) for line in r.stdout.strip().splitlines()]
+    assert r.returncode == 0, "emulated run failed (rc %d) at %s:\n%s" % (r.returncode, cases[len(said)], r.stderr[-3000:])
+    for c, x in zip(cases, said):
+        assert x["bad"] == 0, (c, x)
+
+
+def run(*args, **how):
+    run_all([case(*args, **how)])
 
 
 # weights in bfloat16 and binary16: what test_long_attend.py holds
@@ -51,14 +59,10 @@ def test_weights_of_a_first_row_without_tokens(lens, cache):
 def test_no_call_leaves_its_operands(q_heads, kv_heads, dim, page, cache):
     """Pools without a spare page, tables and lists without a spare number."""
     shape = (q_heads, kv_heads, dim, page, cache, dict(spare=0, seed=3))
-    run("bounds", [1, 0, 5, 3 * page + 1], [0, 9, page - 2, page], *shape)
-    run("score", [1, 3, 1], [40, 3 * page, 5 * page + 3], *shape, pages=3)
-    run("score", [70, 3], [40, 3 * page], *shape, window=50, pad=3, pages=3)
-    run("selected", [1, 5], [600, page], *shape, pages=4, tol=TOL)
-    run("weigh", [1, 2], [600, page], *shape, tol=3e-4)
-    run("weigh", [33, 2], [300, page], *shape, tol=3e-4, window=40)
-    for inplace in (True, False):
-        run("evict", [1, 1, 1], [300, page, 2 * page + 3], *shape, keep=120, first=3, recent=20, most=130, inplace=inplace)
+    run_all([case("bounds", [1, 0, 5, 3 * page + 1], [0, 9, page - 2, page], *shape), case("score", [1, 3, 1], [40, 3 * page, 5 * page + 3], *shape, pages=3),
+             case("score", [70, 3], [40, 3 * page], *shape, window=50, pad=3, pages=3), case("selected", [1, 5], [600, page], *shape, pages=4, tol=TOL),
+             case("weigh", [1, 2], [600, page], *shape, tol=3e-4), case("weigh", [33, 2], [300, page], *shape, tol=3e-4, window=40)] +
+            [case("evict", [1, 1, 1], [300, page, 2 * page + 3], *shape, keep=120, first=3, recent=20, most=130, inplace=inplace) for inplace in (True, False)])
 
 
 # (columns, heads of queries and of keys, dims): lists with several workgroups each, with four waves each, with one
@@ -72,15 +76,13 @@ def test_weights_of_values_are_not_rounded(news, q_heads, kv_heads, dim, cache):
     run("selected", news, [20] * len(news), q_heads, kv_heads, dim, 16, cache, problem=dict(seed=4), pages=2, scale=0.01)
 
 
-@pytest.mark.parametrize("odd", ODD)
 @pytest.mark.parametrize("q_heads, kv_heads, dim, new", MANY[:6:2])
-def test_odd_scales_in_lists_of_8_bit_caches(q_heads, kv_heads, dim, new, odd):
-    run("selected", [new], [60], q_heads, kv_heads, dim, 16, "s8", problem=dict(seed=6), pages=4, scale=0.02, odd=odd)
+def test_odd_scales_in_lists_of_8_bit_caches(q_heads, kv_heads, dim, new):
+    run_all([case("selected", [new], [60], q_heads, kv_heads, dim, 16, "s8", problem=dict(seed=6), pages=4, scale=0.02, odd=odd) for odd in ODD])
 
 
 @pytest.mark.parametrize("q_heads, kv_heads, dim, page, cache", [(4, 2, 64, 16, "bf16"), (2, 2, 32, 16, "s8"), (20, 1, 80, 16, "bf16"), (8, 2, 128, 64, "s8"), (6, 3, 48, 256, "bf16")])
-@pytest.mark.parametrize("news, pasts, shared", SHARED)
-def test_weights_of_shared_pages(news, pasts, shared, q_heads, kv_heads, dim, page, cache):
-    if page > 16:       # (as many pages of another size)
-        pasts = [past * page // 16 for past in pasts]
-    run("weigh", news, pasts, q_heads, kv_heads, dim, page, cache, problem=dict(seed=7), shared=shared, tol=3e-4, window=page * 5 if dim == 32 else 0)
+def test_weights_of_shared_pages(q_heads, kv_heads, dim, page, cache):
+    # (as many pages of another size)
+    run_all([case("weigh", news, [past * page // 16 for past in pasts], q_heads, kv_heads, dim, page, cache, problem=dict(seed=7), shared=shared, tol=3e-4,
+                  window=page * 5 if dim == 32 else 0) for news, pasts, shared in SHARED])
