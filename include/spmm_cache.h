@@ -20,7 +20,9 @@
  *
  * Conventions are those of spmm.h: C linkage, statuses, outputs untouched on error, every pointer is said
  * to be host or device, device pointers stay the caller's until the launch that uses them has finished, and
- * launches are asynchronous on the stream that is handed over.  What lies in device memory (tables, lengths)
+ * launches are asynchronous on the stream that is handed over.  Structures may gain fields at their ends (as spmm_cache_t
+ * has: bounds, weight), and nothing says which a caller knows: callers are compiled against the header of the library
+ * that they load, and set what they do not use to 0.  What lies in device memory (tables, lengths)
  * cannot be checked by the host: the kernels bring it into range, so that a bad entry gives wrong values and
  * never an access outside the operands.
  */
@@ -175,7 +177,8 @@ spmm_status_t spmm_cache_work_bytes(const spmm_cache_t *cache, int64_t n_rows, i
  * spmm_cache_attend_selected   reads the pages of a list for each new token and key/value head instead of all of them.
  * spmm_cache_weigh adds up what attention each token gets, and spmm_cache_evict keeps the tokens that got most of it.
  * Limits (else SPMM_E_UNSUPPORTED): 65535 sequences or rows in spmm_cache_bounds, _weigh and _evict, T * n_heads <= 2^22 and lists of up to 2^20
- * pages in spmm_cache_score, _select and _attend_selected (2^40 numbers of lists in all), lds <= 2^30, n_layers * n_heads <= 2^20 in spmm_cache_evict.
+ * pages in spmm_cache_score, _select and _attend_selected (2^40 numbers of lists in all; in _attend_selected, with G = q_heads / n_heads, also
+ * T * n_heads * ceil(G / 16) * ceil(pages / 1024) < 2^24), lds <= 2^30, n_layers * n_heads <= 2^20 in spmm_cache_evict.
  * "Visible" is what it is in spmm_cache_attend (kv_len, causal, window), token by token; columns at a negative position see nothing. */
 
 /* Bounds of the pages that the batch's new tokens lie in (of layer `layer`): of each head and dim the largest and the
@@ -200,7 +203,9 @@ typedef struct {
  * page i of its sequence's row with a visible token, an upper bound (in S8 caches but for the bounds' rounding) of the products q . k of the page's keys:
  *   max over the query heads of h of   sum_d q_d > 0 ? q_d hi_d : q_d lo_d,
  * binary32 sums of products of the bounds hi, lo; NaN where a bound is.  Pages without a visible token, up to ld_table: -inf.  Columns of no
- * sequence are left as they were.  q: as for spmm_cache_attend.  (pages, first and last are not read, but checked.) */
+ * sequence are left as they were.  q: as for spmm_cache_attend.  (pages, first and last are not read, but checked.)
+ * One kernel is chosen, by the mean number of columns of a sequence: a batch that mixes chunks with single tokens is faster in two calls (63 single tokens
+ * and a chunk of 500, 8 thousand tokens each: 38 us, 73 in one), which give the same scores. */
 spmm_status_t spmm_cache_score(const spmm_cache_t *cache, int32_t layer, const spmm_batch_t *batch, const void *q, int64_t T,
                                const spmm_select_t *how, float *scores, int64_t lds, void *hip_stream);
 

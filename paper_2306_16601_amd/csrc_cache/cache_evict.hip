@@ -4,12 +4,12 @@
 // largest (cache_choose.h).  cache_evict_move: a workgroup moves a slice of a row's head, all of its tokens in their order.  A token never
 // goes to a later place than its own, so that what a step of tokens is written over has been read, where the pages are the same ones,
 // once the step itself has been read; slices (dims of keys, or of values) have nothing to do with each other.  Keys are moved 16 bytes a
-// lane.  Values, whose tokens are contiguous, are gathered one by one, tokens side by side in a wave, so that it finds them in a few lines
-// of memory: nearly all lines of the values are read wherever one token in sixteen stays.
+// lane.  Values, whose tokens are contiguous, go page by page through LDS, 16 dims of all tokens from the next one that stays on, where those that stay are picked
+// out and leave 16 bytes a lane: nearly all lines of the values are read wherever one token in sixteen stays.
 //
-// 8 rows of up to 12 thousand tokens in 8 bits, 8 layers of 8 heads of 128 dims, to 2048 each: 27 us to choose, 223 to move (386 MB read and 291
-// written by the counters, 3 TB/s; without the picks it takes as long, with more workgroups on a CU too: it is the memory's answer to runs of 64 bytes to 1 KB); 4 rows of 1000, 12 layers of 12 heads of 64 dims in
-// bfloat16, to 250: 7.1 and 26 (130 MB with the lines that are read whole, 5 TB/s).
+// 8 rows of up to 12 thousand tokens in 8 bits, 8 layers of 8 heads of 128 dims, to 2048 each: 24.6 us to choose, 221 to move (772 MB read and 291 written by the counters,
+// 4.8 TB/s, as a copy; without the picks it takes as long); 4 rows of 1000, 12 layers of 12 heads of 64 dims in bfloat16, to 250: 6.7 and 25.7 (98 MB read, 38 written, 5.3 TB/s
+// with what the last-level cache has of it).
 #include "cache_choose.h"
 
 #include <type_traits>
@@ -293,7 +293,7 @@ int launch_evict(const EvictArgs& a, const spmm_cache_type_t type, void* stream)
     const dim3 rows((unsigned)heads, (unsigned)a.n_rows);
     int rc;
     // As few waves and registers as hold a row, us, 4 (32) rows of 4 layers of 8 heads: 1000 tokens with 4 registers of 4 waves 5.9 (8.4), with 16 of
-    // them 7.8 (11.9); 4000 with 16 registers of 4 waves 10.1 (17), of 16 waves 12.6 (32); 8000 with 32 registers of 4 waves 18.8 (26.6), with 16 of 16 16.2 (43); 16000 with
+    // them 7.8 (11.9); 4000 with 16 registers of 4 waves 10.1 (17), of 16 waves 12.6 (32); 8000 with 32 registers of 4 waves 16.4 (25.8), with 16 of 16 16.5 (42.6); 16000 with
     // 16 registers of 16 waves 19.8, with weights read again at each pass 58; 32000 26.7 and 146.
     if (most <= 64 * 4 * 4) rc = launch(cache_evict_choose<4, 4>, rows, dim3(64 * 4), a, stream);
     else if (most <= 64 * 4 * 16) rc = launch(cache_evict_choose<4, 16>, rows, dim3(64 * 4), a, stream);

@@ -8,9 +8,9 @@
 // It needs each page's bounds once for all its columns, and writes a score each.  A chunk's waves multiply four tiles of queries with
 // each page, and a workgroup's four waves share the pages through LDS: lanes that lie side by side in the instruction's operand are
 // other pages, so that loads straight into it take a cache line a lane, and those, not bytes, bounded the kernel.  Scores of 500 columns of 32
-// heads for 970 pages of 8: 17.4 us (11 with neither loads nor stores), 25.1 with
+// heads for 970 pages of 8: 17.8 us (11 with neither loads nor stores), 25.1 with
 // loads into operands two steps ahead, 28 one step ahead.  A batch's next tokens, or a few columns each, have one tile, and there
-// each wave takes pages of its own: one token of 16 heads and 486 pages takes 3.9 us, of which a launch is 2.4.
+// each wave takes pages of its own: one token of 16 heads and 486 pages takes 4.0 us, of which a launch is 2.4.
 #include "cache_internal.h"
 
 #include <algorithm>
@@ -262,6 +262,8 @@ int launch_score(const ScoreArgs& a, void* stream)
     f.tokens = many ? 4 * per : a.T > 2 * (int64_t)a.batch.n_seqs ? per : 1;
     const int tokens = many ? f.tokens * WAVES : f.tokens, pages = many ? PAGES : PAGES * WAVES;      // of a workgroup, and of a step of it
     const int64_t blocks = ((int64_t)a.T + tokens - 1) / tokens * a.pool.n_heads, most = (a.batch.ld_table + pages - 1) / pages;
+    // 512 workgroups, or up to 8 steps: 500 columns and 970 pages 17.1 us, 17.1 with 256, 20.6 with 1024, 20.6 with up to 4 steps, 17.0 with 16; 64 single tokens of up to 8
+    // thousand 20.7, 21.1, 22.8, 22.8, 20.7; 4 times 2 columns of 100 thousand 31.7, 31.6, 34.8, 35.3, 31.7; 1024 columns of 30 thousand 56.8, 56.7, 56.8, 54.3, 53.3.
     const int64_t wanted = (blocks * most + 511) / 512, least = most / 65535 + 1;       // (a grid is at most 65535 high)
     f.steps = (int)std::max(std::min(wanted, (int64_t)8), least);
     const dim3 grid((unsigned)blocks, (unsigned)((most + f.steps - 1) / f.steps));

@@ -1,7 +1,7 @@
 // Which pages a new token reads: the first, the last, and those of the highest scores, in ascending order (cache_choose.h).
 //
 // A wave has a row of up to 1024 pages in its registers; longer ones take a workgroup, and those of more than 32 thousand pages are read
-// again at each pass.  Reading the scores once would take 13 us for 16000 rows of 970 of them; it takes 19.7:
+// again at each pass.  Reading the scores once would take 13 us for 16000 rows of 970 of them; it takes 21.1:
 // 600 vector instructions a row are 15 us of it.
 #include "cache_choose.h"
 

@@ -25,11 +25,11 @@ struct Selected {
 };
 
 // Waves that a list of an 8-bit cache has in launch_attend_lists, 1 or 4, or 0: it goes to the workgroups of cache_attend_selected.  One wave / four / those, us,
-// 16 pages of 64 of 15 thousand tokens: 32 heads on 8 of 128 dims 128 lists 37 / 14 / 17, 256 37 / 15 / 20, 768 39 / 33 / 35, 1024 40 / 41 / 43, 1280 62 / 49 / 53,
-// 2048 66 / 73 / 79, 2056 90 / 81 / 84, 4096 121 / 136 / 149, 8192 232 / 263 / 291; 64 pages 128 lists 110 / 33 / 29, 256 111 / 34 / 43, 2056 294 / 227 / 260; 16 heads of 64
-// dims 256 lists 21 / 10 / 14, 1024 23 / 23 / 25, 2048 31 / 38 / 44; 32 heads on 2, which leave no columns free, 256 lists 67 / 24 / 30, 4096 272 / 291 / 279.  Waves of 128 dims
+// 16 pages of 64 of 15 thousand tokens: 32 heads on 8 of 128 dims 128 lists 39 / 15 / 17, 256 39 / 16 / 22, 768 41 / 34 / 38, 1024 42 / 42 / 47, 1280 65 / 51 / 58,
+// 2048 66 / 75 / 83, 2056 91 / 79 / 88, 4096 117 / 134 / 150, 8192 222 / 258 / 290; 64 pages 128 lists 117 / 35 / 30, 256 118 / 37 / 45, 2056 302 / 236 / 264; 16 heads of 64
+// dims 256 lists 22 / 11 / 15, 1024 24 / 24 / 28, 2048 33 / 40 / 48; 32 heads on 2, which leave no columns free, 256 lists 42 / 18 / 24, 4096 162 / 183 / 177.  Waves of 128 dims
 // come in rounds of 1024 lists (one on each SIMD) of 24 us after 16, workgroups take 32 ns a list after 9.  (In bfloat16, where no codes are
-// widened, a wave each gains nothing: 2048 lists 127 / - / 121, 8192 472 / - / 466.)
+// widened, a wave each gained nothing: 2048 lists 127 / - / 121, 8192 472 / - / 466, measured with one term a weight.)
 inline int waves_of(const spmm_cache_type_t type, const int dim, const int64_t lists, const int64_t pages)
 {
     const int64_t rounds = (lists + 1023) / 1024;

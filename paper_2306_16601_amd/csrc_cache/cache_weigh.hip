@@ -11,8 +11,8 @@
 // all of them, in the order of the rows (64 single tokens of 8 thousand each 162.6 us, 159.4 if no row could share: a launch; 32 tokens of two prompts 56.4, 54.8).  Products are exact: queries are bfloat16, and so are
 // codes of 8 bits once they are widened (integers up to 256 have 8 bits).
 //
-// 64 sequences of up to 8192 tokens, 32 heads on 8 of 128 dims, a new token each: 143 us for the statistics (4.2 TB/s of keys) and 16 for the
-// kept scores' shares; 32 tokens of 2 prompts of 16 thousand (256 columns): 22.7 + 4.2 + 28.5, where the keys are read twice (14 us each time at the
+// 64 sequences of up to 8192 tokens, 32 heads on 8 of 128 dims, a new token each: 142.6 us for the statistics (4.2 TB/s of keys; in 8 bits 121, 2.5 TB/s) and 16.4 for the
+// kept scores' shares; 32 tokens of 2 prompts of 16 thousand (256 columns): 21.7 + 4.7 + 29.3 (in 8 bits 31.5 + 4.3 + 33.6), where the keys are read twice (14 us each time at the
 // rate of a copy), and latencies, not the instructions, are what is left.
 #include "cache_attend.h"
 
@@ -606,13 +606,13 @@ struct WeighShape {
 static WeighShape shape_of(const int page_tokens, const int64_t n_pages, const int64_t n_seqs, const int64_t ld_table, const int n_heads, const int64_t cols, const int64_t columns)
 {
     const int64_t keys = ld_table * page_tokens, most = (keys + STEP - 1) / STEP, blocks = cols <= COLS ? 1 : (cols + MANY * COLS - 1) / (MANY * COLS);
-    // Workgroups in all.  Few columns: 64 sequences of up to 8192 tokens of all lengths 143 us with 2048, 164 with 1024; 4 tokens of one of 60 thousand 43
-    // and 39 (more parts, more to join).  Many: 128 columns a head of 2 times 16 thousand 28 us (with the join) with 256, 30 with 512, 37 with 1024, 54 with 2048.
+    // Workgroups in all.  Few columns: 64 sequences of up to 8192 tokens of all lengths 142 us with 2048, 162 with 1024; 4 tokens of one of 60 thousand 42
+    // and 39 (more parts, more to join).  Many: 128 columns a head of 2 times 16 thousand 27 us (with the join) with 256, 29 with 512, 37 with 1024, 43 with 2048.
     const int64_t want = (cols <= COLS ? 2048 : 256) / (n_seqs * n_heads * blocks);
     WeighShape f;
     f.parts = (int)(want < 1 ? 1 : want < most ? want : most);
     const double kept = 4.0 * n_seqs * n_heads * cols * kept_keys(keys);
-    // (with kept scores against without, us: 64 single tokens of 8 thousand each 252 / 414, one 12 / 33, 4 of 60 thousand 43 / 87)
+    // (with kept scores against without, us: 64 single tokens of 8 thousand each 163 / 303, one 12 / 22, 4 of 60 thousand 42 / 87)
     f.keep = cols <= COLS && kept <= KEPT;
     f.owners = (columns * f.parts + 1) / 2 * 16 + (f.keep ? (int64_t)kept : (int64_t)sizeof(Joined) * columns);
     f.bytes = f.owners + (n_seqs > 1 ? 4 * n_pages : 0);
@@ -643,9 +643,9 @@ static int launch_exact(const WeighArgs& a, const int64_t cols, void* stream)
     const int64_t columns = (int64_t)a.T * a.group * a.pool.n_heads, joined = columns + THREADS - 1;
     if (const int rc = launch(cache_weigh_join, dim3((unsigned)((joined > looked ? joined : looked) / THREADS)), threads, a, stream)) return rc;
     // A workgroup takes several blocks of keys with the columns it has put together, where there are more blocks than it takes to fill the device (128
-    // columns a head of 2 times 16 thousand keys: 28 us with 512 workgroups, 34 with 256, 37 with 2048); where there are fewer it takes blocks of 64 keys, and
-    // multiplies four tiles of columns together (1024 tokens on 2048 keys 138 us against 228, 32 on 4000 8.7 against 13; from 288 blocks on the larger
-    // ones are ahead, 26 against 29).
+    // columns a head of 2 times 16 thousand keys: 30 us with 512 workgroups, 37 with 256, 38 with 2048); where there are fewer it takes blocks of 64 keys, and
+    // multiplies four tiles of columns together (1024 tokens on 2048 keys 138 us against 235, 32 on 4000 9.0 against 13.4; with 288 blocks they are
+    // level, 18 against 19).
     dim3 all = blocks_of(16 * 4 * WAVES);
     const int64_t others = (int64_t)all.y * all.z, enough = (512 + others - 1) / others;
     if (all.x * others < 256) return launch(cache_weigh_add<KS, TYPE, EXACT, 1>, blocks_of(16 * WAVES), threads, a, stream);

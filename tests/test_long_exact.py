@@ -99,3 +99,18 @@ def test_weights_are_off_by_what_binary32_is(news, pasts, q_heads, kv_heads, dim
         got, = weights(p, 40, window, scale=scale)
         bad = ~(np.abs(got - want) <= tol)
         assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:3], got[bad][:3], want[bad][:3], tol[bad][:3])
+
+
+@gpu
+@pytest.mark.parametrize("q_heads, kv_heads, dim", [(8, 2, 64), (16, 4, 128), (40, 2, 48)])
+def test_scores_of_a_mixed_batch_are_those_of_two_calls(q_heads, kv_heads, dim):
+    p = Long([1] * 40 + [90], [300] * 41, q_heads, kv_heads, dim, 16, seed=10)
+    cache, whole = p.on_device()
+    start, lens, table = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in (p.start, p.lens, p.table))
+    how, q, width, T = sp.make_select(q_heads, 1, 0, 0, True, 0), p.q.cuda(), p.width, p.tokens
+    one, two = (torch.zeros((T, kv_heads, width), device="cuda") for _ in range(2))
+    sp.spmm_cache_score(cache, 0, whole, q, T, how, one, width, stream())
+    sp.spmm_cache_score(cache, 0, sp.make_batch(start[:41], lens[:40], table[:40]), q, 40, how, two, width, stream())
+    sp.spmm_cache_score(cache, 0, sp.make_batch(start[40:] - 40, lens[40:], table[40:]), q[40:], T - 40, how, two[40:], width, stream())
+    torch.cuda.synchronize()
+    assert torch.equal(one, two)
